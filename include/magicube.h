@@ -527,6 +527,100 @@ int mc_sparse_attention_static(const void *Q_dev, const void *Km_dev, const void
                                float s_p, mc_out_type out_type, const mc_options *options, void *O_dev, void *stream);
 
 /* ------------------------------------------------------------------------------------
+ * Decoding: the operators around the layer once a prompt is in.  Rotary positions of queries and keys, a paged cache that
+ * holds keys and values in 8 or 4 bits, and attention of new tokens over it.
+ * Real-valued tensors of these calls are fp32, fp16 or bf16 (mc_type), (token, head, element) with unit stride along the
+ * elements and any strides of tokens and heads, in ELEMENTS.  Positions, slots, page tables and lengths are device arrays,
+ * which the host cannot check: what each call does with values out of range is said there, and never is an access out of bounds.
+ * ---------------------------------------------------------------------------------- */
+typedef enum { MC_F32 = 0, MC_F16 = 1, MC_BF16 = 2 } mc_type;
+
+/* Inverse frequencies of rotary positions, on the host: inv_freq[j] = base^(-2j / rot), j < rot / 2 (rot even and positive,
+ * base positive), for a context `factor` >= 1 times the one a model was trained with:
+ *   MC_ROPE_PLAIN   as they are (factor and what follows are not looked at)
+ *   MC_ROPE_LINEAR  all divided by factor
+ *   MC_ROPE_BASE    base * factor^(rot / (rot - 2)) in the place of base: the fastest stays, the slowest is divided by factor (rot >= 4)
+ *   MC_ROPE_PARTS   pair j makes r_j = original * inv_freq[j] / (2 pi) turns over the `original` tokens of training; it stays where r_j >= high, is
+ *                   divided by factor where r_j <= low, and in between is mixed linearly in r_j (0 <= low < high; 1 and 32 are usual)
+ * *magnitude (if not NULL): what queries and keys are multiplied by beside, 0.1 ln(factor) + 1 for MC_ROPE_PARTS, else 1. */
+typedef enum { MC_ROPE_PLAIN = 0, MC_ROPE_LINEAR = 1, MC_ROPE_BASE = 2, MC_ROPE_PARTS = 3 } mc_rope_scaling;
+int mc_rope_frequencies(int rot, double base, mc_rope_scaling scaling, double factor, double original, double low, double high,
+                        double *inv_freq_host, double *magnitude_host);
+
+/* Rotary positions: elements (x1, x2) of pair j of every head become
+ *   y1 = magnitude (x1 cos a - x2 sin a),  y2 = magnitude (x1 sin a + x2 cos a),  a = positions[token] * inv_freq[j],
+ * pair j being elements (j, j + rot/2), or (2j, 2j + 1) if `interleaved`; elements from rot on are copied.  `inverse` takes -a for a: with
+ * it the call is the gradient, dx from dy.  Angles are products in double precision, so far positions keep their phase; the rest is fp32.
+ *   x_dev, y_dev        tokens x heads x dim; y_dev may be x_dev with the same strides, else the two must not overlap
+ *   positions_dev       tokens int64, any values;  inv_freq_dev  rot / 2 doubles
+ * Any alignment; tensors whose pointers, strides and rot / 2 elements make whole 16-byte pieces are faster.  rot even, 0 <= rot <= dim;
+ * tokens = 0 is accepted. */
+int mc_rope(const void *x_dev, mc_type type, int64_t tokens, int heads, int dim, int64_t x_token_stride, int64_t x_head_stride,
+            const int64_t *positions_dev, const double *inv_freq_dev, int rot, int interleaved, float magnitude, int inverse,
+            void *y_dev, int64_t y_token_stride, int64_t y_head_stride, void *stream);
+
+/* A paged cache: names for device memory that the caller owns (no handle, nothing to destroy).
+ *   codes    pages x kv_heads x page_size x dk, `bits` each (8: int8; 4: two's-complement nibbles, element 2j in bits 3:0 of byte j)
+ *   scales   pages x kv_heads x page_size fp32: element = code * scale
+ * A token's place is a slot: page * page_size + place in the page.  page_size is a power of two from 16 to 4096, dk a
+ * multiple of 16 (8 bits) or 32 (4 bits) up to 256, pages >= 1; the four arrays are 16-byte aligned.  `device`: where they are; a call with
+ * another device current is refused (MC_EINVAL; mc_last_error_detail() names both).  Widths other than 8 and 4: MC_EUNSUPPORTED. */
+typedef struct mc_cache {
+    void *k_codes, *v_codes;
+    float *k_scales, *v_scales;
+    int64_t pages;
+    int page_size, kv_heads, dk, bits;
+    int device;
+} mc_cache;
+
+/* The rotation of keys on their way into a cache (see mc_rope; halves or interleaved, never inverse).  Here the whole of it is double precision:
+ * codes are decided from the unrounded key. */
+typedef struct mc_rope_keys {
+    const int64_t *positions_dev;
+    const double *inv_freq_dev;
+    int rot, interleaved;
+    float magnitude;
+} mc_rope_keys;
+
+/* Quantises keys and values into the cache: for every vector of dk elements
+ *   scale = fp32(max |x| / qmax),  code = clamp(rint(x / scale), -qmax, qmax), ties to even, decided as in double precision; qmax = 127 or 7.
+ * A vector of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has scale NaN and codes 0, so that it reads back as NaN.
+ *   k_dev, v_dev   tokens x kv_heads x dk, 16-byte aligned, strides whole 16-byte pieces
+ *   slots_dev      tokens int64; a token whose slot is negative or beyond the cache is written nowhere (padding).  Other slots must differ: of
+ *                  two tokens with one slot, each element of either may remain
+ *   rope           NULL: keys as they are
+ * All else in the cache stays as it was. */
+int mc_cache_write(const mc_cache *cache, const void *k_dev, const void *v_dev, mc_type type, int64_t tokens, int64_t k_token_stride,
+                   int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots_dev, const mc_rope_keys *rope,
+                   void *stream);
+/* Reads vectors back: code * scale in fp32, rounded to the type.  Tokens whose slot is negative or beyond the cache become zeros.  k_dev, v_dev as above. */
+int mc_cache_read(const mc_cache *cache, const int64_t *slots_dev, int64_t tokens, mc_type type, void *k_dev, void *v_dev,
+                  int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* Attention of new tokens over the cache that holds their keys and values already: the layer's form for decoding.
+ *   q_dev, o_dev   total_new x heads x dk of `type`, 16-byte aligned, strides whole 16-byte pieces; heads a multiple of kv_heads, query
+ *                  head h reads head h / (heads / kv_heads) of the cache.  o_dev must not overlap q_dev
+ *   starts_dev     batch + 1 int32: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1, at most max_new of them (rows beyond are not
+ *                  computed; neither are sequences whose rows are not rows of q_dev, nor rows of no sequence: these rows of o_dev stay as they were).
+ *                  NULL: max_new rows each, one sequence after the other
+ *   lengths_dev    batch int32: tokens of the sequence in the cache, its n new ones (the last) included; values are cut to 0 .. table_pages * page_size
+ *   table_dev      batch rows of table_pages int32, table_stride entries apart: the pages of a sequence in order.  Tokens of a page that is not
+ *                  0 .. pages - 1 are seen by nobody
+ *   tree_dev       NULL: new token i sees every token up to itself.  Else total_new uint64: new token i of a sequence sees all tokens before the new ones, and new
+ *                  token j where bit j of its word is set (its own bit included, or not); max_new <= 64 then
+ * Softmax over score_scale * (q . k), score_scale finite.  A row that sees nothing is zero; keys and values that a row does not see (an infinity or a NaN
+ * among them) do not change it.  fp32 accumulation; fp16 and bf16 weights of the second product are rounded to 11 bits relative to the row's largest.  Results do not
+ * depend on what else is in the batch beyond the order of fp32 sums, and are the same from call to call.
+ * The workspace (256-byte aligned, contents undefined before and after; calls that may overlap in time need one each) holds what pieces of long sequences
+ * leave for each other.  mc_cache_attention_workspace gives the bytes for these sizes; 0 means that none is needed and NULL will do. */
+size_t mc_cache_attention_workspace(const mc_cache *cache, int heads, int batch, int max_new, int table_pages);
+int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_type type, int64_t total_new, int heads, int64_t q_token_stride,
+                       int64_t q_head_stride, const int32_t *starts_dev, int batch, int max_new, const int32_t *lengths_dev,
+                       const int32_t *table_dev, int64_t table_stride, int table_pages, const uint64_t *tree_dev, float score_scale,
+                       void *o_dev, int64_t o_token_stride, int64_t o_head_stride, void *workspace_dev, size_t workspace_bytes,
+                       void *stream);
+
+/* ------------------------------------------------------------------------------------
  * One-knob setters kept for existing callers, tests and measurements.  Each changes one field of
  * the CALLING THREAD's default options (see mc_set_thread_options); none is needed for
  * correctness, and none affects other threads or the ..._ex entry points.

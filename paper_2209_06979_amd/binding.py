@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
 import torch  # noqa: F401  -- must come first: the library then binds to the HIP runtime torch ships
@@ -54,6 +54,17 @@ class Options(ctypes.Structure):
     _fields_ = [("spmm_row_tile_bytes", c_int), ("spmm_waves", c_int), ("spmm_stages", c_int), ("spmm_splitting", c_int),
                 ("spmm_slab", c_int), ("spmm_slab_waves", c_int), ("spmm_slab_panels", c_int), ("sddmm_waves", c_int), ("softmax_variant", c_int), ("attention_mode", c_int),
                 ("spmm_merge", c_int)]
+
+
+class CacheDescription(ctypes.Structure):
+    """mc_cache: a paged cache in the caller's device memory."""
+    _fields_ = [("k_codes", c_void_p), ("v_codes", c_void_p), ("k_scales", c_void_p), ("v_scales", c_void_p), ("pages", c_int64),
+                ("page_size", c_int), ("kv_heads", c_int), ("dk", c_int), ("bits", c_int), ("device", c_int)]
+
+
+class RopeKeys(ctypes.Structure):
+    """mc_rope_keys: the rotation of keys on their way into a cache."""
+    _fields_ = [("positions_dev", c_void_p), ("inv_freq_dev", c_void_p), ("rot", c_int), ("interleaved", c_int), ("magnitude", c_float)]
 
 
 class MagicubeError(RuntimeError):
@@ -140,6 +151,18 @@ def _load() -> ctypes.CDLL:
     L.mc_spmm_form_us.argtypes = [c_void_p, c_int, c_int, c_int, POINTER(Options)]
     L.mc_spmm_form_us.restype = ctypes.c_double
     L.mc_attention_form.argtypes = [c_void_p, c_int, c_int, POINTER(Options)]
+    L.mc_rope_frequencies.argtypes = [c_int, c_double, c_int, c_double, c_double, c_double, c_double, POINTER(c_double), POINTER(c_double)]
+    L.mc_rope.argtypes = [c_void_p, c_int, c_int64, c_int, c_int, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int, c_float, c_int,
+                          c_void_p, c_int64, c_int64, c_void_p]
+    L.mc_cache_write.argtypes = [POINTER(CacheDescription), c_void_p, c_void_p, c_int, c_int64, c_int64, c_int64, c_int64, c_int64, c_void_p,
+                                 POINTER(RopeKeys), c_void_p]
+    L.mc_cache_read.argtypes = [POINTER(CacheDescription), c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int64,
+                                c_void_p]
+    L.mc_cache_attention_workspace.argtypes = [POINTER(CacheDescription), c_int, c_int, c_int, c_int]
+    L.mc_cache_attention_workspace.restype = c_size_t
+    L.mc_cache_attention.argtypes = [POINTER(CacheDescription), c_void_p, c_int, c_int64, c_int, c_int64, c_int64, c_void_p, c_int, c_int,
+                                     c_void_p, c_void_p, c_int64, c_int, c_void_p, c_float, c_void_p, c_int64, c_int64, c_void_p, c_size_t,
+                                     c_void_p]
     L.mc_set_spmm_variant.argtypes = [c_int, c_int]
     L.mc_set_attention_mode.argtypes = [c_int]
     L.mc_set_spmm_splitting.argtypes = [c_int]
@@ -154,6 +177,7 @@ def _load() -> ctypes.CDLL:
                  "mc_set_spmm_variant", "mc_set_attention_mode", "mc_set_sddmm_variant", "mc_set_spmm_splitting", "mc_set_spmm_stages", "mc_set_spmm_dense",
                  "mc_set_softmax_variant", "mc_set_thread_options", "mc_get_thread_options", "mc_spmm_ex", "mc_sddmm_ex",
                  "mc_sparse_attention_ex", "mc_sparse_attention_static", "mc_blocked_query", "mc_pack_blocked_host", "mc_sddmm_to_mat", "mc_probe_mfma", "mc_spmm_form",
+                 "mc_rope_frequencies", "mc_rope", "mc_cache_write", "mc_cache_read", "mc_cache_attention",
                  "mc_attention_form", "mc_mat_merged_info", "mc_merged_query", "mc_merge_host", "mc_probe_spmm_phases"):
         getattr(L, name).restype = c_int
     return L
@@ -273,6 +297,7 @@ sddmm, sddmm_dequant, sddmm_to_mat = _native.sddmm, _native.sddmm_dequant, _nati
 absmax, quantize = _native.absmax, _native.quantize
 sparse_softmax, sparse_softmax_to_mat = _native.sparse_softmax, _native.sparse_softmax_to_mat
 sparse_attention, sparse_attention_static = _native.sparse_attention, _native.sparse_attention_static
+rope, cache_write, cache_read, cache_attention = _native.rope, _native.cache_write, _native.cache_read, _native.cache_attention
 OUT_TYPE = {torch.float32: 0, torch.float16: 1}
 
 
@@ -313,6 +338,60 @@ class SparseMatrix(_native.Matrix):
             self.close()
         except Exception:
             pass
+
+
+class KVCache(_native.Cache):
+    """A paged cache of keys and values in 8 or 4 bits: names for four device tensors, which the cache keeps alive.
+
+    k_codes, v_codes   (pages, kv_heads, page_size, dk) int8, or for bits=4 (pages, kv_heads, page_size, dk/2) uint8
+    k_scales, v_scales (pages, kv_heads, page_size) float32
+    """
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, bits=8):
+        if bits not in (8, 4):
+            raise MagicubeError(MC_EUNSUPPORTED, "KVCache(bits)")
+        tensors = (k_codes, v_codes, k_scales, v_scales)
+        assert all(t.is_cuda and t.is_contiguous() and t.device == k_codes.device for t in tensors)
+        assert k_codes.dim() == 4 and v_codes.shape == k_codes.shape and k_codes.dtype == v_codes.dtype == (torch.int8 if bits == 8 else torch.uint8)
+        assert all(t.shape == k_codes.shape[:3] and t.dtype == torch.float32 for t in (k_scales, v_scales))
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.bits = *tensors, bits
+        self.pages, self.kv_heads, self.page_size = k_codes.shape[:3]
+        self.dk = k_codes.shape[3] * 8 // bits
+        if any(t.data_ptr() % 16 for t in tensors):
+            raise MagicubeError(MC_EALIGN, "KVCache")
+        if (self.pages < 1 or self.kv_heads < 1 or not 16 <= self.page_size <= 4096 or self.page_size & (self.page_size - 1)
+                or not 1 <= self.dk <= 256 or self.dk % (128 // bits)):
+            raise MagicubeError(MC_EINVAL, "KVCache(sizes)")
+        self._attach(*(t.data_ptr() for t in tensors), self.pages, self.page_size, self.kv_heads, self.dk, bits, k_codes.device.index)
+
+    @classmethod
+    def zeros(cls, pages, page_size, kv_heads, dk, bits=8, device="cuda"):
+        """A cache of its own: every vector zero."""
+        if bits not in (8, 4):
+            raise MagicubeError(MC_EUNSUPPORTED, "KVCache(bits)")
+        shape, dtype = (pages, kv_heads, page_size), (torch.int8 if bits == 8 else torch.uint8)
+        codes = [torch.zeros(shape + (dk * bits // 8,), dtype=dtype, device=device) for _ in "kv"]
+        return cls(*codes, *(torch.zeros(shape, dtype=torch.float32, device=device) for _ in "kv"), bits=bits)
+
+
+ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rope_frequencies(rot, base=10000.0, scaling=None, factor=1.0, original=4096, low=1.0, high=32.0):
+    """(inverse frequencies, magnitude) of rotary positions over `rot` elements: a float64 array of rot / 2, and what rope's
+    and cache_write's `magnitude` is then.  scaling (for contexts `factor` times longer): None, "linear" (all divided by
+    factor), "base" (a larger base) or "parts" (pairs of fewer than `low` turns over `original` tokens divided by factor, of more than
+    `high` left as they are, mixed between)."""
+    out, magnitude = np.zeros(max(rot // 2, 1), np.float64), c_double()
+    _check(lib.mc_rope_frequencies(rot, base, ROPE_SCALING[scaling], factor, original, low, high, out.ctypes.data_as(POINTER(c_double)),
+                                   ctypes.byref(magnitude)), "mc_rope_frequencies")
+    return out, magnitude.value
+
+
+def cache_attention_workspace(cache: KVCache, heads: int, batch: int, max_new: int, table_pages: int) -> int:
+    """Bytes of workspace that cache_attention uses for these sizes (0: none)."""
+    d = CacheDescription(pages=cache.pages, page_size=cache.page_size, kv_heads=cache.kv_heads, dk=cache.dk, bits=cache.bits)
+    return int(lib.mc_cache_attention_workspace(ctypes.byref(d), heads, batch, max_new, table_pages))
 
 
 def set_thread_options(options: Options | None) -> None:

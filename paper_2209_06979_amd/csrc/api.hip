@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <mutex>
@@ -75,7 +76,8 @@ inline bool valid_prec(int p) { return p >= MC_L8R8 && p <= MC_L12R4; }
 
 thread_local char g_detail[256] = "";
 
-// Remembers which HIP call failed and why (read back with mc_last_error_detail).
+} // namespace
+
 bool hip_ok(hipError_t e, const char *what)
 {
     if (e == hipSuccess) return true;
@@ -84,10 +86,15 @@ bool hip_ok(hipError_t e, const char *what)
     return false;
 }
 
-#define MC_HIP(call)                               \
-    do {                                           \
-        if (!hip_ok((call), #call)) return MC_EHIP; \
-    } while (0)
+void note_detail(const char *format, ...)
+{
+    va_list args;
+    va_start(args, format);
+    vsnprintf(g_detail, sizeof g_detail, format, args);
+    va_end(args);
+}
+
+namespace {
 
 // Every compute call works on the device the operand was created on: its buffers are not
 // addressable from another one.

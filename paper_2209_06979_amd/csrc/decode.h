@@ -1,0 +1,93 @@
+// Internal declarations of the operators around decoding: rotary positions, the quantized cache, attention over it.
+#pragma once
+
+#include "internal.h"
+
+// Real-valued element types in kernels (mc_type numbers them).
+template <int TYPE> struct RealOf;
+template <> struct RealOf<MC_F32> { typedef float type; };
+template <> struct RealOf<MC_F16> { typedef _Float16 type; };
+template <> struct RealOf<MC_BF16> { typedef __bf16 type; };
+
+struct RopeArgs {
+    const void *x;
+    void *y;
+    int64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride; // elements
+    const int64_t *positions;
+    const double *inv_freq;
+    int64_t tokens;
+    int heads, dim, rot;
+    int interleaved;
+    double cos_scale, sin_scale; // magnitude, and with the sign of the direction
+    int groups;                  // filled by the launcher: threads that share a token's heads
+};
+
+// K and V written into a cache (and read back): vectors of dk elements, one scale each.
+struct CacheArgs {
+    uint8_t *codes[2];           // K, V
+    float *scales[2];
+    int64_t slots_end;           // pages * page size
+    int page_shift, kv_heads, dk, bits;
+    void *x[2];                  // K, V: read by a write, written by a read
+    int64_t token_stride[2], head_stride[2]; // elements
+    const int64_t *slots;
+    int64_t tokens;
+    // rotation of K (rot 0: none)
+    const int64_t *positions;
+    const double *inv_freq;
+    int rot, interleaved;
+    double magnitude;
+    int groups;                  // filled by the launcher, as in RopeArgs
+};
+
+// Attention of new tokens over a cache (cache_attention_kernels.hip).
+struct CacheAttnArgs {
+    const uint8_t *k_codes, *v_codes;
+    const float *k_scales, *v_scales;
+    int64_t pages;
+    int page_shift, kv_heads, dk, group;
+    const int32_t *lengths, *starts; // starts null: max_new rows per sequence
+    const int32_t *table;
+    int64_t table_stride;
+    int table_pages;             // entries of a row of the table
+    int batch, max_new;
+    int64_t total_new;
+    const uint64_t *tree;        // null: a chain
+    const void *q;
+    int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride; // elements
+    void *o;
+    float score_scale;           // times log2(e)
+    int pieces;                  // pieces that the sequences' tokens are cut into, per head of the cache (see cache_attention_plan)
+    int row_tiles;               // tiles of rows (new token, query head of the group) at max_new tokens
+    float *partial;              // results of pieces that are not a whole sequence; null: no sequence is cut
+};
+
+hipError_t launch_rope(const RopeArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_cache_write(const CacheArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_cache_read(const CacheArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits, hipStream_t s);
+
+constexpr int CACHE_TILE = 32;         // tokens that a wave takes at a time
+constexpr int CACHE_WAVES = 4;         // waves of a workgroup, which share a piece
+constexpr int CACHE_MIN_PIECE = 8;     // tiles of the shortest piece
+constexpr int CACHE_PIECES = 1024;     // pieces asked for, over all heads of the cache and row tiles
+
+// What the launch and its workspace are made for: pieces per head asked for, row tiles, whether a sequence can be cut at all, and
+// the floats of the partial results.
+struct CacheAttnPlan { int pieces, row_tiles, row_tile; bool cut; int64_t slots, floats; };
+inline CacheAttnPlan cache_attention_plan(int kv_heads, int dk, int group, int batch, int max_new, int64_t most_tokens)
+{
+    CacheAttnPlan p = {};
+    const int64_t rows = (int64_t)max_new * group, tiles = (most_tokens + CACHE_TILE - 1) / CACHE_TILE;
+    p.row_tile = 16;
+    p.row_tiles = (int)((rows + p.row_tile - 1) / p.row_tile);
+    const int64_t sharers = (int64_t)kv_heads * (p.row_tiles > 0 ? p.row_tiles : 1);
+    p.pieces = (int)(CACHE_PIECES / sharers > 1 ? CACHE_PIECES / sharers : 1);
+    p.cut = tiles > CACHE_MIN_PIECE && p.row_tiles > 0 && batch > 0;
+    // sequences that are cut have more than one piece, fewer than twice the pieces their share asks for; and every sequence adds one
+    // that is not full
+    p.slots = p.cut ? (2 * (int64_t)p.pieces < (int64_t)p.pieces + batch ? 2 * (int64_t)p.pieces : (int64_t)p.pieces + batch) : 0;
+    const int width = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
+    p.floats = p.slots * kv_heads * p.row_tiles * p.row_tile * (width + 2);
+    return p;
+}

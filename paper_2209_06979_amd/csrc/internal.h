@@ -21,6 +21,16 @@ template <class... P, class... A> inline hipError_t launch_kernel(void (*kernel)
     }, values);
 }
 
+// Remembers which HIP call failed and why (read back with mc_last_error_detail); false if it did.
+bool hip_ok(hipError_t e, const char *what);
+// The message of a refusal that has a detail of its own (printf's arguments).
+void note_detail(const char *format, ...);
+#define MC_HIP(call)                               \
+    do {                                           \
+        if (!hip_ok((call), #call)) return MC_EHIP; \
+    } while (0)
+
+
 struct mc_mat {
     int M, K, V, lhs_bits, P;
     int64_t nvec, nslots, vals_bytes;

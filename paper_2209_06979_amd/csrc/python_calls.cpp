@@ -19,6 +19,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/magicube.h"
 
 namespace {
@@ -682,6 +684,254 @@ PyObject *sparse_attention_static(PyObject *, PyObject *const *args, Py_ssize_t 
     END_HANDLE_TH_ERRORS
 }
 
+// ---- decoding: rotary positions, the quantized cache, attention over it --------------------------------
+// The native part of binding.KVCache: the description that the calls hand on.
+struct Cache {
+    PyObject_HEAD
+    mc_cache cache;       // pages 0 until attached
+};
+
+PyObject *cache_attach(PyObject *self, PyObject *args)
+{
+    unsigned long long kc, vc, ks, vs;
+    long long pages;
+    mc_cache c = {};
+    if (!PyArg_ParseTuple(args, "KKKKLiiiii", &kc, &vc, &ks, &vs, &pages, &c.page_size, &c.kv_heads, &c.dk, &c.bits, &c.device)) return nullptr;
+    c.k_codes = reinterpret_cast<void *>(static_cast<uintptr_t>(kc));
+    c.v_codes = reinterpret_cast<void *>(static_cast<uintptr_t>(vc));
+    c.k_scales = reinterpret_cast<float *>(static_cast<uintptr_t>(ks));
+    c.v_scales = reinterpret_cast<float *>(static_cast<uintptr_t>(vs));
+    c.pages = pages;
+    reinterpret_cast<Cache *>(self)->cache = c;
+    Py_RETURN_NONE;
+}
+
+PyMethodDef cache_methods[] = {
+    {"_attach", cache_attach, METH_VARARGS, "_attach(k_codes, v_codes, k_scales, v_scales, pages, page_size, kv_heads, dk, bits, device)"},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject CacheType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+const mc_cache *cache(PyObject *o)
+{
+    if (!PyObject_TypeCheck(o, &CacheType)) {
+        PyErr_Format(PyExc_TypeError, "expected a KVCache, got %.100s", Py_TYPE(o)->tp_name);
+        return nullptr;
+    }
+    return &reinterpret_cast<Cache *>(o)->cache;
+}
+
+bool real_type(at::ScalarType t, mc_type *type)
+{
+    *type = t == at::kFloat ? MC_F32 : t == at::kHalf ? MC_F16 : MC_BF16;
+    return t == at::kFloat || t == at::kHalf || t == at::kBFloat16;
+}
+// (tokens, heads, elements) on the device, unit stride along the elements
+inline bool token_major(const at::Tensor &t) { return t.is_cuda() && t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1); }
+// a contiguous array of `n` on x's device
+inline bool array(const at::Tensor &t, at::ScalarType type, int64_t n, const at::Tensor &x)
+{
+    return t.is_cuda() && t.device() == x.device() && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n && (n <= 1 || t.stride(0) == 1);
+}
+// what is worked on is on the current device, whose stream the call goes to
+inline bool current(const at::Tensor &t) { return t.device().index() == c10::hip::current_device(); }
+
+Params<7> p_rope = {"rope", 3, {"x", "positions", "inv_freq", "interleaved", "magnitude", "inverse", "out"}, {}};
+
+PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[7];
+    if (!p_rope.parse(args, nargs, kwnames, v)) return nullptr;
+    const at::Tensor *x = tensor(v[0]), *pos = x ? tensor(v[1]) : nullptr, *freq = pos ? tensor(v[2]) : nullptr, *out = nullptr;
+    if (!freq) return nullptr;
+    unsigned interleaved = 0, inverse = 0;
+    float magnitude = 1;
+    if (!truth(v[3], 1, &interleaved) || (v[4] && !number(v[4], &magnitude)) || !truth(v[5], 1, &inverse)) return nullptr;
+    mc_type type;
+    if (!(token_major(*x) && real_type(x->scalar_type(), &type) && array(*pos, at::kLong, x->size(0), *x) && freq->dim() == 1 &&
+          array(*freq, at::kDouble, freq->size(0), *x) && current(*x) && x->size(1) <= 65535 && x->size(2) <= 65536 && freq->size(0) <= 32768))
+        return assertion();
+    if (given(v[6])) {
+        if (!(out = tensor(v[6]))) return nullptr;
+        if (!(token_major(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->sizes() == x->sizes())) return assertion();
+    }
+    at::TensorBase made;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        if (!out) made = empty(x->sizes(), x->scalar_type(), *x);
+        rc = mc_rope(x->data_ptr(), type, x->size(0), (int)x->size(1), (int)x->size(2), x->stride(0), x->stride(1),
+                     static_cast<const int64_t *>(pos->data_ptr()), static_cast<const double *>(freq->data_ptr()), (int)freq->size(0) * 2,
+                     (int)interleaved, magnitude, (int)inverse, out ? out->data_ptr() : made.data_ptr(),
+                     out ? out->stride(0) : x->size(1) * x->size(2), out ? out->stride(1) : x->size(2), stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_rope");
+    return out ? same(v[6]) : wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
+// K and V of a call, (tokens, kv heads, dk) both
+bool keys_values(const mc_cache *c, const at::Tensor &k, const at::Tensor &v, mc_type *type)
+{
+    return token_major(k) && token_major(v) && real_type(k.scalar_type(), type) && v.scalar_type() == k.scalar_type() && v.device() == k.device() &&
+           v.sizes() == k.sizes() && k.size(1) == c->kv_heads && k.size(2) == c->dk && k.device().index() == c->device;
+}
+
+Params<8> p_cache_write = {"cache_write", 4, {"cache", "k", "v", "slots", "positions", "inv_freq", "interleaved", "magnitude"}, {}};
+
+PyObject *cache_write(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[8];
+    if (!p_cache_write.parse(args, nargs, kwnames, v)) return nullptr;
+    const mc_cache *c = cache(v[0]);
+    const at::Tensor *k = c ? tensor(v[1]) : nullptr, *w = k ? tensor(v[2]) : nullptr, *slots = w ? tensor(v[3]) : nullptr;
+    if (!slots) return nullptr;
+    mc_type type;
+    if (!(keys_values(c, *k, *w, &type) && array(*slots, at::kLong, k->size(0), *k))) return assertion();
+    mc_rope_keys turn = {};
+    turn.magnitude = 1;
+    const bool turned = given(v[4]) || given(v[5]);
+    if (turned) {
+        if (!given(v[4]) || !given(v[5])) return assertion();
+        const at::Tensor *pos = tensor(v[4]), *freq = pos ? tensor(v[5]) : nullptr;
+        if (!freq) return nullptr;
+        if (!(array(*pos, at::kLong, k->size(0), *k) && freq->dim() == 1 && array(*freq, at::kDouble, freq->size(0), *k) && freq->size(0) <= 32768)) return assertion();
+        unsigned interleaved = 0;
+        if (!truth(v[6], 1, &interleaved) || (v[7] && !number(v[7], &turn.magnitude))) return nullptr;
+        turn.positions_dev = static_cast<const int64_t *>(pos->data_ptr());
+        turn.inv_freq_dev = static_cast<const double *>(freq->data_ptr());
+        turn.rot = (int)freq->size(0) * 2;
+        turn.interleaved = (int)interleaved;
+    }
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        rc = mc_cache_write(c, k->data_ptr(), w->data_ptr(), type, k->size(0), k->stride(0), k->stride(1), w->stride(0), w->stride(1),
+                            static_cast<const int64_t *>(slots->data_ptr()), turned ? &turn : nullptr, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_cache_write");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+Params<4> p_cache_read = {"cache_read", 2, {"cache", "slots", "dtype", "out"}, {}};
+
+PyObject *cache_read(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[4];
+    if (!p_cache_read.parse(args, nargs, kwnames, v)) return nullptr;
+    const mc_cache *c = cache(v[0]);
+    const at::Tensor *slots = c ? tensor(v[1]) : nullptr, *k = nullptr, *w = nullptr;
+    if (!slots) return nullptr;
+    at::ScalarType dtype = at::kFloat;
+    mc_type type = MC_F32;
+    if (given(v[2])) {
+        if (!THPDtype_Check(v[2]) || !real_type(reinterpret_cast<THPDtype *>(v[2])->scalar_type, &type)) {
+            PyErr_SetObject(PyExc_KeyError, v[2]);
+            return nullptr;
+        }
+        dtype = reinterpret_cast<THPDtype *>(v[2])->scalar_type;
+    }
+    if (!(slots->is_cuda() && slots->dim() == 1 && array(*slots, at::kLong, slots->size(0), *slots) && slots->device().index() == c->device)) return assertion();
+    if (given(v[3])) {
+        if (!PyTuple_Check(v[3]) || PyTuple_GET_SIZE(v[3]) != 2) return assertion();
+        if (!(k = tensor(PyTuple_GET_ITEM(v[3], 0))) || !(w = tensor(PyTuple_GET_ITEM(v[3], 1)))) return nullptr;
+        mc_type of = MC_F32;
+        if (!(keys_values(c, *k, *w, &of) && k->size(0) == slots->size(0) && (!given(v[2]) || of == type))) return assertion();
+        type = of;
+    }
+    at::TensorBase made_k, made_v;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        const int64_t n = slots->size(0), token = (int64_t)c->kv_heads * c->dk, head = c->dk;
+        if (!k) {
+            made_k = empty({n, c->kv_heads, c->dk}, dtype, *slots);
+            made_v = empty({n, c->kv_heads, c->dk}, dtype, *slots);
+        }
+        rc = mc_cache_read(c, static_cast<const int64_t *>(slots->data_ptr()), n, type, k ? k->data_ptr() : made_k.data_ptr(),
+                           k ? w->data_ptr() : made_v.data_ptr(), k ? k->stride(0) : token, k ? k->stride(1) : head, k ? w->stride(0) : token,
+                           k ? w->stride(1) : head, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_cache_read");
+    if (k) return same(v[3]);
+    PyObject *a = wrap(std::move(made_k)), *b = wrap(std::move(made_v)), *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+Params<10> p_cache_attention = {"cache_attention", 4, {"q", "cache", "page_table", "lengths", "starts", "max_new", "tree", "scale", "out", "workspace"}, {}};
+
+PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[10];
+    if (!p_cache_attention.parse(args, nargs, kwnames, v)) return nullptr;
+    const at::Tensor *q = tensor(v[0]);
+    const mc_cache *c = q ? cache(v[1]) : nullptr;
+    const at::Tensor *table = c ? tensor(v[2]) : nullptr, *lengths = table ? tensor(v[3]) : nullptr, *starts = nullptr, *tree = nullptr, *out = nullptr, *ws = nullptr;
+    if (!lengths) return nullptr;
+    mc_type type;
+    if (!(token_major(*q) && real_type(q->scalar_type(), &type) && q->size(2) == c->dk && q->device().index() == c->device && q->size(1) <= 0x7fffffff &&
+          lengths->dim() == 1 && lengths->size(0) <= 65535 && array(*lengths, at::kInt, lengths->size(0), *q) && table->is_cuda() && table->device() == q->device() &&
+          table->scalar_type() == at::kInt && table->dim() == 2 && table->size(0) == lengths->size(0) && (table->stride(1) == 1 || table->size(1) <= 1) &&
+          table->size(1) <= 0x7fffffff))
+        return assertion();
+    const int64_t batch = lengths->size(0), total = q->size(0);
+    int max_new;
+    if (!integer(given(v[5]) ? v[5] : nullptr, -1, &max_new)) return nullptr;
+    if (given(v[4])) {
+        if (!(starts = tensor(v[4]))) return nullptr;
+        if (!array(*starts, at::kInt, batch + 1, *q) || max_new < 0) return assertion(); // (the host does not know the largest step of starts)
+    } else if (max_new < 0) { // the same number of new tokens for every sequence
+        if (batch ? total % batch != 0 || total / batch > 0x7fffffff : total != 0) return assertion();
+        max_new = batch ? (int)(total / batch) : 0;
+    }
+    if (given(v[6])) {
+        if (!(tree = tensor(v[6]))) return nullptr;
+        if (!array(*tree, at::kLong, total, *q)) return assertion();
+    }
+    float scale = (float)(1.0 / std::sqrt((double)(c->dk > 0 ? c->dk : 1)));
+    if (given(v[7]) && !number(v[7], &scale)) return nullptr;
+    if (given(v[8])) {
+        if (!(out = tensor(v[8]))) return nullptr;
+        if (!(token_major(*out) && out->device() == q->device() && out->scalar_type() == q->scalar_type() && out->sizes() == q->sizes())) return assertion();
+    }
+    if (given(v[9])) {
+        if (!(ws = tensor(v[9]))) return nullptr;
+        if (!(ws->is_cuda() && ws->device() == q->device() && ws->is_contiguous())) return assertion();
+    }
+    at::TensorBase made, scratch;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        if (!out) made = empty(q->sizes(), q->scalar_type(), *q);
+        void *w = nullptr;
+        size_t wbytes = 0;
+        if (ws) {
+            w = ws->data_ptr();
+            wbytes = (size_t)ws->numel() * ws->element_size();
+        } else if ((wbytes = mc_cache_attention_workspace(c, (int)q->size(1), (int)batch, max_new, (int)table->size(1))) > 0) {
+            scratch = empty({(int64_t)wbytes}, at::kByte, *q);
+            w = scratch.data_ptr();
+        }
+        rc = mc_cache_attention(c, q->data_ptr(), type, total, (int)q->size(1), q->stride(0), q->stride(1),
+                                starts ? static_cast<const int32_t *>(starts->data_ptr()) : nullptr, (int)batch, max_new,
+                                static_cast<const int32_t *>(lengths->data_ptr()), static_cast<const int32_t *>(table->data_ptr()),
+                                table->size(0) > 1 ? table->stride(0) : table->size(1), (int)table->size(1),
+                                tree ? static_cast<const uint64_t *>(tree->data_ptr()) : nullptr, scale, out ? out->data_ptr() : made.data_ptr(),
+                                out ? out->stride(0) : q->size(1) * q->size(2), out ? out->stride(1) : q->size(2), w, wbytes, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_cache_attention");
+    return out ? same(v[8]) : wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject *set_error_class(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -736,6 +986,25 @@ PyMethodDef functions[] = {
      "sparse_attention_static(Q8, K8, V8, mask, s_q, s_k, s_v, s_p, out, p_bits=8, qkv_bits=8, options=None)\n--\n\n"
      "sparse_attention for callers that cannot allocate: no workspace argument (the library's own per-GPU array\n"
      "holds the intermediates) and a caller-provided ``out``.  This wrapper allocates nothing on the device either."},
+    {"rope", FAST(rope),
+     "rope(x, positions, inv_freq, interleaved=False, magnitude=1.0, inverse=False, out=None)\n--\n\n"
+     "Rotary positions: x (tokens, heads, dim) fp32, fp16 or bf16 with any strides, positions (tokens,) int64, inv_freq (rot/2,) float64\n"
+     "(see rope_frequencies).  Pairs (j, j + rot/2), or (2j, 2j + 1) if interleaved; elements from rot on are copied.  out may be x.\n"
+     "inverse: the angles reversed, which makes the call the gradient (no autograd node is recorded)."},
+    {"cache_write", FAST(cache_write),
+     "cache_write(cache, k, v, slots, positions=None, inv_freq=None, interleaved=False, magnitude=1.0)\n--\n\n"
+     "Quantises k and v (tokens, kv_heads, dk; fp32, fp16 or bf16) into the cache, one scale per vector; slots (tokens,) int64 = page *\n"
+     "page_size + place, negative or beyond the cache: written nowhere; others must differ.  positions and inv_freq: k is rotated first (see rope)."},
+    {"cache_read", FAST(cache_read),
+     "cache_read(cache, slots, dtype=torch.float32, out=None)\n--\n\n"
+     "(k, v) of the slots, (tokens, kv_heads, dk) each: code * scale; zeros where a slot is negative or beyond the cache.\n"
+     "out: a tuple of two tensors to write to (dtype is theirs)."},
+    {"cache_attention", FAST(cache_attention),
+     "cache_attention(q, cache, page_table, lengths, starts=None, max_new=None, tree=None, scale=None, out=None, workspace=None)\n--\n\n"
+     "Attention of new tokens over the cache that holds their keys and values already.  q: (total new tokens, heads, dk); page_table\n"
+     "(batch, pages) int32; lengths (batch,) int32, the new tokens included.  starts (batch + 1,) int32: the rows of each sequence, at most\n"
+     "max_new each (None: the same number for all).  tree (total,) int64: bit j of a row lets it see the sequence's new token j (None: all\n"
+     "up to itself).  scale: None is 1 / sqrt(dk).  See mc_cache_attention in magicube.h for what out-of-range values do."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};
@@ -755,9 +1024,19 @@ PyMODINIT_FUNC PyInit__native(void)
     p_spmm.intern(); p_spmm_dequant.intern(); p_sddmm.intern(); p_sddmm_dequant.intern(); p_sddmm_to_mat.intern();
     p_set_values.intern(); p_absmax.intern(); p_quantize.intern(); p_softmax.intern(); p_softmax_to_mat.intern();
     p_attention.intern(); p_attention_static.intern();
+    CacheType.tp_name = "paper_2209_06979_amd._native.Cache";
+    CacheType.tp_basicsize = sizeof(Cache);
+    CacheType.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_BASETYPE;
+    CacheType.tp_doc = "Native part of binding.KVCache: the description that the compute calls read.";
+    CacheType.tp_methods = cache_methods;
+    CacheType.tp_new = PyType_GenericNew;
+    if (PyType_Ready(&CacheType) < 0) return nullptr;
+    p_rope.intern(); p_cache_write.intern(); p_cache_read.intern(); p_cache_attention.intern();
     PyObject *m = PyModule_Create(&module_def);
     if (!m) return nullptr;
     Py_INCREF(&MatrixType);
     if (PyModule_AddObject(m, "Matrix", reinterpret_cast<PyObject *>(&MatrixType)) < 0) return nullptr;
+    Py_INCREF(&CacheType);
+    if (PyModule_AddObject(m, "Cache", reinterpret_cast<PyObject *>(&CacheType)) < 0) return nullptr;
     return m;
 }
