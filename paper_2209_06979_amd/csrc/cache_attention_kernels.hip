@@ -25,16 +25,20 @@ __device__ __forceinline__ unsigned bits_of(h2 v) { return __builtin_bit_cast(un
 __device__ __forceinline__ h2 halves_of(unsigned v) { return __builtin_bit_cast(h2, v); }
 __device__ __forceinline__ h8 operand(unsigned a, unsigned b, unsigned c, unsigned d) { return __builtin_bit_cast(h8, (v4u){a, b, c, d}); }
 
-// max / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48
+// max / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (a swap of a value with itself leaves the two lanes' values in both)
 __device__ __forceinline__ float max_of_groups(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum_of_groups(float v)
 {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // ---- which piece ---------------------------------------------------------------------------------------
@@ -63,51 +67,54 @@ __device__ __forceinline__ int piece_tiles(const CacheAttnArgs &a, int total)
     return t <= CACHE_MIN_PIECE ? CACHE_MIN_PIECE : (t + CACHE_WAVES - 1) / CACHE_WAVES * CACHE_WAVES;
 }
 
-__device__ __forceinline__ int scan(int v) // inclusive, over the wave
+__device__ __forceinline__ int scan(int v) // inclusive, over the wave: within rows of 16 lanes, then their last lanes' sums into the rows behind
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(v, o, 64);
-        if (lane >= o) v += up;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true); // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false); // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false); // row_bcast:31 into rows 2 and 3
     return v;
 }
+__device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// A sequence (b), the tiles of its pieces, how many there are and the number of its first among the pieces of sequences that are cut.
-struct Cut { int b, each, pieces, slot, index; };
-// The sequence that piece `number` belongs to (BY_PIECE, and its index there), or sequence `number` itself; b = -1: none.
+// A sequence (b), the tiles of its pieces, how many there are, the number of its first among the pieces of sequences that are cut, and the index of
+// the piece asked for.
+struct Cut { int b, each, pieces, slot, index; Sequence of; };
+// The sequence that piece `number` belongs to (BY_PIECE), or sequence `number` itself; b = -1: none.
 template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnArgs &a, int number)
 {
     const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int b = 0; b < a.batch; b += 64) {
-        const int t = b + lane < a.batch ? tiles_of(sequence(a, b + lane)) : 0;
-        total += __shfl(scan(t), 63, 64);
+    const Sequence none = {0, 0, 0};
+    Sequence s = lane < a.batch ? sequence(a, lane) : none;
+    int t = tiles_of(s), total = 0;
+    if (a.partial) {
+        total = at_lane(scan(t), 63);
+        for (int b = 64; b < a.batch; b += 64) total += at_lane(scan(tiles_of(b + lane < a.batch ? sequence(a, b + lane) : none)), 63);
     }
-    Cut c = {-1, a.partial ? piece_tiles(a, total) : 0x7fffffff, 0, 0, 0};
+    Cut c = {-1, a.partial ? piece_tiles(a, total) : 0x7fffffff, 0, 0, 0, none};
     int before = 0, slots = 0;
     for (int b = 0; b < a.batch; b += 64) {
-        const int t = b + lane < a.batch ? tiles_of(sequence(a, b + lane)) : 0;
+        if (b) {
+            s = b + lane < a.batch ? sequence(a, b + lane) : none;
+            t = tiles_of(s);
+        }
         const int pieces = t == 0 ? 0 : (t - 1) / c.each + 1, up_to = scan(pieces), cut_up_to = scan(pieces > 1 ? pieces : 0);
         const bool here = BY_PIECE ? before + up_to - pieces <= number && number < before + up_to : b + lane == number;
         const unsigned long long who = __ballot(here);
         if (who) {
             const int l = __builtin_ctzll(who);
             c.b = b + l;
-            c.pieces = __shfl(pieces, l, 64);
-            c.slot = slots + __shfl(cut_up_to, l, 64) - (c.pieces > 1 ? c.pieces : 0);
-            c.index = number - before - __shfl(up_to, l, 64) + c.pieces;
+            c.pieces = at_lane(pieces, l);
+            c.slot = slots + at_lane(cut_up_to, l) - (c.pieces > 1 ? c.pieces : 0);
+            c.index = number - before - at_lane(up_to, l) + c.pieces;
+            c.of = {at_lane(s.start, l), at_lane(s.n, l), at_lane(s.length, l)};
             break;
         }
-        before += __shfl(up_to, 63, 64);
-        slots += __shfl(cut_up_to, 63, 64);
+        before += at_lane(up_to, 63);
+        slots += at_lane(cut_up_to, 63);
     }
-    c.b = __builtin_amdgcn_readfirstlane(c.b);
-    c.each = __builtin_amdgcn_readfirstlane(c.each);
-    c.pieces = __builtin_amdgcn_readfirstlane(c.pieces);
-    c.slot = __builtin_amdgcn_readfirstlane(c.slot);
-    c.index = __builtin_amdgcn_readfirstlane(c.index);
     return c;
 }
 
@@ -135,7 +142,7 @@ template <int BITS> __device__ __forceinline__ h8 row_operand(unsigned w0, unsig
                        minus((d & 0x000F000Fu) | 0x64006400u, 1032.f), nibble_high((d & 0x00F000F0u) | 0x64006400u));
     }
 }
-__device__ __forceinline__ int nibble_order(int e) { return e / 2 + 4 * (e % 2); } // element of place e
+constexpr int nibble_order(int e) { return e / 2 + 4 * (e % 2); } // element of place e
 
 // Column m of two tokens' words as a pair of halves (BITS 8: byte m of 4; BITS 4: nibble m of 8)
 template <int BITS> __device__ __forceinline__ unsigned column_pair(unsigned first, unsigned second, int m)
@@ -145,235 +152,346 @@ template <int BITS> __device__ __forceinline__ unsigned column_pair(unsigned fir
         return minus(__builtin_amdgcn_perm(second, first, sel) ^ 0x64806480u, 1152.f);
     } else {
         const unsigned sel = 0x0c000c00u | (unsigned)(4 + m / 2) << 16 | (unsigned)(m / 2);
-        const unsigned pair = __builtin_amdgcn_perm(second, first, sel);
-        if (m % 2 == 0) return minus((pair & 0x000F000Fu) ^ 0x64086408u, 1032.f);
-        return nibble_high((pair & 0x00F000F0u) ^ 0x64806480u);
+        const unsigned pair = __builtin_amdgcn_perm(second, first, sel); // (of words whose nibbles' top bits are turned over)
+        if (m % 2 == 0) return minus((pair & 0x000F000Fu) | 0x64006400u, 1032.f);
+        return nibble_high((pair & 0x00F000F0u) | 0x64006400u);
     }
 }
 
 // ---- the pieces ----------------------------------------------------------------------------------------
 template <int N> struct Words { unsigned w[N]; };
-template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t *p)
+// `at` bytes behind a base that is the same for the whole wave
+template <int BYTES> __device__ __forceinline__ Words<(BYTES + 3) / 4> load_bytes(const uint8_t *base, unsigned at)
 {
-    Words<N> v;
-    if constexpr (N >= 4) {
+    Words<(BYTES + 3) / 4> v;
+    if constexpr (BYTES >= 16) {
+        static_assert(BYTES == 16, "one request");
+        const v4u u = *reinterpret_cast<const v4u *>(base + at);
 #pragma unroll
-        for (int q = 0; q < N / 4; ++q) {
-            const v4u u = reinterpret_cast<const v4u *>(p)[q];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v.w[4 * q + e] = u[e];
-        }
-    } else if constexpr (N == 2) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(p);
+        for (int e = 0; e < 4; ++e) v.w[e] = u[e];
+    } else if constexpr (BYTES == 8) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(base + at);
         v.w[0] = u.x;
         v.w[1] = u.y;
+    } else if constexpr (BYTES == 4) {
+        v.w[0] = *reinterpret_cast<const unsigned *>(base + at);
     } else {
-        v.w[0] = *reinterpret_cast<const unsigned *>(p);
+        v.w[0] = *reinterpret_cast<const unsigned short *>(base + at);
     }
     return v;
 }
 
-template <int TYPE> __device__ __forceinline__ float real_at(const void *p, int64_t i) { return (float)static_cast<const typename RealOf<TYPE>::type *>(p)[i]; }
-
-// D: head dimension's tile (64, 128, 256).  Lane l: row l % 16 of the products with q, group g = l / 16 of the reduction.
-// FULL: q in one half each and rounded weights, else (fp32) both in two halves.
-template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 64, 1) void cache_attention_kernel(CacheAttnArgs a)
+// 8 values of a row of q, and N results of a row of o (16-byte pieces, or 8 bytes)
+template <int TYPE> __device__ __forceinline__ void load_real8(const void *p, int64_t at, float (&v)[8])
 {
-    constexpr int PLANES = TYPE == MC_F32 ? 2 : 1;
-    constexpr int C = D / 16;                        // columns of V in a lane
-    constexpr int STEPS = D / 32;                    // of the first product
-    constexpr int KB = D * BITS / 32, PB = KB < 16 ? KB : 16, NK = KB / PB;  // bytes of a row of K in a lane, in pieces
-    constexpr int VW = C * BITS / 32;                // words of a row of V in a lane (D = 64, 4 bits: half a word)
-    constexpr int VN = VW ? VW : 1;
+    typedef typename RealOf<TYPE>::type T;
+    constexpr int N = 16 / sizeof(T);
+    typedef T Vec __attribute__((ext_vector_type(N)));
+#pragma unroll
+    for (int q = 0; q < 8 / N; ++q) {
+        const Vec u = *reinterpret_cast<const Vec *>(static_cast<const T *>(p) + at + q * N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[q * N + e] = (float)u[e];
+    }
+}
+template <int TYPE, int N> __device__ __forceinline__ void store_real(void *p, int64_t at, const float *v)
+{
+    typedef typename RealOf<TYPE>::type T;
+    constexpr int M = N * sizeof(T) < 16 ? N : 16 / sizeof(T);
+    typedef T Vec __attribute__((ext_vector_type(M)));
+#pragma unroll
+    for (int q = 0; q < N / M; ++q) {
+        Vec u;
+#pragma unroll
+        for (int e = 0; e < M; ++e) u[e] = (T)v[q * M + e];
+        *reinterpret_cast<Vec *>(static_cast<T *>(p) + at + q * M) = u;
+    }
+}
+
+// Where a row of results goes: row `row` (new token, query head of the group) of a sequence
+__device__ __forceinline__ int64_t out_at(const CacheAttnArgs &a, const Sequence &s, int head, int row)
+{
+    return (s.start + (int64_t)(row / a.group)) * a.o_token_stride + (int64_t)(head * a.group + row % a.group) * a.o_head_stride;
+}
+
+// Sizes that follow from D (the head dimension's tile: 64, 128 or 256), the width of codes and the type.  Lane l of a wave: row i = l % 16 of a tile of rows in
+// the products with q, group g = l / 16 of the reduction.
+template <int D, int BITS, int TYPE> struct Shape {
+    static constexpr int PLANES = TYPE == MC_F32 ? 2 : 1; // halves that hold a value of q, and a weight
+    static constexpr int C = D / 16;                      // columns of V in a lane
+    static constexpr int STEPS = D / 32;                  // of the first product
+    static constexpr int KB = D * BITS / 32, PB = KB < 16 ? KB : 16, NK = KB / PB, PER = PB / BITS; // bytes of a row of K in a lane, in pieces of PER steps
+    static constexpr int VB = C * BITS / 8;               // bytes of a row of V in a lane
+    // the first of the 8 elements that a lane's codes of a step are
+    static __device__ __forceinline__ int element(int step, int g)
+    {
+        return BITS == 8 ? 64 * (step / 2) + 16 * g + 8 * (step % 2) : PB == 16 ? 128 * (step / 4) + 32 * g + 8 * (step % 4) : 16 * g + 8 * step;
+    }
+};
+
+// A lane's row of q as operands of the first product, times a power of two that brings the row's largest into [1, 2); what scores are multiplied by then
+template <class S, int BITS, int TYPE> __device__ __forceinline__ float load_q(const CacheAttnArgs &a, int64_t at, int g, h8 (&q)[S::PLANES][S::STEPS])
+{
+    float v[S::STEPS][8], top = 0;
+#pragma unroll
+    for (int st = 0; st < S::STEPS; ++st) {
+        const int d = S::element(st, g);
+        if (d < a.dk) load_real8<TYPE>(a.q, at + d, v[st]);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[st][e] = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[st][e]));
+    }
+    top = max_of_groups(top);
+    const int up = top > 0 && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
+#pragma unroll
+    for (int st = 0; st < S::STEPS; ++st)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = __builtin_amdgcn_ldexpf(v[st][BITS == 8 ? e : nibble_order(e)], -up);
+            q[0][st][e] = (_Float16)x;
+            if (S::PLANES == 2) q[S::PLANES - 1][st][e] = (_Float16)(x - (float)(_Float16)x);
+        }
+    return __builtin_amdgcn_ldexpf(a.score_scale, up);
+}
+
+// What a row may see: all tokens below `all`, and those of the bits from `held` on
+struct Sight { int all; uint64_t bits; };
+__device__ __forceinline__ Sight sight_of(const CacheAttnArgs &a, const Sequence &s, int token)
+{
+    const int held = s.length - s.n;
+    if (!a.tree) return {held + token + 1, 0};
+    return {held, a.tree[s.start + token] & (s.n < 64 ? (1ull << s.n) - 1 : ~0ull)};
+}
+// (no branches: as such the compiler lost some of the -infinities between them)
+__device__ __forceinline__ unsigned sees(const Sight &s, int token, int held, bool there)
+{
+    const int later = token - held;
+    const unsigned bit = (unsigned)(s.bits >> (later & 63)) & (unsigned)((unsigned)later < 64u);
+    return (unsigned)there & ((unsigned)(token < s.all) | bit) & 1u;
+}
+
+// Offsets of this lane's pieces of a row of K, row i of 16, and of its part of a row of V
+template <class S> __device__ __forceinline__ unsigned k_offset(int p, int i, int g, int row_bytes)
+{
+    const int at = 64 * p + g * S::PB;
+    return i * row_bytes + (at < row_bytes - S::PB ? at : row_bytes - S::PB); // (what is beyond a row meets zeros of q)
+}
+template <class S> __device__ __forceinline__ unsigned v_offset(int i, int dk) { return i * S::C < dk ? i * S::VB : 0; }
+
+// The page of the 16 tokens from `at` on (-1: none), and their place in the cache in vectors (where a page is none, some place)
+__device__ __forceinline__ int page_at(const CacheAttnArgs &a, const int32_t *table, int last_page, int at)
+{
+    const int nth = at >> a.page_shift;
+    return __builtin_amdgcn_readfirstlane(nth <= last_page ? table[nth] : -1);
+}
+__device__ __forceinline__ bool is_page(const CacheAttnArgs &a, int page) { return page >= 0 && page < a.pages; }
+__device__ __forceinline__ int64_t place_of(const CacheAttnArgs &a, int page, int head, int at)
+{
+    return (((is_page(a, page) ? (int64_t)page : 0) * a.kv_heads + head) << a.page_shift) + (at & ((1 << a.page_shift) - 1));
+}
+
+// A token's scale of V as 2^exponent times the rest
+struct Split { float exponent, back, rest; }; // back = 2^-exponent
+__device__ __forceinline__ Split split_scale(float vs)
+{
+    int x = __builtin_amdgcn_frexp_expf(vs);
+    x = x < -100 ? -100 : x;
+    const float back = __builtin_amdgcn_ldexpf(1.f, -x);
+    return {(float)x, back, vs * back};
+}
+
+// Which piece, head and rows a workgroup has.  Tiles of rows of the same piece and head follow each other on one XCD (workgroups go round the eight of
+// them).
+struct Unit { int piece, head, rows_at; };
+__device__ __forceinline__ Unit unit_of(const CacheAttnArgs &a, int row_tile)
+{
+    int unit = blockIdx.x, tile = 0;
+    if (a.row_tiles > 1) {
+        const int turn = blockIdx.x / (8 * a.row_tiles), in = blockIdx.x - turn * 8 * a.row_tiles;
+        tile = in / 8;
+        unit = turn * 8 + in % 8;
+    }
+    const int head = unit / a.units_per_head;
+    return {unit - head * a.units_per_head, head, tile * row_tile};
+}
+
+// C results of a row from column col on: to the output, or to a piece's place
+template <int D, int TYPE, int C> __device__ __forceinline__ void put(const CacheAttnArgs &a, const Cut &cut, int head, int row, int col, float (&v)[C], float m, float l)
+{
+    if (cut.pieces > 1) {
+        const int64_t line = ((int64_t)(cut.slot + cut.index) * a.kv_heads + head) * a.rows_held + row;
+        store_real<MC_F32, C>(a.partial, line * D + col, v);
+        if (col == 0) *reinterpret_cast<float2 *>(a.sums + line * 2) = make_float2(m, l);
+    } else if (col < a.dk) {
+        const float inv = l == 0 ? 0.f : 1.f / l; // (a row that sees nothing is zero)
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[c] *= inv;
+        store_real<TYPE, C>(a.o, out_at(a, cut.of, head, row) + col, v);
+    }
+}
+
+// Up to 16 rows: the waves of a workgroup take a piece's tiles of 32 tokens in turn, from memory through registers alone.
+template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_kernel(CacheAttnArgs a)
+{
+    typedef Shape<D, BITS, TYPE> S;
+    constexpr int PLANES = S::PLANES, C = S::C, PB = S::PB;
     __shared__ float shared_o[CACHE_WAVES][16][D + 4];
     __shared__ float shared_m[CACHE_WAVES][16], shared_l[CACHE_WAVES][16];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-    const int head = blockIdx.y, row0 = blockIdx.z * 16;
-    const Cut cut = cut_of<true>(a, blockIdx.x);
+    const Unit unit = unit_of(a, 16);
+    if (unit.head >= a.kv_heads) return;
+    const Cut cut = cut_of<true>(a, unit.piece);
     if (cut.b < 0) return;
-    const Sequence s = sequence(a, cut.b);
-    const int n = __builtin_amdgcn_readfirstlane(s.n), length = __builtin_amdgcn_readfirstlane(s.length), start = __builtin_amdgcn_readfirstlane(s.start);
-    if (row0 >= n * a.group) return;
+    const Sequence s = cut.of;
+    const int rows = s.n * a.group, head = unit.head, row0 = unit.rows_at;
+    if (row0 >= rows) return;
+    const int held = s.length - s.n;
 
-    // this lane's row (rows beyond the last repeat it), and what it may see: all tokens below `all`, and those of the tree's bits from `held` on
-    const int row = row0 + i < n * a.group ? row0 + i : n * a.group - 1, token = row / a.group, q_head = head * a.group + row % a.group;
-    const int held = length - n;
-    const int all = a.tree ? held : held + token + 1;
-    const uint64_t bits = a.tree ? a.tree[start + token] & (n < 64 ? (1ull << n) - 1 : ~0ull) : 0;
-    const int last_row = row0 + 15 < n * a.group ? row0 + 15 : n * a.group - 1;
-    const int end = a.tree ? length : held + last_row / a.group + 1; // no row of this tile sees more
-    const int certain = a.tree ? held : held + row0 / a.group + 1;   // every row sees this many
-
-    // q, times a power of two that brings the row's largest into [1, 2)
-    const void *q = a.q;
-    const int64_t q_at = (start + (int64_t)token) * a.q_token_stride + q_head * a.q_head_stride;
-    auto element = [&](int step, int e) { // the code that place e of step `step` meets
-        return BITS == 8 ? (PB == 16 ? 64 * (step / 2) + 16 * g + 8 * (step % 2) + e : 0) : NK > 0 && PB == 16 ? 128 * (step / 4) + 32 * g + 8 * (step % 4) + nibble_order(e)
-                                                                                                              : 16 * g + 8 * step + nibble_order(e);
-    };
-    float top = 0;
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = element(st, e);
-            if (d < a.dk) top = fmaxf(top, fabsf(real_at<TYPE>(q, q_at + d)));
-        }
-    top = max_of_groups(top);
-    int up = top > 0 && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
-    h8 qo[PLANES][STEPS];
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = element(st, e);
-            const float v = d < a.dk ? __builtin_amdgcn_ldexpf(real_at<TYPE>(q, q_at + d), -up) : 0.f;
-            qo[0][st][e] = (_Float16)v;
-            if (PLANES == 2) qo[PLANES - 1][st][e] = (_Float16)((v - (float)(_Float16)v) * 2048.f);
-        }
-    const float row_scale = __builtin_amdgcn_ldexpf(a.score_scale, up);
+    const int row = row0 + i < rows ? row0 + i : rows - 1; // (rows beyond the last repeat it)
+    const Sight sight = sight_of(a, s, row / a.group);
+    h8 q[PLANES][S::STEPS];
+    const float row_scale = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)(row / a.group)) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q);
+    const int last_row = row0 + 15 < rows ? row0 + 15 : rows - 1;
+    const int end = a.tree ? s.length : held + last_row / a.group + 1; // no row sees more
+    const int certain = a.tree ? held : held + row0 / a.group + 1;     // every row sees this many
 
     const int row_bytes = a.dk * BITS / 8;
-    const int v_at = (i * C < a.dk ? i * C : 0) * BITS / 8;
-    int k_at[NK];
+    unsigned k_at[S::NK], v_at[4];
 #pragma unroll
-    for (int p = 0; p < NK; ++p) {
-        const int at = 64 * p + g * PB;
-        k_at[p] = i * row_bytes + (at < row_bytes - PB ? at : row_bytes - PB);
-    }
+    for (int p = 0; p < S::NK; ++p) k_at[p] = k_offset<S>(p, i, g, row_bytes);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v_at[r] = (4 * g + r) * row_bytes + v_offset<S>(i, a.dk);
 
+    struct Pages { int id[2]; };
+    const int last_page = s.length > 0 ? (s.length - 1) >> a.page_shift : -1;
+    const int32_t *table = a.table + cut.b * a.table_stride;
+    auto pages_of = [&](int tile) {
+        return Pages{{page_at(a, table, last_page, tile * CACHE_TILE), page_at(a, table, last_page, tile * CACHE_TILE + 16)}};
+    };
     struct Tile {
-        Words<PB / 4> k[2][NK];
-        Words<VN> v[2][4];
+        Words<PB / 4> k[2][S::NK];
+        Words<(S::VB + 3) / 4> v[2][4];
         v4f ks[2], vs[2];
         bool there[2];
     };
-    const int last_page = length > 0 ? (length - 1) >> a.page_shift : 0;
-    auto load = [&](Tile &t, int tile) {
+    auto load = [&](Tile &t, int tile, Pages pages) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int at = tile * CACHE_TILE + half * 16;
-            const int nth = at >> a.page_shift < last_page ? at >> a.page_shift : last_page;
-            int64_t page = length > 0 ? a.table[cut.b * a.table_stride + nth] : -1;
-            t.there[half] = page >= 0 && page < a.pages;
-            if (!t.there[half]) page = 0;
-            const int64_t first = ((page * a.kv_heads + head) << a.page_shift) + (at & ((1 << a.page_shift) - 1));
+            t.there[half] = is_page(a, pages.id[half]);
+            const int64_t first = place_of(a, pages.id[half], head, tile * CACHE_TILE + half * 16);
             const uint8_t *k = a.k_codes + first * row_bytes, *v = a.v_codes + first * row_bytes;
 #pragma unroll
-            for (int p = 0; p < NK; ++p) t.k[half][p] = load_words<PB / 4>(k + k_at[p]);
+            for (int p = 0; p < S::NK; ++p) t.k[half][p] = load_bytes<PB>(k, k_at[p]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const uint8_t *from = v + (4 * g + r) * row_bytes + v_at;
-                if constexpr (VW == 0) t.v[half][r].w[0] = *reinterpret_cast<const unsigned short *>(from);
-                else t.v[half][r] = load_words<VN>(from);
-            }
+            for (int r = 0; r < 4; ++r) t.v[half][r] = load_bytes<S::VB>(v, v_at[r]);
             t.ks[half] = *reinterpret_cast<const v4f *>(a.k_scales + first + 4 * g);
             t.vs[half] = *reinterpret_cast<const v4f *>(a.v_scales + first + 4 * g);
         }
     };
 
     float m = NONE, l = 0;
-    v4f o[PLANES][C];
+    v4f o[C];
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[p][c] = (v4f){0, 0, 0, 0};
+    for (int c = 0; c < C; ++c) o[c] = (v4f){0, 0, 0, 0};
 
-    auto take = [&](const Tile &t, int tile) {
-        // scores in base 2, plus the exponents of V's scales
-        float x[2][4], f[2][4], w[2][4];
-        int ex[2][4];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            v4f sc[PLANES];
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) sc[p] = (v4f){0, 0, 0, 0};
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                constexpr int PER = PB * 8 / BITS / 8; // steps of a piece
-                const auto &piece = t.k[half][st / PER];
-                const int at = st % PER;
-                const h8 k = BITS == 8 ? row_operand<BITS>(piece.w[2 * at], piece.w[2 * at + 1]) : row_operand<BITS>(piece.w[at], 0u);
-#pragma unroll
-                for (int p = 0; p < PLANES; ++p) sc[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qo[p][st], sc[p], 0, 0, 0);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float vs = t.vs[half][r];
-                int e = __builtin_amdgcn_frexp_expf(vs);
-                e = e < -100 ? -100 : e;
-                ex[half][r] = e;
-                f[half][r] = __builtin_amdgcn_ldexpf(vs, -e);
-                const float sum = PLANES == 2 ? __builtin_fmaf(sc[PLANES - 1][r], 1.f / 2048, sc[0][r]) : sc[0][r];
-                x[half][r] = __builtin_fmaf(sum * row_scale, t.ks[half][r], (float)e);
-            }
-        }
-        const int at = tile * CACHE_TILE;
-        const bool masked = at + CACHE_TILE > certain || !t.there[0] || !t.there[1];
-        if (masked) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int token = at + 16 * half + 4 * g + r, later = token - held;
-                    const bool seen = t.there[half] && token < length && (token < all || (later >= 0 && later < 64 && (bits >> later & 1)));
-                    if (!seen) {
-                        x[half][r] = NONE;
-                        f[half][r] = 0;
-                    }
-                }
-        }
-        float top = NONE;
+    auto take = [&](Tile &tile, int number) {
+        v4f sc[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[half][r]);
+            for (int st = 0; st < S::STEPS; ++st) {
+                const auto &piece = tile.k[half][st / S::PER];
+                const int at = st % S::PER;
+                const h8 k = BITS == 8 ? row_operand<BITS>(piece.w[2 * at % (PB / 4)], piece.w[(2 * at + 1) % (PB / 4)]) : row_operand<BITS>(piece.w[at], 0u);
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+                    sc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][st], st == 0 && p == 0 ? (v4f){0, 0, 0, 0} : sc[half], 0, 0, 0);
+            }
+        const int at = number * CACHE_TILE;
+        const bool masked = at + CACHE_TILE > certain || !tile.there[0] || !tile.there[1];
+        Split split[8];
+        float x[8]; // scores in base 2, plus the exponents of V's scales
+        unsigned seen = 0xff;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            split[e] = split_scale(tile.vs[e / 4][e % 4]);
+            x[e] = __builtin_fmaf(sc[e / 4][e % 4] * row_scale, tile.ks[e / 4][e % 4], split[e].exponent);
+        }
+        if (masked) {
+            seen = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned yes = sees(sight, at + 16 * (e / 4) + 4 * g + e % 4, held, tile.there[e / 4]);
+                seen |= yes << e;
+                x[e] = yes ? x[e] : NONE;
+            }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
         top = max_of_groups(top);
         if (__any(top > m)) {
             const float to = fmaxf(top, m), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= by;
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-                for (int c = 0; c < C; ++c) o[p][c] *= by;
+            for (int c = 0; c < C; ++c) o[c] *= by;
         }
         const float from = (m == NONE ? 0.f : m) - UP;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(x[half][r] - from);
-                l += __builtin_amdgcn_ldexpf(p, -ex[half][r]);
-                w[half][r] = p * f[half][r];
-            }
-        h8 wo[PLANES];
+        h8 w[PLANES];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float v = w[e / 4][e % 4];
+            const float p = __builtin_amdgcn_exp2f(x[e] - from);
+            l = __builtin_fmaf(p, split[e].back, l);
+            float v = p * split[e].rest;
+            if (masked) v = seen >> e & 1 ? v : 0.f; // (whatever the scale there is)
             if (PLANES == 2) asm("" : "+v"(v)); // (one product, rounded once: the first half by a fused rounding, and the second from another would differ at a tie)
-            wo[0][e] = (_Float16)v;
-            if (PLANES == 2) wo[PLANES - 1][e] = (_Float16)((v - (float)(_Float16)v) * 2048.f);
+            w[0][e] = (_Float16)v;
+            if (PLANES == 2) w[PLANES - 1][e] = (_Float16)(v - (float)(_Float16)v);
+        }
+        if (BITS == 4) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < (S::VB + 3) / 4; ++e) tile.v[half][r].w[e] ^= 0x88888888u;
         }
         constexpr int PER_WORD = 32 / BITS; // columns of a word
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int q = c / PER_WORD, in = c % PER_WORD;
-            const h8 v = operand(column_pair<BITS>(t.v[0][0].w[q], t.v[0][1].w[q], in), column_pair<BITS>(t.v[0][2].w[q], t.v[0][3].w[q], in),
-                                 column_pair<BITS>(t.v[1][0].w[q], t.v[1][1].w[q], in), column_pair<BITS>(t.v[1][2].w[q], t.v[1][3].w[q], in));
+            const int n = c / PER_WORD, in = c % PER_WORD;
+            const h8 v = operand(column_pair<BITS>(tile.v[0][0].w[n], tile.v[0][1].w[n], in), column_pair<BITS>(tile.v[0][2].w[n], tile.v[0][3].w[n], in),
+                                 column_pair<BITS>(tile.v[1][0].w[n], tile.v[1][1].w[n], in), column_pair<BITS>(tile.v[1][2].w[n], tile.v[1][3].w[n], in));
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) o[p][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, wo[p], o[p][c], 0, 0, 0);
+            for (int p = 0; p < PLANES; ++p) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[p], o[c], 0, 0, 0);
         }
     };
 
-    // the waves take the piece's tiles in turn
+    // A tile is asked for while the one before is worked on, and its pages one tile earlier.
     const int64_t from_tile = (int64_t)cut.index * cut.each;
     const int tiles = end > 0 ? (end - 1) / CACHE_TILE + 1 : 0, to_tile = tiles - from_tile < cut.each ? tiles : (int)from_tile + cut.each;
-    for (int64_t tile = from_tile + wave; tile < to_tile; tile += CACHE_WAVES) {
-        Tile t;
-        load(t, (int)tile);
-        take(t, (int)tile);
+    int tile = (int)from_tile + wave;
+    if (from_tile + wave < to_tile) {
+        constexpr int STEP = CACHE_WAVES;
+        Tile one, two;
+        load(one, tile, pages_of(tile));
+        Pages next = pages_of(tile + STEP);
+        for (;;) {
+            if (tile + STEP < to_tile) load(two, tile + STEP, next);
+            next = pages_of(tile + 2 * STEP);
+            take(one, tile);
+            tile += STEP;
+            if (tile >= to_tile) break;
+            if (tile + STEP < to_tile) load(one, tile + STEP, next);
+            next = pages_of(tile + 2 * STEP);
+            take(two, tile);
+            tile += STEP;
+            if (tile >= to_tile) break;
+        }
     }
 
     // the waves' results meet in LDS
@@ -382,102 +500,364 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
         shared_m[wave][i] = m;
         shared_l[wave][i] = l;
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < C; c += 4)
+            *reinterpret_cast<v4f *>(&shared_o[wave][i][(4 * g + r) * C + c]) = (v4f){o[c][r], o[c + 1][r], o[c + 2][r], o[c + 3][r]};
     __syncthreads();
-    float top_m = NONE;
-#pragma unroll
-    for (int w = 0; w < CACHE_WAVES; ++w) top_m = fmaxf(top_m, shared_m[w][i]);
-    const float by = m == NONE ? 0.f : __builtin_amdgcn_exp2f(m - top_m);
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float v = PLANES == 2 ? __builtin_fmaf(o[PLANES - 1][c][r], 1.f / 2048, o[0][c][r]) : o[0][c][r];
-            shared_o[wave][i][(4 * g + r) * C + c] = m == NONE ? 0.f : v * by;
-        }
-    __syncthreads();
-    const int out_row = threadIdx.x / 16, col = threadIdx.x % 16 * C;
+    const int of = threadIdx.x / 16, col = threadIdx.x % 16 * C;
     float sum[C] = {}, all_m = NONE, all_l = 0;
 #pragma unroll
-    for (int w = 0; w < CACHE_WAVES; ++w) all_m = fmaxf(all_m, shared_m[w][out_row]);
+    for (int w = 0; w < CACHE_WAVES; ++w) all_m = fmaxf(all_m, shared_m[w][of]);
 #pragma unroll
     for (int w = 0; w < CACHE_WAVES; ++w) {
-        if (shared_m[w][out_row] != NONE) all_l += shared_l[w][out_row] * __builtin_amdgcn_exp2f(shared_m[w][out_row] - all_m);
+        if (shared_m[w][of] == NONE) continue;
+        const float by = __builtin_amdgcn_exp2f(shared_m[w][of] - all_m);
+        all_l += shared_l[w][of] * by;
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum[c] += shared_o[w][out_row][col + c];
+        for (int c = 0; c < C; ++c) sum[c] += shared_o[w][of][col + c] * by;
     }
-    if (cut.pieces > 1) {
-        const int64_t at = (((int64_t)(cut.slot + cut.index) * a.kv_heads + head) * a.row_tiles + blockIdx.z) * 16 + out_row;
-        float *to = a.partial + at * (D + 2);
-        if (threadIdx.x % 16 == 0) {
-            to[D] = all_m;
-            to[D + 1] = all_l;
+    if (row0 + of < rows) put<D, TYPE, C>(a, cut, head, row0 + of, col, sum, all_m, all_l);
+}
+
+// More rows: each wave has R tiles of 16 rows, and the workgroup converts a piece's tokens, 64 at a time (32 for D = 256), once for all of them.  The operands lie in LDS as
+// the MFMAs take them, 16 bytes a lane side by side, two tiles of tokens in turn; beside them what a token's scales are taken apart into.
+template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_rows_kernel(CacheAttnArgs a)
+{
+    typedef Shape<D, BITS, TYPE> S;
+    constexpr int PLANES = S::PLANES, C = S::C, PB = S::PB, STEPS = S::STEPS;
+    constexpr int T = D <= 128 ? 64 : 32, BLOCKS = T / 16, PAIRS = T / 32;  // tokens of a tile, in blocks of 16 and 32
+    constexpr int KU = BLOCKS * S::NK / CACHE_WAVES;                        // pieces of K that a wave converts: 16 tokens each
+    constexpr int VSPLIT = CACHE_WAVES / BLOCKS, VB = S::VB / VSPLIT, VC = C / VSPLIT; // waves that share 16 tokens of V, by columns
+    static_assert(KU * CACHE_WAVES == BLOCKS * S::NK && VC * VSPLIT == C, "even shares");
+    struct Stage {
+        uint8_t k[BLOCKS * STEPS * 1024], v[PAIRS * C * 1024];
+        float scale[T], exponent[T], back[T], rest[T];
+    };
+    __shared__ __attribute__((aligned(16))) Stage stages[2];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+    const Unit unit = unit_of(a, CACHE_WAVES * 16 * R);
+    if (unit.head >= a.kv_heads) return;
+    const Cut cut = cut_of<true>(a, unit.piece);
+    if (cut.b < 0) return;
+    const Sequence s = cut.of;
+    const int rows = s.n * a.group, head = unit.head;
+    if (unit.rows_at >= rows) return;
+    const int held = s.length - s.n;
+    const int group_last = unit.rows_at + CACHE_WAVES * 16 * R - 1 < rows ? unit.rows_at + CACHE_WAVES * 16 * R - 1 : rows - 1;
+    const int end = a.tree ? s.length : held + group_last / a.group + 1;   // no row of the workgroup sees more
+    // this wave's rows (none: it converts for the others), the first token that none of them sees, and the first that not every one sees
+    const int row0 = unit.rows_at + wave * 16 * R, wave_last = row0 + 16 * R - 1 < rows ? row0 + 16 * R - 1 : rows - 1;
+    const int wave_end = row0 >= rows ? 0 : a.tree ? s.length : held + wave_last / a.group + 1;
+    const int certain = a.tree ? held : held + row0 / a.group + 1;
+
+    Sight sight[R];
+    float row_scale[R], m[R], l[R];
+    h8 q[R][PLANES][STEPS];
+    v4f o[R][C];
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const int row = row0 + 16 * t + i < rows ? row0 + 16 * t + i : rows - 1; // (rows beyond the last repeat it)
+        sight[t] = sight_of(a, s, row / a.group);
+        row_scale[t] = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)(row / a.group)) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q[t]);
+        m[t] = NONE;
+        l[t] = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[t][c] = (v4f){0, 0, 0, 0};
+    }
+
+    // what this wave converts: pieces KU wave .. of K (piece p of block p / NK), a block of V and some of its columns; waves 0 and 1 the scales
+    const int row_bytes = a.dk * BITS / 8, v_block = wave % BLOCKS, v_column = wave / BLOCKS * VC;
+    unsigned k_at[KU], v_at[4];
+#pragma unroll
+    for (int u = 0; u < KU; ++u) k_at[u] = k_offset<S>((wave * KU + u) % S::NK, i, g, row_bytes);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v_at[r] = (4 * g + r) * row_bytes + (i * C + v_column < a.dk ? i * S::VB + wave / BLOCKS * VB : 0);
+    const int last_page = s.length > 0 ? (s.length - 1) >> a.page_shift : -1;
+    const int32_t *table = a.table + cut.b * a.table_stride;
+
+    typedef int Pages __attribute__((ext_vector_type(BLOCKS)));
+    auto pages_of = [&](int at) {
+        Pages p;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) p[b] = page_at(a, table, last_page, at + 16 * b);
+        return p;
+    };
+    struct Codes {
+        Words<PB / 4> k[KU];
+        Words<(VB + 3) / 4> v[4];
+        float scale;
+    };
+    auto load = [&](Codes &t, int at, const Pages &pages) {
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+            const int b = (wave * KU + u) / S::NK;
+            int page = pages[0];
+#pragma unroll
+            for (int e = 1; e < BLOCKS; ++e) page = b == e ? pages[e] : page;
+            t.k[u] = load_bytes<PB>(a.k_codes + place_of(a, page, head, at + 16 * b) * row_bytes, k_at[u]);
+        }
+        int page = pages[0];
+#pragma unroll
+        for (int e = 1; e < BLOCKS; ++e) page = v_block == e ? pages[e] : page;
+        const uint8_t *v = a.v_codes + place_of(a, page, head, at + 16 * v_block) * row_bytes;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t.v[r] = load_bytes<VB>(v, v_at[r]);
+        if (wave < 2 && lane < T) {
+            int64_t place = place_of(a, pages[0], head, at);
+#pragma unroll
+            for (int e = 1; e < BLOCKS; ++e) {
+                const int64_t other = place_of(a, pages[e], head, at + 16 * e);
+                place = g == e ? other : place;
+            }
+            t.scale = (wave ? a.v_scales : a.k_scales)[place + i];
+        }
+    };
+    auto convert = [&](Codes &t, Stage &to) {
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+            const int b = (wave * KU + u) / S::NK, p = (wave * KU + u) % S::NK;
+#pragma unroll
+            for (int e = 0; e < S::PER; ++e)
+                *reinterpret_cast<h8 *>(&to.k[(b * STEPS + p * S::PER + e) * 1024 + lane * 16]) =
+                    BITS == 8 ? row_operand<BITS>(t.k[u].w[2 * e % (PB / 4)], t.k[u].w[(2 * e + 1) % (PB / 4)]) : row_operand<BITS>(t.k[u].w[e], 0u);
+        }
+        if (BITS == 4) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < (VB + 3) / 4; ++e) t.v[r].w[e] ^= 0x88888888u;
+        }
+        constexpr int PER_WORD = 32 / BITS;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+            const int n = c / PER_WORD, in = c % PER_WORD;
+            *reinterpret_cast<uint2 *>(&to.v[(v_block / 2 * C + v_column + c) * 1024 + lane * 16 + v_block % 2 * 8]) =
+                make_uint2(column_pair<BITS>(t.v[0].w[n], t.v[1].w[n], in), column_pair<BITS>(t.v[2].w[n], t.v[3].w[n], in));
+        }
+        if (lane < T) {
+            if (wave == 0) to.scale[lane] = t.scale;
+            if (wave == 1) {
+                const Split v = split_scale(t.scale);
+                to.exponent[lane] = v.exponent;
+                to.back[lane] = v.back;
+                to.rest[lane] = v.rest;
+            }
+        }
+    };
+
+    auto take = [&](const Stage &st, int at, const Pages &pages) {
+        bool masked = at + T > certain;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) masked = masked || !is_page(a, pages[b]);
+        v4f sc[R][BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) {
+                const h8 op = *reinterpret_cast<const h8 *>(&st.k[(b * STEPS + k) * 1024 + lane * 16]);
+#pragma unroll
+                for (int t = 0; t < R; ++t)
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p)
+                        sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[t][p][k], k == 0 && p == 0 ? (v4f){0, 0, 0, 0} : sc[t][b], 0, 0, 0);
+            }
+        // scores in base 2, plus the exponents of V's scales
+        unsigned seen[R];
+        float top[R];
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            seen[t] = ~0u;
+            top[t] = NONE;
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c) to[col + c] = sum[c];
-        return;
-    }
-    if (row0 + out_row >= n * a.group || col >= a.dk) return;
-    const int out_token = (row0 + out_row) / a.group, out_head = head * a.group + (row0 + out_row) % a.group;
-    const float inv = all_l == 0 ? 0.f : 1.f / all_l; // (a row that sees nothing is zero)
-    auto *to = static_cast<typename RealOf<TYPE>::type *>(a.o) + (start + (int64_t)out_token) * a.o_token_stride + out_head * a.o_head_stride + col;
+        for (int b = 0; b < BLOCKS; ++b) {
+            const v4f ks = *reinterpret_cast<const v4f *>(&st.scale[16 * b + 4 * g]), ex = *reinterpret_cast<const v4f *>(&st.exponent[16 * b + 4 * g]);
 #pragma unroll
-    for (int c = 0; c < C; ++c) to[c] = (typename RealOf<TYPE>::type)(sum[c] * inv);
+            for (int t = 0; t < R; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sc[t][b][r] = __builtin_fmaf(sc[t][b][r] * row_scale[t], ks[r], ex[r]);
+        }
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                seen[t] = 0;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const unsigned yes = sees(sight[t], at + 16 * b + 4 * g + r, held, is_page(a, pages[b]));
+                        seen[t] |= yes << (4 * b + r);
+                        sc[t][b][r] = yes ? sc[t][b][r] : NONE;
+                    }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top[t] = fmaxf(top[t], sc[t][b][r]);
+            top[t] = max_of_groups(top[t]);
+            if (__any(top[t] > m[t])) {
+                const float to = fmaxf(top[t], m[t]), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m[t] - to);
+                m[t] = to;
+                l[t] *= by;
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[t][c] *= by;
+            }
+        }
+#pragma unroll
+        for (int pair = 0; pair < PAIRS; ++pair) {
+            h8 w[R][PLANES];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int b = 2 * pair + half;
+                const v4f back = *reinterpret_cast<const v4f *>(&st.back[16 * b + 4 * g]), rest = *reinterpret_cast<const v4f *>(&st.rest[16 * b + 4 * g]);
+#pragma unroll
+                for (int t = 0; t < R; ++t) {
+                    const float from = (m[t] == NONE ? 0.f : m[t]) - UP;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float p = __builtin_amdgcn_exp2f(sc[t][b][r] - from);
+                        l[t] = __builtin_fmaf(p, back[r], l[t]);
+                        float v = p * rest[r];
+                        if (masked) v = seen[t] >> (4 * b + r) & 1 ? v : 0.f;
+                        if (PLANES == 2) asm("" : "+v"(v)); // (as above)
+                        w[t][0][4 * half + r] = (_Float16)v;
+                        if (PLANES == 2) w[t][PLANES - 1][4 * half + r] = (_Float16)(v - (float)(_Float16)v);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const h8 v = *reinterpret_cast<const h8 *>(&st.v[(pair * C + c) * 1024 + lane * 16]);
+#pragma unroll
+                for (int t = 0; t < R; ++t)
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][p], o[t][c], 0, 0, 0);
+            }
+        }
+    };
+
+    const int64_t from = (int64_t)cut.index * cut.each * CACHE_TILE, most = from + (int64_t)cut.each * CACHE_TILE;
+    const int to = end < most ? end : (int)most;
+    if (from < to) {
+        Codes codes;
+        int at = (int)from;
+        Pages here = pages_of(at);
+        load(codes, at, here);
+        convert(codes, stages[0]);
+        for (int turn = 0;; turn ^= 1) {
+            __syncthreads();
+            const bool more = at + T < to;
+            Pages next = here;
+            if (more) {
+                next = pages_of(at + T);
+                load(codes, at + T, next);
+            }
+            if (at < wave_end) take(stages[turn], at, here);
+            if (!more) break;
+            convert(codes, stages[turn ^ 1]);
+            at += T;
+            here = next;
+        }
+    }
+
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const float sum_l = sum_of_groups(l[t]);
+        const int row = row0 + 16 * t + i;
+        if (row >= rows) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[c] = o[t][c][r];
+            put<D, TYPE, C>(a, cut, head, row, (4 * g + r) * C, v, m[t], sum_l);
+        }
+    }
 }
 
-// Pieces of a sequence that was cut, joined in their order: one workgroup per sequence, head and row tile.
+// Pieces of sequences that were cut, joined in their order: a wave per row, D / 4 lanes per piece.
 template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheAttnArgs a)
 {
-    constexpr int C = D / 16;
+    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, AHEAD = 8;
     const Cut cut = cut_of<false>(a, blockIdx.x);
     if (cut.pieces <= 1) return;
-    const Sequence s = sequence(a, cut.b);
-    const int out_row = threadIdx.x / 16, col = threadIdx.x % 16 * C, row = blockIdx.z * 16 + out_row;
-    if (row >= s.n * a.group) return;
-    const int64_t step = (int64_t)a.kv_heads * a.row_tiles * 16 * (D + 2);
-    const float *from = a.partial + ((((int64_t)cut.slot * a.kv_heads + blockIdx.y) * a.row_tiles + blockIdx.z) * 16 + out_row) * (D + 2);
-    float m = NONE, l = 0, sum[C] = {};
-    for (int p = 0; p < cut.pieces; ++p) m = fmaxf(m, from[p * step + D]);
-    for (int p = 0; p < cut.pieces; ++p) {
-        const float mp = from[p * step + D];
-        if (mp == NONE) continue;
-        const float by = __builtin_amdgcn_exp2f(mp - m);
-        l += from[p * step + D + 1] * by;
+    const int lane = threadIdx.x & 63, row = blockIdx.z * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
+    if (row >= cut.of.n * a.group) return;
+    const int64_t line = ((int64_t)cut.slot * a.kv_heads + head) * a.rows_held + row, step = (int64_t)a.kv_heads * a.rows_held;
+    const int col = lane % LANES * 4, first = lane / LANES;
+    float m = NONE;
+    for (int p = lane; p < cut.pieces; p += 64) m = fmaxf(m, a.sums[(line + p * step) * 2]);
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum[c] += from[p * step + col + c] * by;
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    float l = 0;
+    v4f sum = {0, 0, 0, 0};
+    for (int p0 = 0; p0 < cut.pieces; p0 += AHEAD * AT_ONCE) {
+        v4f v[AHEAD];
+        float2 ml[AHEAD];
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const int p = p0 + e * AT_ONCE + first;
+            const int64_t at = line + (p < cut.pieces ? p : 0) * step;
+            v[e] = *reinterpret_cast<const v4f *>(a.partial + at * D + col);
+            ml[e] = *reinterpret_cast<const float2 *>(a.sums + at * 2);
+            if (p >= cut.pieces) ml[e].x = NONE;
+        }
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            if (ml[e].x == NONE) continue;
+            const float by = __builtin_amdgcn_exp2f(ml[e].x - m);
+            l += ml[e].y * by;
+            sum += v[e] * by;
+        }
     }
-    if (col >= a.dk) return;
-    const int token = row / a.group, head = blockIdx.y * a.group + row % a.group;
-    const float inv = l == 0 ? 0.f : 1.f / l;
-    auto *to = static_cast<typename RealOf<TYPE>::type *>(a.o) + (s.start + (int64_t)token) * a.o_token_stride + head * a.o_head_stride + col;
 #pragma unroll
-    for (int c = 0; c < C; ++c) to[c] = (typename RealOf<TYPE>::type)(sum[c] * inv);
+    for (int o = LANES; o < 64; o <<= 1) {
+        l += __shfl_xor(l, o, 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o, 64);
+    }
+    if (first != 0 || col >= a.dk) return;
+    const float inv = l == 0 ? 0.f : 1.f / l;
+    const float out[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+    store_real<TYPE, 4>(a.o, out_at(a, cut.of, head, row) + col, out);
 }
 
-template <int D, int BITS, int TYPE> hipError_t launch(const CacheAttnArgs &a, hipStream_t s)
+template <int D, int BITS, int TYPE> hipError_t launch(CacheAttnArgs a, int row_tile, hipStream_t s)
 {
-    const unsigned pieces = (unsigned)(a.partial ? a.pieces + a.batch : a.batch);
-    const hipError_t e = launch_kernel((cache_attention_kernel<D, BITS, TYPE>), dim3(pieces, a.kv_heads, a.row_tiles), dim3(CACHE_WAVES * 64), 0, s, a);
+    a.units_per_head = a.partial ? a.pieces + a.batch : a.batch;
+    int64_t groups = (int64_t)a.units_per_head * a.kv_heads;
+    if (a.row_tiles > 1) groups = (groups + 7) / 8 * 8 * a.row_tiles;
+    const dim3 grid((unsigned)groups), block(CACHE_WAVES * 64);
+    const hipError_t e = row_tile == 16   ? launch_kernel((cache_attention_kernel<D, BITS, TYPE>), grid, block, 0, s, a)
+                         : row_tile == 64 ? launch_kernel((cache_attention_rows_kernel<D, BITS, TYPE, 1>), grid, block, 0, s, a)
+                                          : launch_kernel((cache_attention_rows_kernel<D, BITS, TYPE, 2>), grid, block, 0, s, a);
     if (e != hipSuccess || !a.partial) return e;
-    return launch_kernel((cache_attention_join_kernel<D, TYPE>), dim3(a.batch, a.kv_heads, a.row_tiles), dim3(256), 0, s, a);
+    return launch_kernel((cache_attention_join_kernel<D, TYPE>), dim3(a.batch, a.kv_heads, (a.rows_held + 3) / 4), dim3(256), 0, s, a);
 }
 
-template <int BITS, int TYPE> hipError_t launch_dim(const CacheAttnArgs &a, hipStream_t s)
+template <int BITS, int TYPE> hipError_t launch_dim(const CacheAttnArgs &a, int row_tile, hipStream_t s)
 {
-    if (a.dk <= 64) return launch<64, BITS, TYPE>(a, s);
-    if (a.dk <= 128) return launch<128, BITS, TYPE>(a, s);
-    return launch<256, BITS, TYPE>(a, s);
+    if (a.dk <= 64) return launch<64, BITS, TYPE>(a, row_tile, s);
+    if (a.dk <= 128) return launch<128, BITS, TYPE>(a, row_tile, s);
+    return launch<256, BITS, TYPE>(a, row_tile, s);
 }
 
-template <int BITS> hipError_t launch_type(const CacheAttnArgs &a, mc_type type, hipStream_t s)
+template <int BITS> hipError_t launch_type(const CacheAttnArgs &a, mc_type type, int row_tile, hipStream_t s)
 {
-    if (type == MC_F32) return launch_dim<BITS, MC_F32>(a, s);
-    if (type == MC_F16) return launch_dim<BITS, MC_F16>(a, s);
-    return launch_dim<BITS, MC_BF16>(a, s);
+    if (type == MC_F32) return launch_dim<BITS, MC_F32>(a, row_tile, s);
+    if (type == MC_F16) return launch_dim<BITS, MC_F16>(a, row_tile, s);
+    return launch_dim<BITS, MC_BF16>(a, row_tile, s);
 }
 
 } // namespace
 
-hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits, hipStream_t s)
+hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits, int row_tile, hipStream_t s)
 {
-    return bits == 8 ? launch_type<8>(a, type, s) : launch_type<4>(a, type, s);
+    return bits == 8 ? launch_type<8>(a, type, row_tile, s) : launch_type<4>(a, type, row_tile, s);
 }

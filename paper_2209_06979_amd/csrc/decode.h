@@ -58,36 +58,39 @@ struct CacheAttnArgs {
     void *o;
     float score_scale;           // times log2(e)
     int pieces;                  // pieces that the sequences' tokens are cut into, per head of the cache (see cache_attention_plan)
-    int row_tiles;               // tiles of rows (new token, query head of the group) at max_new tokens
-    float *partial;              // results of pieces that are not a whole sequence; null: no sequence is cut
+    int row_tiles, rows_held;    // tiles of rows (new token, query head of the group) at max_new tokens, and those rows
+    float *partial, *sums;       // rows of pieces that are not a whole sequence, and their (maximum, l); null: no sequence is cut
+    int units_per_head;          // filled by the launcher
 };
 
 hipError_t launch_rope(const RopeArgs &a, mc_type type, hipStream_t s);
 hipError_t launch_cache_write(const CacheArgs &a, mc_type type, hipStream_t s);
 hipError_t launch_cache_read(const CacheArgs &a, mc_type type, hipStream_t s);
-hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits, hipStream_t s);
+// row_tile: 16, 64 or 128 rows
+hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits, int row_tile, hipStream_t s);
 
 constexpr int CACHE_TILE = 32;         // tokens that a wave takes at a time
 constexpr int CACHE_WAVES = 4;         // waves of a workgroup, which share a piece
 constexpr int CACHE_MIN_PIECE = 8;     // tiles of the shortest piece
 constexpr int CACHE_PIECES = 1024;     // pieces asked for, over all heads of the cache and row tiles
 
-// What the launch and its workspace are made for: pieces per head asked for, row tiles, whether a sequence can be cut at all, and
-// the floats of the partial results.
-struct CacheAttnPlan { int pieces, row_tiles, row_tile; bool cut; int64_t slots, floats; };
+// What the launch and its workspace are made for: pieces per head asked for, tiles of rows, whether a sequence can be cut at all, and the
+// places for pieces' results: rows of `width` floats, and two floats for each.
+struct CacheAttnPlan { int pieces, row_tile, row_tiles, rows, width; bool cut; int64_t slots, lines; };
 inline CacheAttnPlan cache_attention_plan(int kv_heads, int dk, int group, int batch, int max_new, int64_t most_tokens)
 {
     CacheAttnPlan p = {};
-    const int64_t rows = (int64_t)max_new * group, tiles = (most_tokens + CACHE_TILE - 1) / CACHE_TILE;
-    p.row_tile = 16;
-    p.row_tiles = (int)((rows + p.row_tile - 1) / p.row_tile);
+    const int64_t tiles = (most_tokens + CACHE_TILE - 1) / CACHE_TILE;
+    p.rows = max_new * group;
+    p.width = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
+    p.row_tile = p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
+    p.row_tiles = (p.rows + p.row_tile - 1) / p.row_tile;
     const int64_t sharers = (int64_t)kv_heads * (p.row_tiles > 0 ? p.row_tiles : 1);
     p.pieces = (int)(CACHE_PIECES / sharers > 1 ? CACHE_PIECES / sharers : 1);
     p.cut = tiles > CACHE_MIN_PIECE && p.row_tiles > 0 && batch > 0;
     // sequences that are cut have more than one piece, fewer than twice the pieces their share asks for; and every sequence adds one
     // that is not full
     p.slots = p.cut ? (2 * (int64_t)p.pieces < (int64_t)p.pieces + batch ? 2 * (int64_t)p.pieces : (int64_t)p.pieces + batch) : 0;
-    const int width = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
-    p.floats = p.slots * kv_heads * p.row_tiles * p.row_tile * (width + 2);
+    p.lines = p.slots * kv_heads * p.rows;
     return p;
 }

@@ -49,7 +49,7 @@ int check_shape(const mc_cache *c, int heads, int batch, int max_new, int table_
 {
     if (heads < 1 || heads % c->kv_heads != 0 || batch < 0 || batch > 65535 || max_new < 0 || table_pages < 0) return MC_EINVAL;
     const int64_t tokens = (int64_t)table_pages * c->page_size, rows = (int64_t)max_new * (heads / c->kv_heads);
-    if (tokens >= MOST_TOKENS || rows > 65535 * 16) return MC_EINVAL;
+    if (tokens >= MOST_TOKENS || rows > 65535 * 4) return MC_EINVAL;
     if (batch * (tokens / CACHE_TILE + 1) >= MOST_TOKENS) return MC_EINVAL; // (tiles are counted in 32 bits)
     return MC_OK;
 }
@@ -152,7 +152,8 @@ extern "C" int mc_cache_read(const mc_cache *cache, const int64_t *slots_dev, in
 extern "C" size_t mc_cache_attention_workspace(const mc_cache *cache, int heads, int batch, int max_new, int table_pages)
 {
     if (!cache || cache->kv_heads < 1 || cache->page_size < 1 || check_shape(cache, heads, batch, max_new, table_pages) != MC_OK) return 0;
-    return (size_t)plan_of(cache, heads, batch, max_new, table_pages).floats * sizeof(float);
+    const CacheAttnPlan p = plan_of(cache, heads, batch, max_new, table_pages);
+    return (size_t)p.lines * (p.width + 2) * sizeof(float);
 }
 
 extern "C" int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_type type, int64_t total_new, int heads, int64_t q_token_stride,
@@ -173,7 +174,7 @@ extern "C" int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_t
         return MC_EALIGN;
     const CacheAttnPlan p = plan_of(cache, heads, batch, max_new, table_pages);
     if (p.cut) {
-        if (!workspace_dev || workspace_bytes < (size_t)p.floats * sizeof(float)) return MC_ENOMEM;
+        if (!workspace_dev || workspace_bytes < (size_t)p.lines * (p.width + 2) * sizeof(float)) return MC_ENOMEM;
         if ((reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0) return MC_EALIGN;
     }
     CacheAttnArgs a = {};
@@ -185,7 +186,9 @@ extern "C" int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_t
     a.q = q_dev; a.q_token_stride = q_token_stride; a.q_head_stride = q_head_stride;
     a.o = o_dev; a.o_token_stride = o_token_stride; a.o_head_stride = o_head_stride;
     a.score_scale = (float)(score_scale * 1.4426950408889634); // (scores in base 2)
-    a.pieces = p.pieces; a.row_tiles = p.row_tiles; a.partial = p.cut ? static_cast<float *>(workspace_dev) : nullptr;
-    MC_HIP(launch_cache_attention(a, type, cache->bits, static_cast<hipStream_t>(stream)));
+    a.pieces = p.pieces; a.row_tiles = p.row_tiles; a.rows_held = p.rows;
+    a.partial = p.cut ? static_cast<float *>(workspace_dev) : nullptr;
+    a.sums = p.cut ? a.partial + p.lines * p.width : nullptr;
+    MC_HIP(launch_cache_attention(a, type, cache->bits, p.row_tile, static_cast<hipStream_t>(stream)));
     return MC_OK;
 }

@@ -24,7 +24,7 @@ void note_detail(const char *, ...) {}
 hipError_t launch_rope(const RopeArgs &, mc_type, hipStream_t) { return ++launches, hipSuccess; }
 hipError_t launch_cache_write(const CacheArgs &, mc_type, hipStream_t) { return ++launches, hipSuccess; }
 hipError_t launch_cache_read(const CacheArgs &, mc_type, hipStream_t) { return ++launches, hipSuccess; }
-hipError_t launch_cache_attention(const CacheAttnArgs &, mc_type, int, hipStream_t) { return ++launches, hipSuccess; }
+hipError_t launch_cache_attention(const CacheAttnArgs &, mc_type, int, int, hipStream_t) { return ++launches, hipSuccess; }
 """
 NAMES = ("mc_rope", "mc_cache_write", "mc_cache_read", "mc_cache_attention", "mc_cache_attention_workspace")
 
