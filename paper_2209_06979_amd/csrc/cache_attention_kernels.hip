@@ -119,27 +119,38 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
 }
 
 // ---- codes to halves -----------------------------------------------------------------------------------
-// 0x6400 | u is 1024 + u in half precision, and u - 128 (a signed byte with its top bit turned over) is exact
+// Codes enter the matrix unit as half-precision numbers, in which they are exact.  0x6400 | u is 1024 + u, and a signed code with its top bit turned over
+// is u - 128 (u - 8).  In the first product the subtraction is left out where the type allows it (RAW): a half with the bits u is the subnormal number u 2^-24 (16 u 2^-24
+// a nibble higher up), and the offset is the same for all tokens: offset * sum of the row's q, once a row.  That costs the sums one or two bits of fp32.  (In the
+// second product the offset would be of the size of all weights together, which long contexts exceed their mean by far.)
 __device__ __forceinline__ unsigned minus(unsigned v, float bias) { return bits_of(halves_of(v) - (h2){(_Float16)bias, (_Float16)bias}); }
 __device__ __forceinline__ unsigned nibble_high(unsigned v) // 1024 + 16 u -> u - 8
 {
     const h2 k = {(_Float16)0.0625f, (_Float16)0.0625f}, m = {(_Float16)-72.f, (_Float16)-72.f};
     return bits_of(__builtin_elementwise_fma(halves_of(v), k, m));
 }
+constexpr float RAW_SCALE = 0x1p24f;
+template <int BITS> constexpr float raw_offset() { return BITS == 8 ? 128.f : 8.f; }
+// what an element of q at place e of an operand is divided by for RAW codes
+template <int BITS> constexpr float raw_share(int e) { return BITS == 4 && e / 2 % 2 == 1 ? 0.0625f : 1.f; }
 
 // 8 codes of one token as an operand: bytes in their order, nibbles in the order 0 4 1 5 2 6 3 7
-template <int BITS> __device__ __forceinline__ h8 row_operand(unsigned w0, unsigned w1)
+template <int BITS, bool RAW> __device__ __forceinline__ h8 row_operand(unsigned w0, unsigned w1)
 {
     if constexpr (BITS == 8) {
-        constexpr unsigned HI = 0x64646464u, P01 = 0x04010400u, P23 = 0x04030402u;
+        constexpr unsigned HI = RAW ? 0u : 0x64646464u, P01 = RAW ? 0x0c010c00u : 0x04010400u, P23 = RAW ? 0x0c030c02u : 0x04030402u;
         w0 ^= 0x80808080u;
         w1 ^= 0x80808080u;
-        return operand(minus(__builtin_amdgcn_perm(HI, w0, P01), 1152.f), minus(__builtin_amdgcn_perm(HI, w0, P23), 1152.f),
-                       minus(__builtin_amdgcn_perm(HI, w1, P01), 1152.f), minus(__builtin_amdgcn_perm(HI, w1, P23), 1152.f));
+        const unsigned a = __builtin_amdgcn_perm(HI, w0, P01), b = __builtin_amdgcn_perm(HI, w0, P23), c = __builtin_amdgcn_perm(HI, w1, P01),
+                       d = __builtin_amdgcn_perm(HI, w1, P23);
+        if constexpr (RAW) return operand(a, b, c, d);
+        return operand(minus(a, 1152.f), minus(b, 1152.f), minus(c, 1152.f), minus(d, 1152.f));
     } else {
-        const unsigned u = w0 ^ 0x88888888u, d = u >> 8;
-        return operand(minus((u & 0x000F000Fu) | 0x64006400u, 1032.f), nibble_high((u & 0x00F000F0u) | 0x64006400u),
-                       minus((d & 0x000F000Fu) | 0x64006400u, 1032.f), nibble_high((d & 0x00F000F0u) | 0x64006400u));
+        constexpr unsigned LO = RAW ? 0x00080008u : 0x64086408u, HI = RAW ? 0x00800080u : 0x64806480u;
+        const unsigned d = w0 >> 8;
+        const unsigned a = (w0 & 0x000F000Fu) ^ LO, b = (w0 & 0x00F000F0u) ^ HI, c = (d & 0x000F000Fu) ^ LO, e = (d & 0x00F000F0u) ^ HI;
+        if constexpr (RAW) return operand(a, b, c, e);
+        return operand(minus(a, 1032.f), nibble_high(b), minus(c, 1032.f), nibble_high(e));
     }
 }
 constexpr int nibble_order(int e) { return e / 2 + 4 * (e % 2); } // element of place e
@@ -152,9 +163,9 @@ template <int BITS> __device__ __forceinline__ unsigned column_pair(unsigned fir
         return minus(__builtin_amdgcn_perm(second, first, sel) ^ 0x64806480u, 1152.f);
     } else {
         const unsigned sel = 0x0c000c00u | (unsigned)(4 + m / 2) << 16 | (unsigned)(m / 2);
-        const unsigned pair = __builtin_amdgcn_perm(second, first, sel); // (of words whose nibbles' top bits are turned over)
-        if (m % 2 == 0) return minus((pair & 0x000F000Fu) | 0x64006400u, 1032.f);
-        return nibble_high((pair & 0x00F000F0u) | 0x64006400u);
+        const unsigned pair = __builtin_amdgcn_perm(second, first, sel);
+        if (m % 2 == 0) return minus((pair & 0x000F000Fu) ^ 0x64086408u, 1032.f);
+        return nibble_high((pair & 0x00F000F0u) ^ 0x64806480u);
     }
 }
 
@@ -218,6 +229,7 @@ __device__ __forceinline__ int64_t out_at(const CacheAttnArgs &a, const Sequence
 // the products with q, group g = l / 16 of the reduction.
 template <int D, int BITS, int TYPE> struct Shape {
     static constexpr int PLANES = TYPE == MC_F32 ? 2 : 1; // halves that hold a value of q, and a weight
+    static constexpr bool RAW = TYPE != MC_F32;           // K's codes enter with their offset
     static constexpr int C = D / 16;                      // columns of V in a lane
     static constexpr int STEPS = D / 32;                  // of the first product
     static constexpr int KB = D * BITS / 32, PB = KB < 16 ? KB : 16, NK = KB / PB, PER = PB / BITS; // bytes of a row of K in a lane, in pieces of PER steps
@@ -229,8 +241,9 @@ template <int D, int BITS, int TYPE> struct Shape {
     }
 };
 
-// A lane's row of q as operands of the first product, times a power of two that brings the row's largest into [1, 2); what scores are multiplied by then
-template <class S, int BITS, int TYPE> __device__ __forceinline__ float load_q(const CacheAttnArgs &a, int64_t at, int g, h8 (&q)[S::PLANES][S::STEPS])
+// A lane's row of q as operands of the first product, times a power of two that brings the row's largest into [1, 2); a score is sum * scale + offset then
+struct RowScale { float scale, offset; };
+template <class S, int BITS, int TYPE> __device__ __forceinline__ RowScale load_q(const CacheAttnArgs &a, int64_t at, int g, h8 (&q)[S::PLANES][S::STEPS])
 {
     float v[S::STEPS][8], top = 0;
 #pragma unroll
@@ -245,15 +258,19 @@ template <class S, int BITS, int TYPE> __device__ __forceinline__ float load_q(c
     }
     top = max_of_groups(top);
     const int up = top > 0 && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
+    float sum = 0;
 #pragma unroll
     for (int st = 0; st < S::STEPS; ++st)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_ldexpf(v[st][BITS == 8 ? e : nibble_order(e)], -up);
+            const float x = __builtin_amdgcn_ldexpf(v[st][BITS == 8 ? e : nibble_order(e)], -up) * (S::RAW ? raw_share<BITS>(e) : 1.f);
             q[0][st][e] = (_Float16)x;
             if (S::PLANES == 2) q[S::PLANES - 1][st][e] = (_Float16)(x - (float)(_Float16)x);
+            if (S::RAW) sum += (float)q[0][st][e] / raw_share<BITS>(e); // (what the products are made with)
         }
-    return __builtin_amdgcn_ldexpf(a.score_scale, up);
+    const float scale = __builtin_amdgcn_ldexpf(a.score_scale, up);
+    if (!S::RAW) return {scale, 0.f};
+    return {scale * RAW_SCALE, -scale * raw_offset<BITS>() * sum_of_groups(sum)};
 }
 
 // What a row may see: all tokens below `all`, and those of the bits from `held` on
@@ -300,6 +317,13 @@ __device__ __forceinline__ Split split_scale(float vs)
     x = x < -100 ? -100 : x;
     const float back = __builtin_amdgcn_ldexpf(1.f, -x);
     return {(float)x, back, vs * back};
+}
+// A scale that is not finite makes the exponent NaN, and with it the rows that see the token; the rest is finite, so that a weight of zero makes nothing of
+// it.
+__device__ __forceinline__ void keep_apart(Split &v, float vs)
+{
+    v.exponent = __builtin_fmaf(vs, 0.f, v.exponent);
+    v.rest = __builtin_amdgcn_fmed3f(v.rest, -1.f, 1.f);
 }
 
 // Which piece, head and rows a workgroup has.  Tiles of rows of the same piece and head follow each other on one XCD (workgroups go round the eight of
@@ -353,7 +377,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
     const int row = row0 + i < rows ? row0 + i : rows - 1; // (rows beyond the last repeat it)
     const Sight sight = sight_of(a, s, row / a.group);
     h8 q[PLANES][S::STEPS];
-    const float row_scale = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)(row / a.group)) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q);
+    const RowScale row_scale = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)(row / a.group)) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q);
     const int last_row = row0 + 15 < rows ? row0 + 15 : rows - 1;
     const int end = a.tree ? s.length : held + last_row / a.group + 1; // no row sees more
     const int certain = a.tree ? held : held + row0 / a.group + 1;     // every row sees this many
@@ -405,29 +429,57 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
             for (int st = 0; st < S::STEPS; ++st) {
                 const auto &piece = tile.k[half][st / S::PER];
                 const int at = st % S::PER;
-                const h8 k = BITS == 8 ? row_operand<BITS>(piece.w[2 * at % (PB / 4)], piece.w[(2 * at + 1) % (PB / 4)]) : row_operand<BITS>(piece.w[at], 0u);
+                const h8 k = BITS == 8 ? row_operand<BITS, S::RAW>(piece.w[2 * at % (PB / 4)], piece.w[(2 * at + 1) % (PB / 4)]) : row_operand<BITS, S::RAW>(piece.w[at], 0u);
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
                     sc[half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][st], st == 0 && p == 0 ? (v4f){0, 0, 0, 0} : sc[half], 0, 0, 0);
             }
         const int at = number * CACHE_TILE;
         const bool masked = at + CACHE_TILE > certain || !tile.there[0] || !tile.there[1];
-        Split split[8];
-        float x[8]; // scores in base 2, plus the exponents of V's scales
+        float vs[8];
         unsigned seen = 0xff;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            split[e] = split_scale(tile.vs[e / 4][e % 4]);
-            x[e] = __builtin_fmaf(sc[e / 4][e % 4] * row_scale, tile.ks[e / 4][e % 4], split[e].exponent);
-        }
+        for (int e = 0; e < 8; ++e) vs[e] = tile.vs[e / 4][e % 4];
         if (masked) {
             seen = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const unsigned yes = sees(sight, at + 16 * (e / 4) + 4 * g + e % 4, held, tile.there[e / 4]);
                 seen |= yes << e;
-                x[e] = yes ? x[e] : NONE;
+                vs[e] = yes ? vs[e] : 0.f; // (whatever there is)
             }
+        }
+        // Scores in base 2, plus exponents of V's scales: of each token's own, or (one half to a weight) that of the largest of a lane's eight, whose others
+        // keep their 11 bits while they are within 2^25 of it.
+        float x[8], exponent[8], back[8], rest[8];
+        if (PLANES == 2) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const Split v = split_scale(vs[e]);
+                exponent[e] = v.exponent;
+                back[e] = v.back;
+                rest[e] = v.rest;
+            }
+        } else {
+            float most = fabsf(vs[0]);
+#pragma unroll
+            for (int e = 1; e < 8; ++e) most = fmaxf(most, fabsf(vs[e]));
+            const Split v = split_scale(most);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                exponent[e] = v.exponent;
+                back[e] = v.back;
+                rest[e] = vs[e] * v.back;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float score = S::RAW ? __builtin_fmaf(sc[e / 4][e % 4], row_scale.scale, row_scale.offset) : sc[e / 4][e % 4] * row_scale.scale;
+            x[e] = __builtin_fmaf(score, tile.ks[e / 4][e % 4], exponent[e]);
+        }
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? x[e] : NONE;
         }
         float top = x[0];
 #pragma unroll
@@ -445,20 +497,11 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = __builtin_amdgcn_exp2f(x[e] - from);
-            l = __builtin_fmaf(p, split[e].back, l);
-            float v = p * split[e].rest;
-            if (masked) v = seen >> e & 1 ? v : 0.f; // (whatever the scale there is)
+            l = __builtin_fmaf(p, back[e], l);
+            float v = p * rest[e];
             if (PLANES == 2) asm("" : "+v"(v)); // (one product, rounded once: the first half by a fused rounding, and the second from another would differ at a tie)
             w[0][e] = (_Float16)v;
             if (PLANES == 2) w[PLANES - 1][e] = (_Float16)(v - (float)(_Float16)v);
-        }
-        if (BITS == 4) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int e = 0; e < (S::VB + 3) / 4; ++e) tile.v[half][r].w[e] ^= 0x88888888u;
         }
         constexpr int PER_WORD = 32 / BITS; // columns of a word
 #pragma unroll
@@ -554,7 +597,8 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     const int certain = a.tree ? held : held + row0 / a.group + 1;
 
     Sight sight[R];
-    float row_scale[R], m[R], l[R];
+    RowScale row_scale[R];
+    float m[R], l[R];
     h8 q[R][PLANES][STEPS];
     v4f o[R][C];
 #pragma unroll
@@ -622,13 +666,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 #pragma unroll
             for (int e = 0; e < S::PER; ++e)
                 *reinterpret_cast<h8 *>(&to.k[(b * STEPS + p * S::PER + e) * 1024 + lane * 16]) =
-                    BITS == 8 ? row_operand<BITS>(t.k[u].w[2 * e % (PB / 4)], t.k[u].w[(2 * e + 1) % (PB / 4)]) : row_operand<BITS>(t.k[u].w[e], 0u);
-        }
-        if (BITS == 4) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int e = 0; e < (VB + 3) / 4; ++e) t.v[r].w[e] ^= 0x88888888u;
+                    BITS == 8 ? row_operand<BITS, S::RAW>(t.k[u].w[2 * e % (PB / 4)], t.k[u].w[(2 * e + 1) % (PB / 4)]) : row_operand<BITS, S::RAW>(t.k[u].w[e], 0u);
         }
         constexpr int PER_WORD = 32 / BITS;
 #pragma unroll
@@ -640,7 +678,8 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
         if (lane < T) {
             if (wave == 0) to.scale[lane] = t.scale;
             if (wave == 1) {
-                const Split v = split_scale(t.scale);
+                Split v = split_scale(t.scale);
+                keep_apart(v, t.scale);
                 to.exponent[lane] = v.exponent;
                 to.back[lane] = v.back;
                 to.rest[lane] = v.rest;
@@ -654,9 +693,9 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
         for (int b = 0; b < BLOCKS; ++b) masked = masked || !is_page(a, pages[b]);
         v4f sc[R][BLOCKS];
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
+        for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
+            for (int b = 0; b < BLOCKS; ++b) { // (sums that follow each other are of other blocks)
                 const h8 op = *reinterpret_cast<const h8 *>(&st.k[(b * STEPS + k) * 1024 + lane * 16]);
 #pragma unroll
                 for (int t = 0; t < R; ++t)
@@ -665,44 +704,33 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
                         sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[t][p][k], k == 0 && p == 0 ? (v4f){0, 0, 0, 0} : sc[t][b], 0, 0, 0);
             }
         // scores in base 2, plus the exponents of V's scales
-        unsigned seen[R];
-        float top[R];
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
-            seen[t] = ~0u;
-            top[t] = NONE;
-        }
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
             const v4f ks = *reinterpret_cast<const v4f *>(&st.scale[16 * b + 4 * g]), ex = *reinterpret_cast<const v4f *>(&st.exponent[16 * b + 4 * g]);
 #pragma unroll
             for (int t = 0; t < R; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sc[t][b][r] = __builtin_fmaf(sc[t][b][r] * row_scale[t], ks[r], ex[r]);
+                for (int r = 0; r < 4; ++r) {
+                    const float score = S::RAW ? __builtin_fmaf(sc[t][b][r], row_scale[t].scale, row_scale[t].offset) : sc[t][b][r] * row_scale[t].scale;
+                    sc[t][b][r] = __builtin_fmaf(score, ks[r], ex[r]);
+                }
         }
         if (masked) {
 #pragma unroll
-            for (int t = 0; t < R; ++t) {
-                seen[t] = 0;
+            for (int t = 0; t < R; ++t)
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const unsigned yes = sees(sight[t], at + 16 * b + 4 * g + r, held, is_page(a, pages[b]));
-                        seen[t] |= yes << (4 * b + r);
-                        sc[t][b][r] = yes ? sc[t][b][r] : NONE;
-                    }
-            }
+                    for (int r = 0; r < 4; ++r) sc[t][b][r] = sees(sight[t], at + 16 * b + 4 * g + r, held, is_page(a, pages[b])) ? sc[t][b][r] : NONE;
         }
 #pragma unroll
         for (int t = 0; t < R; ++t) {
+            float top = sc[t][0][0];
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top[t] = fmaxf(top[t], sc[t][b][r]);
-            top[t] = max_of_groups(top[t]);
-            if (__any(top[t] > m[t])) {
-                const float to = fmaxf(top[t], m[t]), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m[t] - to);
+            for (int e = 1; e < 4 * BLOCKS; ++e) top = fmaxf(top, sc[t][e / 4][e % 4]);
+            top = max_of_groups(top);
+            if (__any(top > m[t])) {
+                const float to = fmaxf(top, m[t]), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m[t] - to);
                 m[t] = to;
                 l[t] *= by;
 #pragma unroll
@@ -724,7 +752,6 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
                         const float p = __builtin_amdgcn_exp2f(sc[t][b][r] - from);
                         l[t] = __builtin_fmaf(p, back[r], l[t]);
                         float v = p * rest[r];
-                        if (masked) v = seen[t] >> (4 * b + r) & 1 ? v : 0.f;
                         if (PLANES == 2) asm("" : "+v"(v)); // (as above)
                         w[t][0][4 * half + r] = (_Float16)v;
                         if (PLANES == 2) w[t][PLANES - 1][4 * half + r] = (_Float16)(v - (float)(_Float16)v);

@@ -53,7 +53,7 @@ class Problem:
 
     def check(self, got, scale=None):
         want, tol = ref.attention(self.q.double().cpu().numpy(), self.kc, self.vc, self.ks, self.vs, self.table, self.lengths, self.starts, self.tree, scale,
-                                  HALF[self.dtype], WEIGHT[self.dtype])
+                                  HALF[self.dtype], WEIGHT[self.dtype], own_exponents=self.dtype == "float32")
         tol = tol + (2.0 ** -25 if self.dtype == "float16" else 0)   # (half a step of fp16's subnormal numbers)
         err = np.abs(got.double().cpu().numpy() - want)
         assert (err <= tol).all(), float(np.nanmax(err / tol))
@@ -124,9 +124,12 @@ def test_rows_that_see_nothing_are_zero():
     assert bool((out[:5] == 0).all()) and bool((out[11:] == 0).all())
 
 
-def test_bits_and_tokens_beyond_a_sequence_are_not_looked_at():
-    """Bits of the tree from n on, pages behind the last token, and the rest of its last page: scales of NaN and infinity there do not show."""
-    p = Problem([20, 77], [5, 9], page=64, seed=13, spare=3)
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("group", [1, 2, 8])
+def test_bits_and_tokens_beyond_a_sequence_are_not_looked_at(dtype, group):
+    """Bits of the tree from n on, pages behind the last token, and the rest of its last page: scales of NaN, of infinity and of 1e30 there do not
+    show; nor does a scale of 1e30 at a new token in the rows that do not see it."""
+    p = Problem([20, 77], [5, 9], group=group, page=64, seed=13, spare=3, dtype=dtype)
     p.tree = [(1 << i + 1) - 1 | ~((1 << 20) - 1) & (1 << 64) - 1 for n in (5, 9) for i in range(n)]
     used = set()
     for b, length in enumerate(p.lengths):
@@ -135,9 +138,17 @@ def test_bits_and_tokens_beyond_a_sequence_are_not_looked_at():
     for page in range(p.ks.shape[0]):
         for o in range(64):
             if (page, o) not in used:
-                p.ks[page, :, o], p.vs[page, :, o] = np.nan, (np.inf if o % 2 else np.nan)
+                p.ks[page, :, o], p.vs[page, :, o] = (np.nan, 1e30, -np.inf)[o % 3], (np.inf, np.nan, 1e30, -1e30)[o % 4]
     p.table[:, -1] = -1
     p.check(p.run())
+    p.tree = [1 << i for n in (5, 9) for i in range(n)]          # every new token sees itself alone
+    p.vs[p.table[0, 0], :, 22] = 1e30 if dtype != "float16" else 100
+    p.ks[p.table[1, 1], :, 80 % 64] = 1e30
+    out = p.run()
+    p.starts, p.lengths = p.starts[:2], p.lengths[:1]             # (row 80 - 77 of the second sequence is not finite)
+    p.q, p.tree = p.q[:5], p.tree[:5]
+    p.check(out[:5])
+    assert bool(out[[5, 6, 7, 9, 10]].isfinite().all())
 
 
 def test_what_is_not_finite_stays_with_the_rows_that_see_it():
