@@ -6,21 +6,25 @@
 #include "decode.h"
 #include "rope.h"
 
+#include <type_traits>
+
 namespace {
 
-constexpr int E = 8; // elements of a lane
+constexpr int E = 8;     // elements of a lane
+constexpr int AHEAD = 3; // vectors asked for before they are worked on
 
-template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[E])
-{
+// 8 elements as they lie in memory, and as fp32
+template <class T> struct Raw8 {
     typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
-    constexpr int N = 16 / sizeof(T);
+    static constexpr int N = 16 / sizeof(T);
+    Vec w[E / N];
+    __device__ __forceinline__ void load(const T *p)
+    {
 #pragma unroll
-    for (int q = 0; q < E / N; ++q) {
-        const Vec w = reinterpret_cast<const Vec *>(p)[q];
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[q * N + e] = (float)w[e];
+        for (int q = 0; q < E / N; ++q) w[q] = reinterpret_cast<const Vec *>(p)[q];
     }
-}
+    __device__ __forceinline__ float operator[](int e) const { return (float)w[e / N][e % N]; }
+};
 
 template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[E])
 {
@@ -35,116 +39,207 @@ template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)
     }
 }
 
-// A vector's place in a cache, in vectors; -1 for slots that are none
-__device__ __forceinline__ int64_t place_of(const CacheArgs &a, int64_t slot, int head)
+// The place of a token's head 0 in a cache, in vectors (the next heads follow a page's size apart); -1 for slots that are none
+__device__ __forceinline__ int64_t place_of(const CacheArgs &a, int64_t slot)
 {
     if (slot < 0 || slot >= a.slots_end) return -1;
-    const int64_t page = slot >> a.page_shift, in_page = slot & (((int64_t)1 << a.page_shift) - 1);
-    return ((page * a.kv_heads + head) << a.page_shift) + in_page;
+    return ((slot >> a.page_shift) * a.kv_heads << a.page_shift) + (slot & (((int64_t)1 << a.page_shift) - 1));
 }
 
-// Codes of 8 values (REAL: float as read, or double after a rotation) and their scale; LANES lanes share the vector.
-template <class REAL, int BITS, int LANES> __device__ __forceinline__ float codes_of(const REAL (&v)[E], bool there, unsigned (&w)[2])
+// The largest over the LANES (8, 16 or 32) lanes that share a vector: rotations within rows of 16 lanes, the halves of 8 mirrored, and a swap of rows
+template <int CTRL> __device__ __forceinline__ float moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL> __device__ __forceinline__ double moved(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = (unsigned)__builtin_amdgcn_mov_dpp((int)(unsigned)b, CTRL, 0xF, 0xF, true), hi = (unsigned)__builtin_amdgcn_mov_dpp((int)(unsigned)(b >> 32), CTRL, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, hi << 32 | lo);
+}
+template <int LANES, class REAL> __device__ __forceinline__ REAL max_of_lanes(REAL m)
+{
+    auto take = [&](REAL b) { m = b > m ? b : m; };
+    take(moved<0xB1>(m));  // quad_perm 1 0 3 2
+    take(moved<0x4E>(m));  // quad_perm 2 3 0 1
+    take(moved<0x141>(m)); // row_half_mirror
+    if (LANES >= 16) take(moved<0x140>(m)); // row_mirror
+    if (LANES == 32) take(__shfl_xor(m, 16, 64));
+    return m;
+}
+
+// m / qmax rounded to fp32 once.  (fp32 division is correctly rounded; in double the product with the inverse is within 2^-51, and only where that leaves the
+// rounding open the division is made.)
+__device__ __forceinline__ float scale_of(float m, float qmax) { return m / qmax; }
+__device__ __forceinline__ float scale_of(double m, float qmax)
+{
+    const double q = m * (1.0 / qmax);
+    const float lo = (float)(q * (1 - 0x1p-50)), hi = (float)(q * (1 + 0x1p-50));
+    return lo == hi ? lo : (float)(m / (double)qmax);
+}
+
+// Codes of 8 values (REAL: float as read, or double after a rotation) and their scale; LANES lanes share the vector.  finite: all eight are.
+// An fp32 quotient decides unless it lies within 1e-4 of a border of rounding (the value rounded to fp32, the inverse scale and their product are each within
+// 2^-23: 5e-5 of 127 in all), and only then the division in double precision, for all eight.
+template <class REAL, int BITS, int LANES> __device__ __forceinline__ float codes_of(const REAL (&v)[E], bool there, bool finite, unsigned (&w)[2])
 {
     constexpr int QMAX = BITS == 8 ? 127 : 7;
-    REAL m = 0;
+    constexpr float MAGIC = 0x1.8p23f; // added, it rounds to whole numbers, ties to even, which then are the low bits
+    REAL m = __builtin_elementwise_abs(v[0]);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const REAL b = __builtin_fabs(v[e]);
-        m = b > m || !(b < (REAL)__builtin_inf()) ? ((b < (REAL)__builtin_inf()) ? b : (REAL)__builtin_inf()) : m; // (a NaN counts as infinity)
-    }
+    for (int e = 1; e < E; ++e) m = __builtin_elementwise_max(m, __builtin_elementwise_abs(v[e]));
+    if (!finite) m = (REAL)__builtin_inf();
     if (!there) m = 0;
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
-        const REAL b = __shfl_xor(m, o, 64);
-        m = b > m ? b : m;
-    }
-    const bool finite = m < (REAL)__builtin_inf();
-    const float scale = finite ? (float)((double)m / QMAX) : __builtin_nanf("");
+    m = max_of_lanes<LANES>(m);
+    const bool all_finite = m < (REAL)__builtin_inf();
+    const float scale = all_finite ? scale_of(m, (float)QMAX) : __builtin_nanf("");
     w[0] = w[1] = 0;
-    if (finite && scale > 0) {
-        const double inv = 1.0 / (double)scale;
+    auto put = [&](int e, unsigned code) {
+        if (BITS == 8) w[e / 4] |= (code & 255u) << (8 * (e % 4));
+        else w[0] |= (code & 15u) << (4 * e);
+    };
+    if (scale >= 0x1p-100f) {
+        const float inv = __builtin_amdgcn_rcpf(scale);
+        float off = 0;
+        unsigned code[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const double q = (double)v[e] * inv;
-            double c = __builtin_rint(q);
-            if (__builtin_fabs(__builtin_fabs(q - c) - 0.5) < 1e-9) c = __builtin_rint((double)v[e] / (double)scale);
-            const int code = (int)__builtin_fmin(__builtin_fmax(c, (double)-QMAX), (double)QMAX);
-            if (BITS == 8) w[e / 4] |= (unsigned)(code & 255) << (8 * (e % 4));
-            else w[0] |= (unsigned)(code & 15) << (4 * e);
+            const float r = (float)v[e] * inv, up = r + MAGIC;
+            code[e] = __builtin_bit_cast(unsigned, up);
+            off = __builtin_fmaxf(off, __builtin_fabsf(r - (up - MAGIC)));
         }
+        if (off > 0.4999f) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) code[e] = (unsigned)(int)__builtin_rint((double)v[e] / (double)scale);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) put(e, code[e]); // (|v| / scale is at most qmax (1 + 2^-24))
+    } else if (scale > 0) { // (too small for its inverse; and a subnormal scale can be off by more)
+#pragma unroll
+        for (int e = 0; e < E; ++e) put(e, (unsigned)(int)__builtin_fmin(__builtin_fmax(__builtin_rint((double)v[e] / (double)scale), (double)-QMAX), (double)QMAX));
     }
     return scale;
 }
 
-// Lanes in groups of LANES (a power of two, at least dk / 8) take a token's K and V vectors one after the other.
-template <int TYPE, int BITS, int LANES, bool ROPE> __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a)
+// How a key's elements find their partners: no rotation, the other element of the pair among the same lane's eight, eight elements side by side (rot / 2 a multiple of
+// 8), or anywhere.
+enum { PLAIN, PAIRS, HALVES, ANY_HALVES };
+
+// Lanes in groups of LANES (a power of two, at least dk / 8) take a token's K and V vectors one after the other; a key's sines are worked out once.
+template <int TYPE, int BITS, int LANES, int ROPE> __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a)
 {
     typedef typename RealOf<TYPE>::type T;
-    const int64_t line = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, token = line / a.groups;
+    const unsigned line = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, token = line / a.groups; // (threads are counted in 31 bits)
     const int first = (int)(line - token * a.groups), lane = threadIdx.x % LANES;
     if (token >= a.tokens) return;
-    const int64_t slot = a.slots[token];
+    const int64_t place0 = place_of(a, a.slots[token]);
+    if (place0 < 0) return;
     const bool there = lane * E < a.dk;
     const int at = there ? lane * E : 0, half = a.rot / 2;
-    double c[E], s[E]; // of each element's pair
-    int other[E];      // the pair's other element
-    if constexpr (ROPE) {
+    double c[E], s[E];       // of each element's pair
+    bool turns = true;       // they are finite
+    int other = at;          // where the other elements of the pairs are (HALVES)
+    if (ROPE != PLAIN && first < a.kv_heads) {
         const double position = (double)a.positions[token];
+        if (ROPE == HALVES && at < a.rot) other = at < half ? at + half : at - half;
+        double f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) { // (all requests before the first use; elements beyond rot have the first frequency and no use for it)
+            const int i = at + e;
+            f[e] = a.inv_freq[i >= a.rot ? 0 : ROPE == PAIRS ? i / 2 : i >= half ? i - half : i];
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int i = at + e;
-            c[e] = 1;
-            s[e] = 0;
-            other[e] = i;
-            if (i < a.rot) {
-                const bool second = a.interleaved ? i & 1 : i >= half;
-                const SinCos<double> t = sin_cos_of<double>(position, a.inv_freq[a.interleaved ? i / 2 : second ? i - half : i]);
-                c[e] = t.c * a.magnitude;
-                s[e] = (second ? t.s : -t.s) * a.magnitude;
-                other[e] = a.interleaved ? i ^ 1 : second ? i - half : i + half;
+            if (ROPE == PAIRS && e % 2 == 1) {
+                c[e] = c[e - 1];
+                s[e] = -s[e - 1];
+                continue;
             }
+            const SinCos<double> t = sin_cos_of<double>(position, f[e]);
+            c[e] = i < a.rot ? t.c * a.magnitude : 1.0;
+            s[e] = i < a.rot ? (ROPE != PAIRS && i >= half ? t.s : -t.s) * a.magnitude : 0.0;
+            turns = turns && __builtin_fabs(c[e]) < __builtin_inf() && __builtin_fabs(s[e]) < __builtin_inf();
         }
     }
-    for (int j = first; j < 2 * a.kv_heads; j += a.groups) {
-        const int which = j >= a.kv_heads, head = which ? j - a.kv_heads : j;
-        const int64_t place = place_of(a, slot, head);
-        if (place < 0) continue;
+    struct Vector { Raw8<T> own, other; };
+    // `turned`: keys on their rotation.  Heads from `head` on, `groups` apart; AHEAD of them are on their way while one is worked on.
+    auto vectors = [&](auto turned, int which, int head) {
+        constexpr bool TURNED = decltype(turned)::value;
         const T *x = static_cast<const T *>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which];
-        float v[E];
-        unsigned w[2];
-        float scale;
-        load8(x + at, v);
-        if (ROPE && !which) {
-            double y[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = (double)v[e] * c[e] + (double)(float)x[other[e]] * s[e];
-            scale = codes_of<double, BITS, LANES>(y, there, w);
-        } else {
-            scale = codes_of<float, BITS, LANES>(v, there, w);
-        }
-        if (!there) continue;
+        const int64_t step = a.groups * a.head_stride[which], place_step = (int64_t)a.groups << a.page_shift, place = place0 + ((int64_t)head << a.page_shift);
         uint8_t *to = a.codes[which] + (place * a.dk + at) * BITS / 8;
-        if (BITS == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-        else *reinterpret_cast<unsigned *>(to) = w[0];
-        if (lane == 0) a.scales[which][place] = scale;
+        float *scale_to = a.scales[which] + place;
+        auto fetch = [&](Vector &v) {
+            v.own.load(x + at);
+            if (TURNED && ROPE == HALVES) v.other.load(x + other);
+            if (TURNED && ROPE == ANY_HALVES) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v.other.w[e / Raw8<T>::N][e % Raw8<T>::N] = x[at + e >= a.rot ? at + e : at + e < half ? at + e + half : at + e - half];
+            }
+            x += step;
+        };
+        Vector v[AHEAD + 1];
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d)
+            if (head + d * a.groups < a.kv_heads) fetch(v[d]);
+        for (int h = head; h < a.kv_heads; h += a.groups) {
+            if (h + AHEAD * a.groups < a.kv_heads) fetch(v[AHEAD]);
+            float own[E];
+            unsigned w[2], bits = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                own[e] = v[0].own[e];
+                const unsigned b = __builtin_bit_cast(unsigned, own[e]) & 0x7fffffffu;
+                bits = b > bits ? b : bits;
+            }
+            const bool finite = bits < 0x7f800000u; // (an element that is not has its rotated pair among the vector's)
+            float scale;
+            if constexpr (TURNED) {
+                double y[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = (double)own[e] * c[e] + (double)(ROPE == PAIRS ? own[e ^ 1] : v[0].other[e]) * s[e];
+                if (at + E > a.rot) { // (an infinity beyond rot has no part in its neighbour)
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (at + e >= a.rot) y[e] = (double)own[e];
+                }
+                scale = codes_of<double, BITS, LANES>(y, there, finite && turns, w);
+            } else {
+                scale = codes_of<float, BITS, LANES>(own, there, finite, w);
+            }
+            if (there) {
+                if (BITS == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<unsigned *>(to) = w[0];
+                if (lane == 0) *scale_to = scale;
+            }
+            to += place_step * a.dk * BITS / 8;
+            scale_to += place_step;
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) v[d] = v[d + 1];
+        }
+    };
+    int j = first;
+    if (first < a.kv_heads) {
+        vectors(std::integral_constant<bool, ROPE != PLAIN>{}, 0, first);
+        j += (a.kv_heads - first + a.groups - 1) / a.groups * a.groups;
     }
+    if (j < 2 * a.kv_heads) vectors(std::false_type{}, 1, j - a.kv_heads);
 }
 
 // A lane takes 8 elements of its token's K and V vectors, one vector after the other.
 template <int TYPE, int BITS> __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a)
 {
     typedef typename RealOf<TYPE>::type T;
-    const int pieces = a.dk / E;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, line = id / pieces, token = line / a.groups;
+    const unsigned pieces = a.dk / E, id = blockIdx.x * 256 + threadIdx.x, line = id / pieces, token = line / a.groups; // (threads are counted in 31 bits)
     const int at = (int)(id - line * pieces) * E, first = (int)(line - token * a.groups);
     if (token >= a.tokens) return;
-    const int64_t slot = a.slots[token];
+    const int64_t place0 = place_of(a, a.slots[token]);
     for (int j = first; j < 2 * a.kv_heads; j += a.groups) {
         const int which = j >= a.kv_heads, head = which ? j - a.kv_heads : j;
-        const int64_t place = place_of(a, slot, head);
+        const int64_t place = place0 + ((int64_t)head << a.page_shift);
         float v[E] = {};
-        if (place >= 0) {
+        if (place0 >= 0) {
             const float scale = a.scales[which][place];
             const uint8_t *from = a.codes[which] + (place * a.dk + at) * BITS / 8;
             unsigned w[2] = {};
@@ -165,12 +260,22 @@ template <int TYPE, int BITS> __global__ __launch_bounds__(256) void cache_read_
     }
 }
 
+// Lanes' groups that share a token's vectors: as many as fill the device (a group that takes several keys has their sines once)
+constexpr int64_t THREADS = 256 * 1024;
+int groups_of(const CacheArgs &a, int lanes)
+{
+    const int64_t per_token = a.tokens * lanes, groups = (THREADS + per_token - 1) / per_token;
+    return groups < 2 * a.kv_heads ? (int)groups : 2 * a.kv_heads;
+}
+
 template <int TYPE, int BITS, int LANES> hipError_t write(CacheArgs a, hipStream_t s)
 {
-    a.groups = 2 * a.kv_heads;
+    a.groups = groups_of(a, LANES);
     const dim3 grid((unsigned)((a.tokens * a.groups + 256 / LANES - 1) / (256 / LANES))), block(256);
-    if (a.rot) return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, true>), grid, block, 0, s, a);
-    return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, false>), grid, block, 0, s, a);
+    if (a.rot == 0) return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, PLAIN>), grid, block, 0, s, a);
+    if (a.interleaved) return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, PAIRS>), grid, block, 0, s, a);
+    if (a.rot / 2 % E == 0) return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, HALVES>), grid, block, 0, s, a);
+    return launch_kernel((cache_write_kernel<TYPE, BITS, LANES, ANY_HALVES>), grid, block, 0, s, a);
 }
 
 template <int TYPE, int BITS> hipError_t write_bits(const CacheArgs &a, hipStream_t s)

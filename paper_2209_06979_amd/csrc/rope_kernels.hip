@@ -13,25 +13,37 @@ template <int TYPE, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(256)
 {
     typedef typename RealOf<TYPE>::type T;
     typedef T Vec __attribute__((ext_vector_type(VEC > 1 ? VEC : 2)));
-    const int half = a.rot / 2, turned = half / VEC, rest = a.dim - a.rot, pieces = turned + (rest + 2 * VEC - 1) / (2 * VEC);
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t line = id / pieces, token = line / a.groups;
+    const int half = a.rot / 2, turned = half / VEC, rest = a.dim - a.rot;
+    const unsigned id = blockIdx.x * 256 + threadIdx.x, pieces = turned + (rest + 2 * VEC - 1) / (2 * VEC); // (threads are counted in 31 bits)
+    const unsigned line = id / pieces, token = line / a.groups;
     const int piece = (int)(id - line * pieces), first = (int)(line - token * a.groups);
     if (token >= a.tokens) return;
     const T *x = static_cast<const T *>(a.x) + token * a.x_token_stride;
     T *y = static_cast<T *>(a.y) + token * a.y_token_stride;
     if (piece >= turned) { // copied
         const int at = a.rot + (piece - turned) * 2 * VEC, n = a.dim - at < 2 * VEC ? a.dim - at : 2 * VEC;
-        for (int h = first; h < a.heads; h += a.groups)
-            for (int e = 0; e < n; ++e) y[h * a.y_head_stride + at + e] = x[h * a.x_head_stride + at + e];
+        for (int64_t h = first; h < a.heads; h += a.groups) {
+            const T *from = x + h * a.x_head_stride + at;
+            T *to = y + h * a.y_head_stride + at;
+            if (VEC > 1 && n == 2 * VEC) {
+                const Vec v1 = reinterpret_cast<const Vec *>(from)[0], v2 = reinterpret_cast<const Vec *>(from)[1];
+                reinterpret_cast<Vec *>(to)[0] = v1;
+                reinterpret_cast<Vec *>(to)[1] = v2;
+            } else {
+                for (int e = 0; e < n; ++e) to[e] = from[e];
+            }
+        }
         return;
     }
     const int j = piece * VEC;
     const double position = (double)a.positions[token];
     float c[VEC], s[VEC];
+    double f[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = a.inv_freq[j + e];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-        const SinCos<float> t = sin_cos_of<float>(position, a.inv_freq[j + e]);
+        const SinCos<float> t = sin_cos_of<float>(position, f[e]);
         c[e] = t.c * (float)a.cos_scale;
         s[e] = t.s * (float)a.sin_scale;
     }
@@ -69,6 +81,9 @@ template <int TYPE, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(256)
     for (int64_t h = first; h < a.heads; h += a.groups) turn(h);
 }
 
+// Threads that share a token's heads: as many as fill the device twice over (a thread that takes several heads has its sines for them once)
+constexpr int64_t THREADS = 2 * 256 * 2048;
+
 template <int TYPE, int VEC> hipError_t launch(const RopeArgs &a, hipStream_t s)
 {
     const int64_t pieces = a.rot / 2 / VEC + (a.dim - a.rot + 2 * VEC - 1) / (2 * VEC), threads = a.tokens * a.groups * pieces;
@@ -82,7 +97,8 @@ template <int TYPE> hipError_t launch_type(RopeArgs a, hipStream_t s)
     constexpr int VEC = 16 / sizeof(typename RealOf<TYPE>::type);
     const int64_t strides = a.x_token_stride | a.x_head_stride | a.y_token_stride | a.y_head_stride | (a.rot / 2);
     const bool wide = strides % VEC == 0 && ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y)) & 15) == 0;
-    a.groups = a.heads;
+    const int64_t per_token = a.tokens * ((a.dim + 1) / 2 / (wide ? VEC : 1) + 1), groups = (THREADS + per_token - 1) / per_token;
+    a.groups = groups < a.heads ? (int)groups : a.heads;
     return wide ? launch<TYPE, VEC>(a, s) : launch<TYPE, 1>(a, s);
 }
 
