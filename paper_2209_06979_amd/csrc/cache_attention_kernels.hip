@@ -337,8 +337,8 @@ __device__ __forceinline__ Unit unit_of(const CacheAttnArgs &a, int row_tile)
         tile = in / 8;
         unit = turn * 8 + in % 8;
     }
-    const int head = unit / a.units_per_head;
-    return {unit - head * a.units_per_head, head, tile * row_tile};
+    const int piece = unit / a.kv_heads; // (numbers without a piece come last, so that no XCD has more of them than another)
+    return {piece, unit - piece * a.kv_heads, tile * row_tile};
 }
 
 // C results of a row from column col on: to the output, or to a piece's place
@@ -366,7 +366,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const Unit unit = unit_of(a, 16);
-    if (unit.head >= a.kv_heads) return;
+    if (unit.piece >= a.units_per_head) return;
     const Cut cut = cut_of<true>(a, unit.piece);
     if (cut.b < 0) return;
     const Sequence s = cut.of;
@@ -582,7 +582,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const Unit unit = unit_of(a, CACHE_WAVES * 16 * R);
-    if (unit.head >= a.kv_heads) return;
+    if (unit.piece >= a.units_per_head) return;
     const Cut cut = cut_of<true>(a, unit.piece);
     if (cut.b < 0) return;
     const Sequence s = cut.of;
