@@ -60,11 +60,18 @@ __device__ __forceinline__ Sequence sequence(const CacheAttnArgs &a, int b)
     return s;
 }
 __device__ __forceinline__ int tiles_of(const Sequence &s) { return s.n == 0 ? 0 : s.length <= 0 ? 1 : (s.length - 1) / CACHE_TILE + 1; }
-// Tiles of a piece, for this many tiles in all
+// Tiles that a piece should have, for this many tiles in all
 __device__ __forceinline__ int piece_tiles(const CacheAttnArgs &a, int total)
 {
     const int t = (total + a.pieces - 1) / a.pieces;
-    return t <= CACHE_MIN_PIECE ? CACHE_MIN_PIECE : (t + CACHE_WAVES - 1) / CACHE_WAVES * CACHE_WAVES;
+    return t < CACHE_MIN_PIECE ? CACHE_MIN_PIECE : t;
+}
+// Pieces of a sequence: one while it has up to a quarter more than that (a remnant costs more than it relieves the others of)
+__device__ __forceinline__ int pieces_of(int tiles, int each)
+{
+    if (tiles == 0) return 0;
+    const int n = (tiles - 1 + each - each / 4) / each;
+    return n < 1 ? 1 : n;
 }
 
 __device__ __forceinline__ int scan(int v) // inclusive, over the wave: within rows of 16 lanes, then their last lanes' sums into the rows behind
@@ -93,20 +100,23 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
         total = at_lane(scan(t), 63);
         for (int b = 64; b < a.batch; b += 64) total += at_lane(scan(tiles_of(b + lane < a.batch ? sequence(a, b + lane) : none)), 63);
     }
-    Cut c = {-1, a.partial ? piece_tiles(a, total) : 0x7fffffff, 0, 0, 0, none};
+    const int each = a.partial ? piece_tiles(a, total) : 0x40000000;
+    Cut c = {-1, 0, 0, 0, 0, none};
     int before = 0, slots = 0;
     for (int b = 0; b < a.batch; b += 64) {
         if (b) {
             s = b + lane < a.batch ? sequence(a, b + lane) : none;
             t = tiles_of(s);
         }
-        const int pieces = t == 0 ? 0 : (t - 1) / c.each + 1, up_to = scan(pieces), cut_up_to = scan(pieces > 1 ? pieces : 0);
+        const int pieces = pieces_of(t, each), up_to = scan(pieces), cut_up_to = scan(pieces > 1 ? pieces : 0);
         const bool here = BY_PIECE ? before + up_to - pieces <= number && number < before + up_to : b + lane == number;
         const unsigned long long who = __ballot(here);
         if (who) {
             const int l = __builtin_ctzll(who);
             c.b = b + l;
             c.pieces = at_lane(pieces, l);
+            // equal pieces, but for whole rounds of the waves
+            c.each = (at_lane(t, l) + c.pieces * CACHE_WAVES - 1) / (c.pieces * CACHE_WAVES) * CACHE_WAVES;
             c.slot = slots + at_lane(cut_up_to, l) - (c.pieces > 1 ? c.pieces : 0);
             c.index = number - before - at_lane(up_to, l) + c.pieces;
             c.of = {at_lane(s.start, l), at_lane(s.n, l), at_lane(s.length, l)};
@@ -808,51 +818,52 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     }
 }
 
-// Pieces of sequences that were cut, joined in their order: a wave per row, D / 4 lanes per piece.
+// Pieces of sequences that were cut, joined in their order: a wave per row (and further rows after it), D / 4 lanes per piece.
 template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheAttnArgs a)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, AHEAD = 8;
     const Cut cut = cut_of<false>(a, blockIdx.x);
     if (cut.pieces <= 1) return;
-    const int lane = threadIdx.x & 63, row = blockIdx.z * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
-    if (row >= cut.of.n * a.group) return;
-    const int64_t line = ((int64_t)cut.slot * a.kv_heads + head) * a.rows_held + row, step = (int64_t)a.kv_heads * a.rows_held;
-    const int col = lane % LANES * 4, first = lane / LANES;
-    float m = NONE;
-    for (int p = lane; p < cut.pieces; p += 64) m = fmaxf(m, a.sums[(line + p * step) * 2]);
+    const int lane = threadIdx.x & 63, head = blockIdx.y, col = lane % LANES * 4, first = lane / LANES;
+    const int64_t step = (int64_t)a.kv_heads * a.rows_held;
+    for (int row = blockIdx.z * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < cut.of.n * a.group; row += gridDim.z * 4) {
+        const int64_t line = ((int64_t)cut.slot * a.kv_heads + head) * a.rows_held + row;
+        float m = NONE;
+        for (int p = lane; p < cut.pieces; p += 64) m = fmaxf(m, a.sums[(line + p * step) * 2]);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    float l = 0;
-    v4f sum = {0, 0, 0, 0};
-    for (int p0 = 0; p0 < cut.pieces; p0 += AHEAD * AT_ONCE) {
-        v4f v[AHEAD];
-        float2 ml[AHEAD];
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        float l = 0;
+        v4f sum = {0, 0, 0, 0};
+        for (int p0 = 0; p0 < cut.pieces; p0 += AHEAD * AT_ONCE) {
+            v4f v[AHEAD];
+            float2 ml[AHEAD];
 #pragma unroll
-        for (int e = 0; e < AHEAD; ++e) {
-            const int p = p0 + e * AT_ONCE + first;
-            const int64_t at = line + (p < cut.pieces ? p : 0) * step;
-            v[e] = *reinterpret_cast<const v4f *>(a.partial + at * D + col);
-            ml[e] = *reinterpret_cast<const float2 *>(a.sums + at * 2);
-            if (p >= cut.pieces) ml[e].x = NONE;
+            for (int e = 0; e < AHEAD; ++e) {
+                const int p = p0 + e * AT_ONCE + first;
+                const int64_t at = line + (p < cut.pieces ? p : 0) * step;
+                v[e] = *reinterpret_cast<const v4f *>(a.partial + at * D + col);
+                ml[e] = *reinterpret_cast<const float2 *>(a.sums + at * 2);
+                if (p >= cut.pieces) ml[e].x = NONE;
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                if (ml[e].x == NONE) continue;
+                const float by = __builtin_amdgcn_exp2f(ml[e].x - m);
+                l += ml[e].y * by;
+                sum += v[e] * by;
+            }
         }
 #pragma unroll
-        for (int e = 0; e < AHEAD; ++e) {
-            if (ml[e].x == NONE) continue;
-            const float by = __builtin_amdgcn_exp2f(ml[e].x - m);
-            l += ml[e].y * by;
-            sum += v[e] * by;
+        for (int o = LANES; o < 64; o <<= 1) {
+            l += __shfl_xor(l, o, 64);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o, 64);
         }
+        if (first != 0 || col >= a.dk) continue;
+        const float inv = l == 0 ? 0.f : 1.f / l;
+        const float out[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+        store_real<TYPE, 4>(a.o, out_at(a, cut.of, head, row) + col, out);
     }
-#pragma unroll
-    for (int o = LANES; o < 64; o <<= 1) {
-        l += __shfl_xor(l, o, 64);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o, 64);
-    }
-    if (first != 0 || col >= a.dk) return;
-    const float inv = l == 0 ? 0.f : 1.f / l;
-    const float out[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
-    store_real<TYPE, 4>(a.o, out_at(a, cut.of, head, row) + col, out);
 }
 
 template <int D, int BITS, int TYPE> hipError_t launch(CacheAttnArgs a, int row_tile, hipStream_t s)
@@ -865,7 +876,9 @@ template <int D, int BITS, int TYPE> hipError_t launch(CacheAttnArgs a, int row_
                          : row_tile == 64 ? launch_kernel((cache_attention_rows_kernel<D, BITS, TYPE, 1>), grid, block, 0, s, a)
                                           : launch_kernel((cache_attention_rows_kernel<D, BITS, TYPE, 2>), grid, block, 0, s, a);
     if (e != hipSuccess || !a.partial) return e;
-    return launch_kernel((cache_attention_join_kernel<D, TYPE>), dim3(a.batch, a.kv_heads, (a.rows_held + 3) / 4), dim3(256), 0, s, a);
+    // enough workgroups for the device, and few enough to be gone at once where nothing was cut
+    const int most = (a.rows_held + 3) / 4, some = 2048 / (a.batch * a.kv_heads) + 1;
+    return launch_kernel((cache_attention_join_kernel<D, TYPE>), dim3(a.batch, a.kv_heads, most < some ? most : some), dim3(256), 0, s, a);
 }
 
 template <int BITS, int TYPE> hipError_t launch_dim(const CacheAttnArgs &a, int row_tile, hipStream_t s)

@@ -72,7 +72,7 @@ hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits
 constexpr int CACHE_TILE = 32;         // tokens that a wave takes at a time
 constexpr int CACHE_WAVES = 4;         // waves of a workgroup, which share a piece
 constexpr int CACHE_MIN_PIECE = 8;     // tiles of the shortest piece
-constexpr int CACHE_PIECES = 1024;     // pieces asked for, over all heads of the cache and row tiles
+constexpr int CACHE_PIECES = 512;     // pieces asked for, over all heads of the cache and row tiles
 
 // What the launch and its workspace are made for: pieces per head asked for, tiles of rows, whether a sequence can be cut at all, and the
 // places for pieces' results: rows of `width` floats, and two floats for each.
