@@ -100,7 +100,14 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
         total = at_lane(scan(t), 63);
         for (int b = 64; b < a.batch; b += 64) total += at_lane(scan(tiles_of(b + lane < a.batch ? sequence(a, b + lane) : none)), 63);
     }
-    const int each = a.partial ? piece_tiles(a, total) : 0x40000000;
+    int each = a.partial ? piece_tiles(a, total) : 0x40000000;
+    if (a.partial && a.batch <= 64 && a.batch < a.pieces) { // (the whole pieces are more than asked for: longer ones, until they run at once)
+        for (int i = 0; i < 6; ++i) {
+            const int n = at_lane(scan(pieces_of(t, each)), 63);
+            if (n <= a.pieces) break;
+            each += (int)((int64_t)each * (n - a.pieces) / (2 * a.pieces)) + 1;
+        }
+    }
     Cut c = {-1, 0, 0, 0, 0, none};
     int before = 0, slots = 0;
     for (int b = 0; b < a.batch; b += 64) {
@@ -581,9 +588,8 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     typedef Shape<D, BITS, TYPE> S;
     constexpr int PLANES = S::PLANES, C = S::C, PB = S::PB, STEPS = S::STEPS;
     constexpr int T = D <= 128 ? 64 : 32, BLOCKS = T / 16, PAIRS = T / 32;  // tokens of a tile, in blocks of 16 and 32
-    constexpr int KU = BLOCKS * S::NK / CACHE_WAVES;                        // pieces of K that a wave converts: 16 tokens each
-    constexpr int VSPLIT = CACHE_WAVES / BLOCKS, VB = S::VB / VSPLIT, VC = C / VSPLIT; // waves that share 16 tokens of V, by columns
-    static_assert(KU * CACHE_WAVES == BLOCKS * S::NK && VC * VSPLIT == C, "even shares");
+    constexpr int SHARE = CACHE_WAVES / BLOCKS, KU = S::NK / SHARE, VB = S::VB / SHARE, VC = C / SHARE; // waves that convert 16 tokens, each some pieces of K and columns of V
+    static_assert(KU * SHARE == S::NK && VC * SHARE == C, "even shares");
     struct Stage {
         uint8_t k[BLOCKS * STEPS * 1024], v[PAIRS * C * 1024];
         float scale[T], exponent[T], back[T], rest[T];
@@ -622,85 +628,66 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
         for (int c = 0; c < C; ++c) o[t][c] = (v4f){0, 0, 0, 0};
     }
 
-    // what this wave converts: pieces KU wave .. of K (piece p of block p / NK), a block of V and some of its columns; waves 0 and 1 the scales
-    const int row_bytes = a.dk * BITS / 8, v_block = wave % BLOCKS, v_column = wave / BLOCKS * VC;
+    // What this wave converts: of a tile's tokens 16 (one page), and their scales, of K in lanes 0 .. 15 and of V in the next 16.  The page is asked for a tile's
+    // turn ahead.
+    const int row_bytes = a.dk * BITS / 8, block = wave / SHARE, share = wave % SHARE;
     unsigned k_at[KU], v_at[4];
 #pragma unroll
-    for (int u = 0; u < KU; ++u) k_at[u] = k_offset<S>((wave * KU + u) % S::NK, i, g, row_bytes);
+    for (int u = 0; u < KU; ++u) k_at[u] = k_offset<S>(share * KU + u, i, g, row_bytes);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v_at[r] = (4 * g + r) * row_bytes + (i * C + v_column < a.dk ? i * S::VB + wave / BLOCKS * VB : 0);
+    for (int r = 0; r < 4; ++r) v_at[r] = (4 * g + r) * row_bytes + (i * C + share * VC < a.dk ? i * S::VB + share * VB : 0);
     const int last_page = s.length > 0 ? (s.length - 1) >> a.page_shift : -1;
     const int32_t *table = a.table + cut.b * a.table_stride;
-
-    typedef int Pages __attribute__((ext_vector_type(BLOCKS)));
-    auto pages_of = [&](int at) {
-        Pages p;
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) p[b] = page_at(a, table, last_page, at + 16 * b);
-        return p;
+    auto ask_page = [&](int at) { // (a load by lanes: as a scalar one it would hold up the waits for LDS, which share its counter)
+        const int nth = (at + 16 * block) >> a.page_shift;
+        return nth <= last_page ? table[nth + (lane & 0)] : -1;
     };
     struct Codes {
         Words<PB / 4> k[KU];
         Words<(VB + 3) / 4> v[4];
         float scale;
+        int page;
     };
-    auto load = [&](Codes &t, int at, const Pages &pages) {
+    const float *scales = g == 0 ? a.k_scales : a.v_scales;
+    auto load = [&](Codes &t, int at, int page) {
+        t.page = __builtin_amdgcn_readfirstlane(page);
+        const int64_t first = place_of(a, t.page, head, at + 16 * block);
+        const uint8_t *k = a.k_codes + first * row_bytes, *v = a.v_codes + first * row_bytes;
 #pragma unroll
-        for (int u = 0; u < KU; ++u) {
-            const int b = (wave * KU + u) / S::NK;
-            int page = pages[0];
-#pragma unroll
-            for (int e = 1; e < BLOCKS; ++e) page = b == e ? pages[e] : page;
-            t.k[u] = load_bytes<PB>(a.k_codes + place_of(a, page, head, at + 16 * b) * row_bytes, k_at[u]);
-        }
-        int page = pages[0];
-#pragma unroll
-        for (int e = 1; e < BLOCKS; ++e) page = v_block == e ? pages[e] : page;
-        const uint8_t *v = a.v_codes + place_of(a, page, head, at + 16 * v_block) * row_bytes;
+        for (int u = 0; u < KU; ++u) t.k[u] = load_bytes<PB>(k, k_at[u]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) t.v[r] = load_bytes<VB>(v, v_at[r]);
-        if (wave < 2 && lane < T) {
-            int64_t place = place_of(a, pages[0], head, at);
-#pragma unroll
-            for (int e = 1; e < BLOCKS; ++e) {
-                const int64_t other = place_of(a, pages[e], head, at + 16 * e);
-                place = g == e ? other : place;
-            }
-            t.scale = (wave ? a.v_scales : a.k_scales)[place + i];
-        }
+        t.scale = scales[first + i];
     };
     auto convert = [&](Codes &t, Stage &to) {
 #pragma unroll
-        for (int u = 0; u < KU; ++u) {
-            const int b = (wave * KU + u) / S::NK, p = (wave * KU + u) % S::NK;
+        for (int u = 0; u < KU; ++u)
 #pragma unroll
             for (int e = 0; e < S::PER; ++e)
-                *reinterpret_cast<h8 *>(&to.k[(b * STEPS + p * S::PER + e) * 1024 + lane * 16]) =
+                *reinterpret_cast<h8 *>(&to.k[(block * STEPS + (share * KU + u) * S::PER + e) * 1024 + lane * 16]) =
                     BITS == 8 ? row_operand<BITS, S::RAW>(t.k[u].w[2 * e % (PB / 4)], t.k[u].w[(2 * e + 1) % (PB / 4)]) : row_operand<BITS, S::RAW>(t.k[u].w[e], 0u);
-        }
         constexpr int PER_WORD = 32 / BITS;
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
             const int n = c / PER_WORD, in = c % PER_WORD;
-            *reinterpret_cast<uint2 *>(&to.v[(v_block / 2 * C + v_column + c) * 1024 + lane * 16 + v_block % 2 * 8]) =
+            *reinterpret_cast<uint2 *>(&to.v[(block / 2 * C + share * VC + c) * 1024 + lane * 16 + block % 2 * 8]) =
                 make_uint2(column_pair<BITS>(t.v[0].w[n], t.v[1].w[n], in), column_pair<BITS>(t.v[2].w[n], t.v[3].w[n], in));
         }
-        if (lane < T) {
-            if (wave == 0) to.scale[lane] = t.scale;
-            if (wave == 1) {
-                Split v = split_scale(t.scale);
-                keep_apart(v, t.scale);
-                to.exponent[lane] = v.exponent;
-                to.back[lane] = v.back;
-                to.rest[lane] = v.rest;
+        if (share == 0) { // (tokens of a page that is none: a score of -infinity for every row)
+            const bool there = is_page(a, t.page);
+            if (g == 0) to.scale[16 * block + i] = there ? t.scale : 0.f;
+            if (g == 1) {
+                Split v = split_scale(there ? t.scale : 0.f);
+                keep_apart(v, there ? t.scale : 0.f);
+                to.exponent[16 * block + i] = there ? v.exponent : NONE;
+                to.back[16 * block + i] = v.back;
+                to.rest[16 * block + i] = v.rest;
             }
         }
     };
 
-    auto take = [&](const Stage &st, int at, const Pages &pages) {
-        bool masked = at + T > certain;
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) masked = masked || !is_page(a, pages[b]);
+    auto take = [&](const Stage &st, int at) {
+        const bool masked = at + T > certain;
         v4f sc[R][BLOCKS];
 #pragma unroll
         for (int k = 0; k < STEPS; ++k)
@@ -731,7 +718,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[t][b][r] = sees(sight[t], at + 16 * b + 4 * g + r, held, is_page(a, pages[b])) ? sc[t][b][r] : NONE;
+                    for (int r = 0; r < 4; ++r) sc[t][b][r] = sees(sight[t], at + 16 * b + 4 * g + r, held, true) ? sc[t][b][r] : NONE;
         }
 #pragma unroll
         for (int t = 0; t < R; ++t) {
@@ -784,22 +771,20 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     if (from < to) {
         Codes codes;
         int at = (int)from;
-        Pages here = pages_of(at);
-        load(codes, at, here);
+        int page = ask_page(at + T);
+        load(codes, at, ask_page(at));
         convert(codes, stages[0]);
         for (int turn = 0;; turn ^= 1) {
             __syncthreads();
             const bool more = at + T < to;
-            Pages next = here;
             if (more) {
-                next = pages_of(at + T);
-                load(codes, at + T, next);
+                load(codes, at + T, page);
+                page = ask_page(at + 2 * T);
             }
-            if (at < wave_end) take(stages[turn], at, here);
+            if (at < wave_end) take(stages[turn], at);
             if (!more) break;
             convert(codes, stages[turn ^ 1]);
             at += T;
-            here = next;
         }
     }
 
