@@ -188,23 +188,25 @@ template <int BITS> __device__ __forceinline__ unsigned column_pair(unsigned fir
 
 // ---- the pieces ----------------------------------------------------------------------------------------
 template <int N> struct Words { unsigned w[N]; };
-// `at` bytes behind a base that is the same for the whole wave
-template <int BYTES> __device__ __forceinline__ Words<(BYTES + 3) / 4> load_bytes(const uint8_t *base, unsigned at)
+// `at` bytes behind a base that is the same for the whole wave (STREAM: that nobody reads again)
+template <int BYTES, bool STREAM = false> __device__ __forceinline__ Words<(BYTES + 3) / 4> load_bytes(const uint8_t *base, unsigned at)
 {
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    auto get = [&](auto *p) { return STREAM ? __builtin_nontemporal_load(p) : *p; };
     Words<(BYTES + 3) / 4> v;
     if constexpr (BYTES >= 16) {
         static_assert(BYTES == 16, "one request");
-        const v4u u = *reinterpret_cast<const v4u *>(base + at);
+        const v4u u = get(reinterpret_cast<const v4u *>(base + at));
 #pragma unroll
         for (int e = 0; e < 4; ++e) v.w[e] = u[e];
     } else if constexpr (BYTES == 8) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(base + at);
+        const v2u u = get(reinterpret_cast<const v2u *>(base + at));
         v.w[0] = u.x;
         v.w[1] = u.y;
     } else if constexpr (BYTES == 4) {
-        v.w[0] = *reinterpret_cast<const unsigned *>(base + at);
+        v.w[0] = get(reinterpret_cast<const unsigned *>(base + at));
     } else {
-        v.w[0] = *reinterpret_cast<const unsigned short *>(base + at);
+        v.w[0] = get(reinterpret_cast<const unsigned short *>(base + at));
     }
     return v;
 }
@@ -425,9 +427,9 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
             const int64_t first = place_of(a, pages.id[half], head, tile * CACHE_TILE + half * 16);
             const uint8_t *k = a.k_codes + first * row_bytes, *v = a.v_codes + first * row_bytes;
 #pragma unroll
-            for (int p = 0; p < S::NK; ++p) t.k[half][p] = load_bytes<PB>(k, k_at[p]);
+            for (int p = 0; p < S::NK; ++p) t.k[half][p] = load_bytes<PB, true>(k, k_at[p]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) t.v[half][r] = load_bytes<S::VB>(v, v_at[r]);
+            for (int r = 0; r < 4; ++r) t.v[half][r] = load_bytes<S::VB, true>(v, v_at[r]);
             t.ks[half] = *reinterpret_cast<const v4f *>(a.k_scales + first + 4 * g);
             t.vs[half] = *reinterpret_cast<const v4f *>(a.v_scales + first + 4 * g);
         }
