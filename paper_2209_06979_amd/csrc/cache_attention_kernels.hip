@@ -322,10 +322,10 @@ __device__ __forceinline__ int page_at(const CacheAttnArgs &a, const int32_t *ta
     const int nth = at >> a.page_shift;
     return __builtin_amdgcn_readfirstlane(nth <= last_page ? table[nth] : -1);
 }
-__device__ __forceinline__ bool is_page(const CacheAttnArgs &a, int page) { return page >= 0 && page < a.pages; }
+__device__ __forceinline__ bool is_page(const CacheAttnArgs &a, int page) { return (unsigned)page < (unsigned)a.pages; } // (at most 2^31 of them)
 __device__ __forceinline__ int64_t place_of(const CacheAttnArgs &a, int page, int head, int at)
 {
-    return (((is_page(a, page) ? (int64_t)page : 0) * a.kv_heads + head) << a.page_shift) + (at & ((1 << a.page_shift) - 1));
+    return (int64_t)((uint64_t)(is_page(a, page) ? (unsigned)page : 0u) * a.page_vectors + ((unsigned)head << a.page_shift) + ((unsigned)at & ((1u << a.page_shift) - 1)));
 }
 
 // A token's scale of V as 2^exponent times the rest
@@ -412,7 +412,10 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
     const int last_page = s.length > 0 ? (s.length - 1) >> a.page_shift : -1;
     const int32_t *table = a.table + cut.b * a.table_stride;
     auto pages_of = [&](int tile) {
-        return Pages{{page_at(a, table, last_page, tile * CACHE_TILE), page_at(a, table, last_page, tile * CACHE_TILE + 16)}};
+        Pages p;
+        p.id[0] = p.id[1] = page_at(a, table, last_page, tile * CACHE_TILE);
+        if (a.page_shift < 5) p.id[1] = page_at(a, table, last_page, tile * CACHE_TILE + 16);
+        return p;
     };
     struct Tile {
         Words<PB / 4> k[2][S::NK];
@@ -421,10 +424,13 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
         bool there[2];
     };
     auto load = [&](Tile &t, int tile, Pages pages) {
+        const int64_t place = place_of(a, pages.id[0], head, tile * CACHE_TILE);
+        int64_t other = place + 16;
+        if (a.page_shift < 5) other = place_of(a, pages.id[1], head, tile * CACHE_TILE + 16);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             t.there[half] = is_page(a, pages.id[half]);
-            const int64_t first = place_of(a, pages.id[half], head, tile * CACHE_TILE + half * 16);
+            const int64_t first = half ? other : place;
             const uint8_t *k = a.k_codes + first * row_bytes, *v = a.v_codes + first * row_bytes;
 #pragma unroll
             for (int p = 0; p < S::NK; ++p) t.k[half][p] = load_bytes<PB, true>(k, k_at[p]);

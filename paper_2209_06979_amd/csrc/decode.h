@@ -46,6 +46,7 @@ struct CacheAttnArgs {
     const float *k_scales, *v_scales;
     int64_t pages;
     int page_shift, kv_heads, dk, group;
+    unsigned page_vectors;       // kv_heads * page size
     const int32_t *lengths, *starts; // starts null: max_new rows per sequence
     const int32_t *table;
     int64_t table_stride;

@@ -181,6 +181,7 @@ extern "C" int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_t
     a.k_codes = static_cast<const uint8_t *>(cache->k_codes); a.v_codes = static_cast<const uint8_t *>(cache->v_codes);
     a.k_scales = cache->k_scales; a.v_scales = cache->v_scales;
     a.pages = cache->pages; a.page_shift = shift_of(cache->page_size); a.kv_heads = cache->kv_heads; a.dk = cache->dk; a.group = heads / cache->kv_heads;
+    a.page_vectors = (unsigned)cache->kv_heads * (unsigned)cache->page_size;
     a.lengths = lengths_dev; a.starts = starts_dev; a.table = table_dev; a.table_stride = table_stride; a.table_pages = table_pages;
     a.batch = batch; a.max_new = max_new; a.total_new = total_new; a.tree = tree_dev;
     a.q = q_dev; a.q_token_stride = q_token_stride; a.q_head_stride = q_head_stride;
