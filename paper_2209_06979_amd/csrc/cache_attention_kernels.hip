@@ -4,8 +4,9 @@
 // registers: S^T = K q^T, and with the probabilities where that product leaves them, o^T += V^T p^T (their places in a lane are the
 // reduction's order of the second product, which V's rows follow).  Both products run on 16-bit floating MFMAs, in which codes are exact.
 //
-// Scales of V: with s^v = f 2^e, 1/2 <= f < 1, the running maximum is taken over x + e instead of x (x the score in base 2), so that the
-// weights  w = 2^(x + e - max) f  of the second product are near 1 for the terms that count, whatever the scales; l = sum 2^(x + e - max) 2^-e.
+// Weights of the second product are halves of w = 2^(x - r) s^v, x the score in base 2 and r a reference of the row that follows the largest of x + e, e the
+// exponent of s^v: so they are of the size of 1 for the terms that count, whatever the scales.  The reference stays while no w is beyond 2^15, and is moved, with l and
+// o, so that the largest is about 2^7; a half keeps what is 2^-24 of 1.  l = sum 2^(x - r) in fp32.
 //
 // Sequences are cut into pieces of equal length, as many as fill the device: every workgroup works out its piece from the sequences' lengths,
 // which the host does not know.  A piece that is not its whole sequence leaves (maximum, l, o) to a second kernel.
@@ -18,7 +19,7 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
-constexpr float UP = 15.f;             // weights are held 2^15 times as large: f16 keeps what is 2^-24 of that
+constexpr float UP = 7.f, MOST = 15.f; // binary logarithm of a row's largest weight when its reference is moved, and when it has to be
 constexpr float NONE = -__builtin_inff();
 
 __device__ __forceinline__ unsigned bits_of(h2 v) { return __builtin_bit_cast(unsigned, v); }
@@ -40,6 +41,8 @@ __device__ __forceinline__ float sum_of_groups(float v)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+
+__device__ __forceinline__ float max_of(v4f v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
 
 // ---- which piece ---------------------------------------------------------------------------------------
 struct Sequence { int start, n, length; }; // first new token, new tokens, tokens in the cache with them
@@ -328,22 +331,40 @@ __device__ __forceinline__ int64_t place_of(const CacheAttnArgs &a, int page, in
     return (int64_t)((uint64_t)(is_page(a, page) ? (unsigned)page : 0u) * a.page_vectors + ((unsigned)head << a.page_shift) + ((unsigned)at & ((1u << a.page_shift) - 1)));
 }
 
-// A token's scale of V as 2^exponent times the rest
-struct Split { float exponent, back, rest; }; // back = 2^-exponent
-__device__ __forceinline__ Split split_scale(float vs)
+// The exponent of a scale: |scale| is below 2^exponent.  (At least -100: 2^(x - r) stays a number of fp32.)
+__device__ __forceinline__ float exponent_of(float scale)
 {
-    int x = __builtin_amdgcn_frexp_expf(vs);
-    x = x < -100 ? -100 : x;
-    const float back = __builtin_amdgcn_ldexpf(1.f, -x);
-    return {(float)x, back, vs * back};
+    const int e = __builtin_amdgcn_frexp_expf(scale);
+    return (float)(e < -100 ? -100 : e);
 }
-// A scale that is not finite makes the exponent NaN, and with it the rows that see the token; the rest is finite, so that a weight of zero makes nothing of
-// it.
-__device__ __forceinline__ void keep_apart(Split &v, float vs)
-{
-    v.exponent = __builtin_fmaf(vs, 0.f, v.exponent);
-    v.rest = __builtin_amdgcn_fmed3f(v.rest, -1.f, 1.f);
-}
+
+// A row's reference and sums
+template <int C> struct Row {
+    float m, l; // m: the reference, and 7 (NONE: nothing seen)
+    v4f o[C];
+    __device__ __forceinline__ float to_add() const { return m == NONE ? 0.f : UP - m; } // what scores become x - r by
+    __device__ __forceinline__ void clear()
+    {
+        m = NONE;
+        l = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = (v4f){0, 0, 0, 0};
+    }
+    // top: logarithm of the largest weight of some scores x - r, the same in the four lanes of a row.  Whether references move (of any row of the wave); by: what
+    // these scores are less then
+    __device__ __forceinline__ bool move(float top, float &by)
+    {
+        const bool must = top > MOST || (m == NONE && top > NONE);
+        if (!__any(must)) return false;
+        by = must ? top - UP : 0.f;
+        const float factor = m == NONE ? 1.f : __builtin_amdgcn_exp2f(-by);
+        m = must ? (m == NONE ? UP : m) + by : m;
+        l *= factor;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] *= factor;
+        return true;
+    }
+};
 
 // Which piece, head and rows a workgroup has.  Tiles of rows of the same piece and head follow each other on one XCD (workgroups go round the eight of
 // them).
@@ -441,10 +462,8 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
         }
     };
 
-    float m = NONE, l = 0;
-    v4f o[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = (v4f){0, 0, 0, 0};
+    Row<C> sums;
+    sums.clear();
 
     auto take = [&](Tile &tile, int number) {
         v4f sc[2];
@@ -474,56 +493,44 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
                 vs[e] = yes ? vs[e] : 0.f; // (whatever there is)
             }
         }
-        // Scores in base 2, plus exponents of V's scales: of each token's own, or (one half to a weight) that of the largest of a lane's eight, whose others
-        // keep their 11 bits while they are within 2^25 of it.
-        float x[8], exponent[8], back[8], rest[8];
-        if (PLANES == 2) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const Split v = split_scale(vs[e]);
-                exponent[e] = v.exponent;
-                back[e] = v.back;
-                rest[e] = v.rest;
-            }
-        } else {
-            float most = fabsf(vs[0]);
-#pragma unroll
-            for (int e = 1; e < 8; ++e) most = fmaxf(most, fabsf(vs[e]));
-            const Split v = split_scale(most);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                exponent[e] = v.exponent;
-                back[e] = v.back;
-                rest[e] = vs[e] * v.back;
-            }
-        }
+        float x[8];
+        const float to_add = sums.to_add();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float score = S::RAW ? __builtin_fmaf(sc[e / 4][e % 4], row_scale.scale, row_scale.offset) : sc[e / 4][e % 4] * row_scale.scale;
-            x[e] = __builtin_fmaf(score, tile.ks[e / 4][e % 4], exponent[e]);
+            x[e] = __builtin_fmaf(score, tile.ks[e / 4][e % 4], to_add);
         }
         if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? x[e] : NONE;
         }
-        float top = x[0];
+        // The largest weight: by each token's exponent, or (one half to a weight) by that of the largest scale of a lane's eight, whose others keep their 11 bits
+        // while they are within 2^20 of it.
+        float top, most = fabsf(vs[0]);
+        if (PLANES == 2) {
+            top = x[0] + exponent_of(vs[0]);
 #pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-        top = max_of_groups(top);
-        if (__any(top > m)) {
-            const float to = fmaxf(top, m), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= by;
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e] + exponent_of(vs[e]));
+        } else {
+            top = x[0];
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] *= by;
+            for (int e = 1; e < 8; ++e) {
+                top = fmaxf(top, x[e]);
+                most = fmaxf(most, fabsf(vs[e]));
+            }
+            top += exponent_of(most);
         }
-        const float from = (m == NONE ? 0.f : m) - UP;
+        float by;
+        if (sums.move(max_of_groups(top), by)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] -= by;
+        }
         h8 w[PLANES];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[e] - from);
-            l = __builtin_fmaf(p, back[e], l);
-            float v = p * rest[e];
+            const float p = __builtin_amdgcn_exp2f(x[e]);
+            sums.l += p;
+            float v = p * vs[e];
             if (PLANES == 2) asm("" : "+v"(v)); // (one product, rounded once: the first half by a fused rounding, and the second from another would differ at a tie)
             w[0][e] = (_Float16)v;
             if (PLANES == 2) w[PLANES - 1][e] = (_Float16)(v - (float)(_Float16)v);
@@ -535,7 +542,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
             const h8 v = operand(column_pair<BITS>(tile.v[0][0].w[n], tile.v[0][1].w[n], in), column_pair<BITS>(tile.v[0][2].w[n], tile.v[0][3].w[n], in),
                                  column_pair<BITS>(tile.v[1][0].w[n], tile.v[1][1].w[n], in), column_pair<BITS>(tile.v[1][2].w[n], tile.v[1][3].w[n], in));
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[p], o[c], 0, 0, 0);
+            for (int p = 0; p < PLANES; ++p) sums.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[p], sums.o[c], 0, 0, 0);
         }
     };
 
@@ -563,16 +570,16 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
     }
 
     // the waves' results meet in LDS
-    l = sum_of_groups(l);
+    const float sum_l = sum_of_groups(sums.l);
     if (g == 0) {
-        shared_m[wave][i] = m;
-        shared_l[wave][i] = l;
+        shared_m[wave][i] = sums.m;
+        shared_l[wave][i] = sum_l;
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < C; c += 4)
-            *reinterpret_cast<v4f *>(&shared_o[wave][i][(4 * g + r) * C + c]) = (v4f){o[c][r], o[c + 1][r], o[c + 2][r], o[c + 3][r]};
+            *reinterpret_cast<v4f *>(&shared_o[wave][i][(4 * g + r) * C + c]) = (v4f){sums.o[c][r], sums.o[c + 1][r], sums.o[c + 2][r], sums.o[c + 3][r]};
     __syncthreads();
     const int of = threadIdx.x / 16, col = threadIdx.x % 16 * C;
     float sum[C] = {}, all_m = NONE, all_l = 0;
@@ -580,8 +587,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
     for (int w = 0; w < CACHE_WAVES; ++w) all_m = fmaxf(all_m, shared_m[w][of]);
 #pragma unroll
     for (int w = 0; w < CACHE_WAVES; ++w) {
-        if (shared_m[w][of] == NONE) continue;
-        const float by = __builtin_amdgcn_exp2f(shared_m[w][of] - all_m);
+        const float by = all_m == NONE ? 1.f : __builtin_amdgcn_exp2f(shared_m[w][of] - all_m);
         all_l += shared_l[w][of] * by;
 #pragma unroll
         for (int c = 0; c < C; ++c) sum[c] += shared_o[w][of][col + c] * by;
@@ -598,11 +604,12 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     constexpr int T = D <= 128 ? 64 : 32, BLOCKS = T / 16, PAIRS = T / 32;  // tokens of a tile, in blocks of 16 and 32
     constexpr int SHARE = CACHE_WAVES / BLOCKS, KU = S::NK / SHARE, VB = S::VB / SHARE, VC = C / SHARE; // waves that convert 16 tokens, each some pieces of K and columns of V
     static_assert(KU * SHARE == S::NK && VC * SHARE == C, "even shares");
-    struct Stage {
+    struct alignas(16) Stage {
         uint8_t k[BLOCKS * STEPS * 1024], v[PAIRS * C * 1024];
-        float scale[T], exponent[T], back[T], rest[T];
+        float k_scale[T], v_scale[T], exponent[T / 4]; // (of the largest of four tokens' scales of V)
+        uint8_t there[4];                              // whether a block's page is one
     };
-    __shared__ __attribute__((aligned(16))) Stage stages[2];
+    __shared__ Stage stages[2];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const Unit unit = unit_of(a, CACHE_WAVES * 16 * R);
@@ -620,30 +627,25 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     const int wave_end = row0 >= rows ? 0 : a.tree ? s.length : held + wave_last / a.group + 1;
     const int certain = a.tree ? held : held + row0 / a.group + 1;
 
-    Sight sight[R];
+    int token[R]; // of this lane's rows
     RowScale row_scale[R];
-    float m[R], l[R];
     h8 q[R][PLANES][STEPS];
-    v4f o[R][C];
+    Row<C> sums[R];
 #pragma unroll
     for (int t = 0; t < R; ++t) {
         const int row = row0 + 16 * t + i < rows ? row0 + 16 * t + i : rows - 1; // (rows beyond the last repeat it)
-        sight[t] = sight_of(a, s, row / a.group);
-        row_scale[t] = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)(row / a.group)) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q[t]);
-        m[t] = NONE;
-        l[t] = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[t][c] = (v4f){0, 0, 0, 0};
+        token[t] = row / a.group;
+        row_scale[t] = load_q<S, BITS, TYPE>(a, (s.start + (int64_t)token[t]) * a.q_token_stride + (int64_t)(head * a.group + row % a.group) * a.q_head_stride, g, q[t]);
+        sums[t].clear();
     }
 
     // What this wave converts: of a tile's tokens 16 (one page), and their scales, of K in lanes 0 .. 15 and of V in the next 16.  The page is asked for a tile's
     // turn ahead.
     const int row_bytes = a.dk * BITS / 8, block = wave / SHARE, share = wave % SHARE;
-    unsigned k_at[KU], v_at[4];
+    unsigned k_at[KU];
 #pragma unroll
     for (int u = 0; u < KU; ++u) k_at[u] = k_offset<S>(share * KU + u, i, g, row_bytes);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v_at[r] = (4 * g + r) * row_bytes + (i * C + share * VC < a.dk ? i * S::VB + share * VB : 0);
+    const unsigned v_at = 4 * g * row_bytes + (i * C + share * VC < a.dk ? i * S::VB + share * VB : 0);
     const int last_page = s.length > 0 ? (s.length - 1) >> a.page_shift : -1;
     const int32_t *table = a.table + cut.b * a.table_stride;
     auto ask_page = [&](int at) { // (a load by lanes: as a scalar one it would hold up the waits for LDS, which share its counter)
@@ -653,19 +655,20 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     struct Codes {
         Words<PB / 4> k[KU];
         Words<(VB + 3) / 4> v[4];
-        float scale;
-        int page;
+        float k_scale, v_scale;
+        bool there;
     };
-    const float *scales = g == 0 ? a.k_scales : a.v_scales;
     auto load = [&](Codes &t, int at, int page) {
-        t.page = __builtin_amdgcn_readfirstlane(page);
-        const int64_t first = place_of(a, t.page, head, at + 16 * block);
+        page = __builtin_amdgcn_readfirstlane(page);
+        t.there = is_page(a, page);
+        const int64_t first = place_of(a, page, head, at + 16 * block);
         const uint8_t *k = a.k_codes + first * row_bytes, *v = a.v_codes + first * row_bytes;
 #pragma unroll
         for (int u = 0; u < KU; ++u) t.k[u] = load_bytes<PB>(k, k_at[u]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) t.v[r] = load_bytes<VB>(v, v_at[r]);
-        t.scale = scales[first + i];
+        for (int r = 0; r < 4; ++r) t.v[r] = load_bytes<VB>(v + r * row_bytes, v_at);
+        t.k_scale = a.k_scales[first + i];
+        t.v_scale = a.v_scales[first + i];
     };
     auto convert = [&](Codes &t, Stage &to) {
 #pragma unroll
@@ -681,21 +684,24 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
             *reinterpret_cast<uint2 *>(&to.v[(block / 2 * C + share * VC + c) * 1024 + lane * 16 + block % 2 * 8]) =
                 make_uint2(column_pair<BITS>(t.v[0].w[n], t.v[1].w[n], in), column_pair<BITS>(t.v[2].w[n], t.v[3].w[n], in));
         }
-        if (share == 0) { // (tokens of a page that is none: a score of -infinity for every row)
-            const bool there = is_page(a, t.page);
-            if (g == 0) to.scale[16 * block + i] = there ? t.scale : 0.f;
-            if (g == 1) {
-                Split v = split_scale(there ? t.scale : 0.f);
-                keep_apart(v, there ? t.scale : 0.f);
-                to.exponent[16 * block + i] = there ? v.exponent : NONE;
-                to.back[16 * block + i] = v.back;
-                to.rest[16 * block + i] = v.rest;
+        if (share == 0) {
+            // a scale of V that is not finite goes into the scores, from where it reaches the rows that see the token and no other
+            const bool finite = fabsf(t.v_scale) < __builtin_inff();
+            const float v = finite ? t.v_scale : 0.f;
+            float most = fabsf(v);
+            most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0xB1, 0xF, 0xF, true))); // quad_perm 1 0 3 2
+            most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0x4E, 0xF, 0xF, true))); // quad_perm 2 3 0 1
+            if (g == 0) {
+                to.k_scale[16 * block + i] = finite ? t.k_scale : __builtin_nanf("");
+                to.v_scale[16 * block + i] = v;
+                to.exponent[4 * block + i / 4] = exponent_of(most);
+                to.there[block] = (uint8_t)t.there;
             }
         }
     };
 
     auto take = [&](const Stage &st, int at) {
-        const bool masked = at + T > certain;
+        const unsigned there = *reinterpret_cast<const unsigned *>(st.there), all_there = BLOCKS == 4 ? 0x01010101u : 0x0101u;
         v4f sc[R][BLOCKS];
 #pragma unroll
         for (int k = 0; k < STEPS; ++k)
@@ -708,38 +714,55 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
                     for (int p = 0; p < PLANES; ++p)
                         sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[t][p][k], k == 0 && p == 0 ? (v4f){0, 0, 0, 0} : sc[t][b], 0, 0, 0);
             }
-        // scores in base 2, plus the exponents of V's scales
+        float to_add[R];
+#pragma unroll
+        for (int t = 0; t < R; ++t) to_add[t] = sums[t].to_add();
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-            const v4f ks = *reinterpret_cast<const v4f *>(&st.scale[16 * b + 4 * g]), ex = *reinterpret_cast<const v4f *>(&st.exponent[16 * b + 4 * g]);
+            const v4f ks = *reinterpret_cast<const v4f *>(&st.k_scale[16 * b + 4 * g]);
 #pragma unroll
             for (int t = 0; t < R; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float score = S::RAW ? __builtin_fmaf(sc[t][b][r], row_scale[t].scale, row_scale[t].offset) : sc[t][b][r] * row_scale[t].scale;
-                    sc[t][b][r] = __builtin_fmaf(score, ks[r], ex[r]);
+                    sc[t][b][r] = __builtin_fmaf(score, ks[r], to_add[t]);
                 }
         }
-        if (masked) {
+        // the largest weight: by the exponent of four tokens, or of each where not all of them are seen
+        float top[R];
 #pragma unroll
-            for (int t = 0; t < R; ++t)
+        for (int t = 0; t < R; ++t) top[t] = NONE;
+        if (at + T > certain || (__builtin_amdgcn_readfirstlane(there) & all_there) != all_there) {
+            Sight sight[R];
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b)
+            for (int t = 0; t < R; ++t) sight[t] = sight_of(a, s, token[t]);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[t][b][r] = sees(sight[t], at + 16 * b + 4 * g + r, held, true) ? sc[t][b][r] : NONE;
+            for (int b = 0; b < BLOCKS; ++b) {
+                const v4f vs = *reinterpret_cast<const v4f *>(&st.v_scale[16 * b + 4 * g]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float ex = exponent_of(vs[r]);
+#pragma unroll
+                    for (int t = 0; t < R; ++t) {
+                        sc[t][b][r] = sees(sight[t], at + 16 * b + 4 * g + r, held, there >> 8 * b & 1) ? sc[t][b][r] : NONE;
+                        top[t] = fmaxf(top[t], sc[t][b][r] + ex);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const float ex = st.exponent[4 * b + g];
+#pragma unroll
+                for (int t = 0; t < R; ++t) top[t] = fmaxf(top[t], max_of(sc[t][b]) + ex);
+            }
         }
 #pragma unroll
         for (int t = 0; t < R; ++t) {
-            float top = sc[t][0][0];
+            float by;
+            if (sums[t].move(max_of_groups(top[t]), by)) {
 #pragma unroll
-            for (int e = 1; e < 4 * BLOCKS; ++e) top = fmaxf(top, sc[t][e / 4][e % 4]);
-            top = max_of_groups(top);
-            if (__any(top > m[t])) {
-                const float to = fmaxf(top, m[t]), by = to == NONE ? 1.f : __builtin_amdgcn_exp2f(m[t] - to);
-                m[t] = to;
-                l[t] *= by;
-#pragma unroll
-                for (int c = 0; c < C; ++c) o[t][c] *= by;
+                for (int b = 0; b < BLOCKS; ++b) sc[t][b] -= by;
             }
         }
 #pragma unroll
@@ -748,20 +771,18 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int b = 2 * pair + half;
-                const v4f back = *reinterpret_cast<const v4f *>(&st.back[16 * b + 4 * g]), rest = *reinterpret_cast<const v4f *>(&st.rest[16 * b + 4 * g]);
+                const v4f vs = *reinterpret_cast<const v4f *>(&st.v_scale[16 * b + 4 * g]);
 #pragma unroll
-                for (int t = 0; t < R; ++t) {
-                    const float from = (m[t] == NONE ? 0.f : m[t]) - UP;
+                for (int t = 0; t < R; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(sc[t][b][r] - from);
-                        l[t] = __builtin_fmaf(p, back[r], l[t]);
-                        float v = p * rest[r];
+                        const float p = __builtin_amdgcn_exp2f(sc[t][b][r]);
+                        sums[t].l += p;
+                        float v = p * vs[r];
                         if (PLANES == 2) asm("" : "+v"(v)); // (as above)
                         w[t][0][4 * half + r] = (_Float16)v;
                         if (PLANES == 2) w[t][PLANES - 1][4 * half + r] = (_Float16)(v - (float)(_Float16)v);
                     }
-                }
             }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -769,7 +790,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 #pragma unroll
                 for (int t = 0; t < R; ++t)
 #pragma unroll
-                    for (int p = 0; p < PLANES; ++p) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][p], o[t][c], 0, 0, 0);
+                    for (int p = 0; p < PLANES; ++p) sums[t].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][p], sums[t].o[c], 0, 0, 0);
             }
         }
     };
@@ -798,15 +819,15 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-        const float sum_l = sum_of_groups(l[t]);
+        const float sum_l = sum_of_groups(sums[t].l);
         const int row = row0 + 16 * t + i;
         if (row >= rows) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float v[C];
 #pragma unroll
-            for (int c = 0; c < C; ++c) v[c] = o[t][c][r];
-            put<D, TYPE, C>(a, cut, head, row, (4 * g + r) * C, v, m[t], sum_l);
+            for (int c = 0; c < C; ++c) v[c] = sums[t].o[c][r];
+            put<D, TYPE, C>(a, cut, head, row, (4 * g + r) * C, v, sums[t].m, sum_l);
         }
     }
 }
@@ -836,12 +857,11 @@ template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attentio
                 const int64_t at = line + (p < cut.pieces ? p : 0) * step;
                 v[e] = *reinterpret_cast<const v4f *>(a.partial + at * D + col);
                 ml[e] = *reinterpret_cast<const float2 *>(a.sums + at * 2);
-                if (p >= cut.pieces) ml[e].x = NONE;
             }
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
-                if (ml[e].x == NONE) continue;
-                const float by = __builtin_amdgcn_exp2f(ml[e].x - m);
+                if (p0 + e * AT_ONCE + first >= cut.pieces) continue;
+                const float by = m == NONE ? 1.f : __builtin_amdgcn_exp2f(ml[e].x - m);
                 l += ml[e].y * by;
                 sum += v[e] * by;
             }

@@ -159,6 +159,10 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it():
     p.vs[page, 0, t % 16] = np.nan
     out = p.run()
     assert bool(torch.isfinite(out[:6]).all()) and bool(torch.isnan(out[6:]).all())
+    p.tree = [1 << i for i in range(12)]
+    out = p.run()
+    assert bool(torch.isnan(out[6]).all()) and bool(torch.isfinite(out[[0, 5, 7, 11]]).all())
+    p.tree = None
     p.vs[page, 0, t % 16] = 1
     p.ks[page, 0, t % 16] = np.inf
     out = p.run()
@@ -172,6 +176,18 @@ def test_pages_that_are_none_are_seen_by_nobody():
     out = p.run()
     p.check(out)
     assert bool((out[5:] == 0).all())
+
+
+@pytest.mark.parametrize("group", [1, 8])
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_rows_that_see_nothing_but_nan_are_nan(dtype, group):
+    """... and neither rows of zeros nor other rows: no history, every new token by itself, one value's scale and one key's not finite."""
+    import torch
+    p = Problem([0], [12], kv_heads=1, group=group, dtype=dtype, seed=24)
+    p.tree = [1 << i for i in range(11)] + [0]
+    p.vs[p.table[0, 0], 0, 3], p.ks[p.table[0, 0], 0, 8] = np.nan, np.nan
+    out = p.run()
+    assert bool(torch.isnan(out[[3, 8]]).all()) and bool(torch.isfinite(out[[0, 1, 2, 4, 5, 6, 7, 9, 10]]).all()) and bool((out[11] == 0).all())
 
 
 @pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
