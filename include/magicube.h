@@ -600,14 +600,16 @@ int mc_cache_read(const mc_cache *cache, const int64_t *slots_dev, int64_t token
 /* Attention of new tokens over the cache that holds their keys and values already: the layer's form for decoding.
  *   q_dev, o_dev   total_new x heads x dk of `type`, 16-byte aligned, strides whole 16-byte pieces; heads a multiple of kv_heads, query
  *                  head h reads head h / (heads / kv_heads) of the cache.  o_dev must not overlap q_dev
- *   starts_dev     batch + 1 int32: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1, at most max_new of them (rows beyond are not
- *                  computed; neither are sequences whose rows are not rows of q_dev, nor rows of no sequence: these rows of o_dev stay as they were).
+ *   starts_dev     batch + 1 int32: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1, at most max_new of them (rows beyond are new
+ *                  tokens, too, but not computed; neither are sequences whose rows are not rows of q_dev, nor rows of no sequence: these rows of o_dev stay as they were).
  *                  NULL: max_new rows each, one sequence after the other
- *   lengths_dev    batch int32: tokens of the sequence in the cache, its n new ones (the last) included; values are cut to 0 .. table_pages * page_size
+ *   lengths_dev    batch int32: tokens of the sequence in the cache, its n new ones (the last) included; values are cut to 0 .. table_pages * page_size,
+ *                  which is at most 2^30 (all sequences together: 2^30 tiles of 32)
  *   table_dev      batch rows of table_pages int32, table_stride entries apart: the pages of a sequence in order.  Tokens of a page that is not
  *                  0 .. pages - 1 are seen by nobody
  *   tree_dev       NULL: new token i sees every token up to itself.  Else total_new uint64: new token i of a sequence sees all tokens before the new ones, and new
  *                  token j where bit j of its word is set (its own bit included, or not); max_new <= 64 then
+ * batch is at most 65535, max_new * heads / kv_heads at most 262140, and (batch + 512) * kv_heads for each 128 rows of that at most some 8 million.
  * Softmax over score_scale * (q . k), score_scale finite.  A row that sees nothing is zero; keys and values that a row does not see (an infinity or a NaN
  * among them) do not change it.  fp32 accumulation; fp16 and bf16 weights of the second product are rounded to 11 bits relative to the row's largest.  Results do not
  * depend on what else is in the batch beyond the order of fp32 sums, and are the same from call to call.

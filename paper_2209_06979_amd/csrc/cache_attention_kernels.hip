@@ -45,21 +45,22 @@ __device__ __forceinline__ float sum_of_groups(float v)
 __device__ __forceinline__ float max_of(v4f v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
 
 // ---- which piece ---------------------------------------------------------------------------------------
-struct Sequence { int start, n, length; }; // first new token, new tokens, tokens in the cache with them
+struct Sequence { int start, n, length, held; }; // first new token, new tokens, tokens in the cache with them and before them
 __device__ __forceinline__ Sequence sequence(const CacheAttnArgs &a, int b)
 {
     Sequence s;
     const int64_t most = (int64_t)a.table_pages << a.page_shift;
     const int length = a.lengths[b];
     s.length = length < 0 ? 0 : length > most ? (int)most : length;
+    int fresh = a.max_new;
+    s.start = b * a.max_new;
     if (a.starts) {
         s.start = a.starts[b];
         const int behind = a.starts[b + 1];
-        s.n = s.start < 0 || behind <= s.start || behind > a.total_new ? 0 : behind - s.start < a.max_new ? behind - s.start : a.max_new;
-    } else {
-        s.start = b * a.max_new;
-        s.n = a.max_new;
+        fresh = s.start < 0 || behind <= s.start || behind > a.total_new ? 0 : behind - s.start;
     }
+    s.n = fresh < a.max_new ? fresh : a.max_new; // (rows beyond are not computed)
+    s.held = s.length - fresh;
     return s;
 }
 __device__ __forceinline__ int tiles_of(const Sequence &s) { return s.n == 0 ? 0 : s.length <= 0 ? 1 : (s.length - 1) / CACHE_TILE + 1; }
@@ -96,7 +97,7 @@ struct Cut { int b, each, pieces, slot, index; Sequence of; };
 template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnArgs &a, int number)
 {
     const int lane = threadIdx.x & 63;
-    const Sequence none = {0, 0, 0};
+    const Sequence none = {0, 0, 0, 0};
     Sequence s = lane < a.batch ? sequence(a, lane) : none;
     int t = tiles_of(s), total = 0;
     if (a.partial) {
@@ -129,7 +130,7 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
             c.each = (at_lane(t, l) + c.pieces * CACHE_WAVES - 1) / (c.pieces * CACHE_WAVES) * CACHE_WAVES;
             c.slot = slots + at_lane(cut_up_to, l) - (c.pieces > 1 ? c.pieces : 0);
             c.index = number - before - at_lane(up_to, l) + c.pieces;
-            c.of = {at_lane(s.start, l), at_lane(s.n, l), at_lane(s.length, l)};
+            c.of = {at_lane(s.start, l), at_lane(s.n, l), at_lane(s.length, l), at_lane(s.held, l)};
             break;
         }
         before += at_lane(up_to, 63);
@@ -299,9 +300,9 @@ template <class S, int BITS, int TYPE> __device__ __forceinline__ RowScale load_
 struct Sight { int all; uint64_t bits; };
 __device__ __forceinline__ Sight sight_of(const CacheAttnArgs &a, const Sequence &s, int token)
 {
-    const int held = s.length - s.n;
-    if (!a.tree) return {held + token + 1, 0};
-    return {held, a.tree[s.start + token] & (s.n < 64 ? (1ull << s.n) - 1 : ~0ull)};
+    if (!a.tree) return {s.held + token + 1, 0};
+    const int fresh = s.length - s.held;
+    return {s.held, a.tree[s.start + token] & (fresh < 64 ? (1ull << fresh) - 1 : ~0ull)};
 }
 // (no branches: as such the compiler lost some of the -infinities between them)
 __device__ __forceinline__ unsigned sees(const Sight &s, int token, int held, bool there)
@@ -412,7 +413,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
     const Sequence s = cut.of;
     const int rows = s.n * a.group, head = unit.head, row0 = unit.rows_at;
     if (row0 >= rows) return;
-    const int held = s.length - s.n;
+    const int held = s.held;
 
     const int row = row0 + i < rows ? row0 + i : rows - 1; // (rows beyond the last repeat it)
     const Sight sight = sight_of(a, s, row / a.group);
@@ -619,7 +620,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     const Sequence s = cut.of;
     const int rows = s.n * a.group, head = unit.head;
     if (unit.rows_at >= rows) return;
-    const int held = s.length - s.n;
+    const int held = s.held;
     const int group_last = unit.rows_at + CACHE_WAVES * 16 * R - 1 < rows ? unit.rows_at + CACHE_WAVES * 16 * R - 1 : rows - 1;
     const int end = a.tree ? s.length : held + group_last / a.group + 1;   // no row of the workgroup sees more
     // this wave's rows (none: it converts for the others), the first token that none of them sees, and the first that not every one sees
@@ -890,7 +891,7 @@ template <int D, int BITS, int TYPE> hipError_t launch(CacheAttnArgs a, int row_
                                           : launch_kernel((cache_attention_rows_kernel<D, BITS, TYPE, 2>), grid, block, 0, s, a);
     if (e != hipSuccess || !a.partial) return e;
     // enough workgroups for the device, and few enough to be gone at once where nothing was cut
-    const int most = (a.rows_held + 3) / 4, some = 2048 / (a.batch * a.kv_heads) + 1;
+    const int most = (a.rows_held + 3) / 4, some = 2048 / (a.batch * a.kv_heads) + 1; // (batch * kv_heads is less than the workgroups above)
     return launch_kernel((cache_attention_join_kernel<D, TYPE>), dim3(a.batch, a.kv_heads, most < some ? most : some), dim3(256), 0, s, a);
 }
 

@@ -12,7 +12,7 @@ inline int size_of(mc_type t) { return t == MC_F32 ? 4 : 2; }
 // strides of (token, head) tensors: whole 16-byte pieces
 inline bool whole_pieces(int64_t a, int64_t b, int size) { return a * size % 16 == 0 && b * size % 16 == 0; }
 
-constexpr int64_t MOST_TOKENS = (int64_t)1 << 31, MOST_GROUPS = 0x7fffffff / 256; // (a grid's threads are counted in 32 bits)
+constexpr int64_t MOST_TOKENS = (int64_t)1 << 31, MOST_CACHED = (int64_t)1 << 30, MOST_GROUPS = 0x7fffffff / 256; // (a grid's threads are counted in 32 bits)
 
 // Checks a cache and that its device is the current one.
 int check(const mc_cache *c)
@@ -44,19 +44,21 @@ CacheArgs args_of(const mc_cache *c)
     return a;
 }
 
+CacheAttnPlan plan_of(const mc_cache *c, int heads, int batch, int max_new, int table_pages)
+{
+    return cache_attention_plan(c->kv_heads, c->dk, heads / c->kv_heads, batch, max_new, (int64_t)table_pages * c->page_size);
+}
+
 // The shape of a call of the attention: what it and its workspace agree on.
 int check_shape(const mc_cache *c, int heads, int batch, int max_new, int table_pages)
 {
     if (heads < 1 || heads % c->kv_heads != 0 || batch < 0 || batch > 65535 || max_new < 0 || table_pages < 0) return MC_EINVAL;
     const int64_t tokens = (int64_t)table_pages * c->page_size, rows = (int64_t)max_new * (heads / c->kv_heads);
-    if (tokens >= MOST_TOKENS || rows > 65535 * 4) return MC_EINVAL;
-    if (batch * (tokens / CACHE_TILE + 1) >= MOST_TOKENS) return MC_EINVAL; // (tiles are counted in 32 bits)
+    // (tokens, a few tiles behind them too, and all sequences' tiles, are counted in 31 bits)
+    if (tokens > MOST_CACHED || rows > 65535 * 4 || batch * (tokens / CACHE_TILE + 1) > MOST_CACHED) return MC_EINVAL;
+    const CacheAttnPlan p = plan_of(c, heads, batch, max_new, table_pages);
+    if (((int64_t)p.pieces + batch) * c->kv_heads > (MOST_GROUPS - 4096) / (p.row_tiles > 0 ? p.row_tiles : 1)) return MC_EINVAL;
     return MC_OK;
-}
-
-CacheAttnPlan plan_of(const mc_cache *c, int heads, int batch, int max_new, int table_pages)
-{
-    return cache_attention_plan(c->kv_heads, c->dk, heads / c->kv_heads, batch, max_new, (int64_t)table_pages * c->page_size);
 }
 
 } // namespace

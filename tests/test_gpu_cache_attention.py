@@ -260,6 +260,21 @@ def test_malformed_starts_compute_what_is_there():
     assert torch.equal(out[:2], want[:2]) and bool((out[4] == 5).all()) and bool((out[8:] == 5).all())
 
 
+@pytest.mark.parametrize("tree", [False, True])
+def test_rows_beyond_max_new_are_tokens_but_not_computed(tree):
+    import torch
+    p = Problem([33, 100, 8], [2, 7, 5], seed=23)
+    if tree:
+        p.tree = [1 << i | 1 for n in (2, 7, 5) for i in range(n)]
+        p.tree[3] |= 1 << 6                                      # a later token, none of the rows
+    out = torch.full_like(p.q, 5.0)
+    p.run(out=out, max_new=3)
+    assert bool((out[5:9] == 5).all()) and bool((out[12:] == 5).all())
+    whole = p.run()
+    out[5:9], out[12:] = whole[5:9], whole[12:]
+    p.check(out)
+
+
 def test_empty_calls():
     import torch
     from paper_2209_06979_amd import binding as mc
@@ -342,3 +357,31 @@ def test_a_decoding_loop_as_it_is_used():
             other = mc.cache_attention(q, cache, table, lengths)
             side.synchronize()
             assert torch.equal(out, want) and torch.equal(other, want)
+
+
+def test_two_captured_calls_with_their_workspaces():
+    """Sequences that are cut, captured twice (one workspace given, one made inside), replayed on two streams at once between eager calls; the
+    lengths that a replay reads are those of the moment."""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    p = Problem([5000, 300, 9000], [1] * 3, kv_heads=2, group=4, dk=128, page=64, seed=25)
+    cache, (table, lengths, _) = p.cache(), p.args()
+    need = mc.cache_attention_workspace(cache, 8, 3, 1, table.shape[1])
+    assert need > 0
+    ws, full, half = torch.empty(need, dtype=torch.uint8, device="cuda"), lengths.clone(), lengths // 2
+    want = [mc.cache_attention(p.q, cache, table, n) for n in (full, half)]
+    p.check(want[0])
+    streams, outs, graphs = [torch.cuda.Stream() for _ in "ab"], [torch.empty_like(p.q) for _ in "ab"], [torch.cuda.CUDAGraph() for _ in "ab"]
+    torch.cuda.synchronize()
+    for s, o, g, w in zip(streams, outs, graphs, (ws, None)):
+        with torch.cuda.graph(g, stream=s):
+            mc.cache_attention(p.q, cache, table, lengths, out=o, workspace=w)
+    for turn in range(4):
+        lengths.copy_(half if turn % 2 else full)
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = mc.cache_attention(p.q, cache, table, lengths)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[turn % 2]) for o in outs + [eager])

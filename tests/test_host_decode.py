@@ -89,7 +89,8 @@ REFUSED = [
     (_attend, dict(starts=None, total=4), mc.MC_EINVAL), (_attend, dict(q=None), mc.MC_EINVAL), (_attend, dict(o=None), mc.MC_EINVAL), (_attend, dict(lengths=None), mc.MC_EINVAL),
     (_attend, dict(table=None), mc.MC_EINVAL), (_attend, dict(q=AT + 8), mc.MC_EALIGN), (_attend, dict(o=AT + 4), mc.MC_EALIGN), (_attend, dict(type=1, qhs=68), mc.MC_EALIGN),
     (_attend, dict(max_new=1 << 20, heads=1000), mc.MC_EINVAL), (_attend, dict(pages=1 << 27, stride=1 << 27), mc.MC_EINVAL),
-    (_attend, dict(pages=1 << 20, stride=1 << 20, batch=65535), mc.MC_EINVAL),
+    (_attend, dict(pages=1 << 20, stride=1 << 20, batch=65535), mc.MC_EINVAL), (_attend, dict(pages=(1 << 26) + 1, stride=1 << 27), mc.MC_EINVAL),
+    (_attend, dict(cache=_cache(kv_heads=65535), heads=65535, batch=500), mc.MC_EINVAL), (_attend, dict(batch=65535, max_new=65535, total=65535), mc.MC_EINVAL),
     (_attend, dict(pages=4000, stride=4000), mc.MC_ENOMEM), (_attend, dict(pages=4000, stride=4000, ws=AT, ws_bytes=1024), mc.MC_ENOMEM),
     (_attend, dict(pages=4000, stride=4000, ws=AT + 16, ws_bytes=1 << 40), mc.MC_EALIGN),
 ]
@@ -130,6 +131,7 @@ def test_workspace(lib):
                                                         kw.get("max_new", 1), kw.get("pages", 4000))
     assert ask(pages=16) == 0 and ask(pages=0) == 0 and ask(batch=0) == 0 and ask(max_new=0) == 0 and ask(heads=3) == 0
     assert ask() > 0 and ask() % 4 == 0 and ask(batch=60000) >= ask() and ask(batch=60000) <= 2 * 1024 * 16 * (64 + 2) * 4
+    assert ask(kv_heads=65535, heads=65535, batch=500) == 0 and ask(pages=(1 << 26) + 1) == 0 and ask(pages=1 << 26) > 0   # (sizes that are refused; the longest)
     need = ask(dk=64)
     assert _attend(lib, batch=8, total=8, pages=4000, stride=4000, ws=AT, ws_bytes=need) == 0
     assert _attend(lib, batch=8, total=8, pages=4000, stride=4000, ws=AT, ws_bytes=need - 4) == mc.MC_ENOMEM
