@@ -9,7 +9,8 @@
 // o, so that the largest is about 2^7; a half keeps what is 2^-24 of 1.  l = sum 2^(x - r) in fp32.
 //
 // Sequences are cut into pieces of equal length, as many as fill the device: every workgroup works out its piece from the sequences' lengths,
-// which the host does not know.  A piece that is not its whole sequence leaves (maximum, l, o) to a second kernel.
+// which the host does not know.  A piece that is not its whole sequence leaves (reference, l, o) to a second kernel.
+// (Pieces of the same length through sequences' borders, each workgroup with parts of two, were slower: short parts, and registers for two sequences.)
 #include "decode.h"
 
 namespace {
@@ -398,6 +399,10 @@ template <int D, int TYPE, int C> __device__ __forceinline__ void put(const Cach
 }
 
 // Up to 16 rows: the waves of a workgroup take a piece's tiles of 32 tokens in turn, from memory through registers alone.
+// Memory bounds it where there is much to read: 2216 MB (64 sequences of 16384, 8 heads of 128, 8 bits) in 340 us, 6.5 TB/s of 6.9 that reading alone reaches; with ordinary
+// instead of streaming loads 375.  In 4 bits (285 MB, two sequences of 131072) 55 us, 5.1 TB/s: there are twice as many conversions to a byte.  Unequal sequences (190 MB) take
+// 43 us: 3 us until lengths and first pages are there, and workgroups of unequal work at the end.  Tried without gain: tiles three ahead, page ids a wave holds in its lanes, three waves
+// of longer tiles, wave priorities.
 template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_kernel(CacheAttnArgs a)
 {
     typedef Shape<D, BITS, TYPE> S;
@@ -597,7 +602,11 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 }
 
 // More rows: each wave has R tiles of 16 rows, and the workgroup converts a piece's tokens, 64 at a time (32 for D = 256), once for all of them.  The operands lie in LDS as
-// the MFMAs take them, 16 bytes a lane side by side, two tiles of tokens in turn; beside them what a token's scales are taken apart into.
+// the MFMAs take them, 16 bytes a lane side by side, two tiles of tokens in turn; beside them their scales.
+// What bounds it is the issue of what is not a matrix product: 4 sequences of 512 new tokens over 4096, 32 heads of 128, 133 Gflop in 205 us (650 Tflop/s; a library's bf16 product of 8192^3 reaches 1216), the
+// matrix unit busy 25 % and the vector unit 51 % of the cycles, LDS conflicts 3 %.  Of 314 vector instructions a wave and tile (R = 2), 82 convert, 74 make scores, 46 find the largest weight, and 112,
+// 32 of them exponentials at a quarter of the rate, make weights.  Codes that each wave converted for itself took 595 us.  Tried without gain: weights made first and the largest sought only
+// where they do not fit (registers spill: 527 - 710 us), weights by one mixed multiply-add (212), wave priorities, 32 tokens at a time.
 template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_rows_kernel(CacheAttnArgs a)
 {
     typedef Shape<D, BITS, TYPE> S;
@@ -833,7 +842,9 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
     }
 }
 
-// Pieces of sequences that were cut, joined in their order: a wave per row (and further rows after it), D / 4 lanes per piece.
+// Pieces of sequences that were cut, joined in their order: a wave per row (and further rows after it), D / 4 lanes per piece.  3.5 - 5 us where rows are few: a launch and three trips to memory.
+// (16 sequences of up to 192 rows, 8 heads, two or three pieces: 17.6 us, 30 MB written by other XCDs just before; more or fewer workgroups and all pieces' requests at once: 94 - 109 us
+// for the whole call instead of 93.)
 template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheAttnArgs a)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, AHEAD = 8;
