@@ -4,7 +4,7 @@
 // registers: S^T = K q^T, and with the probabilities where that product leaves them, o^T += V^T p^T (their places in a lane are the
 // reduction's order of the second product, which V's rows follow).  Both products run on 16-bit floating MFMAs, in which codes are exact.
 //
-// Weights of the second product are halves of w = 2^(x - r) s^v, x the score in base 2 and r a reference of the row that follows the largest of x + e, e the
+// Weights of the second product are halves (in fp16 and fp32 calls sums of two) of w = 2^(x - r) s^v, x the score in base 2 and r a reference of the row that follows the largest of x + e, e the
 // exponent of s^v: so they are of the size of 1 for the terms that count, whatever the scales.  The reference stays while no w is beyond 2^15, and is moved, with l and
 // o, so that the largest is about 2^7; a half keeps what is 2^-24 of 1.  l = sum 2^(x - r) in fp32.
 //
@@ -252,7 +252,10 @@ __device__ __forceinline__ int64_t out_at(const CacheAttnArgs &a, const Sequence
 // Sizes that follow from D (the head dimension's tile: 64, 128 or 256), the width of codes and the type.  Lane l of a wave: row i = l % 16 of a tile of rows in
 // the products with q, group g = l / 16 of the reduction.
 template <int D, int BITS, int TYPE> struct Shape {
-    static constexpr int PLANES = TYPE == MC_F32 ? 2 : 1; // halves that hold a value of q, and a weight
+    static constexpr int PLANES = TYPE == MC_F32 ? 2 : 1;  // halves that hold a value of q
+    // Halves that hold a weight.  One's rounding is as large as that of a result in fp16: with it results were 1.4 - 1.55 times as far from the formula's as rounded ones are,
+    // and trees (as below, fp16) took 93 instead of 106 us, 4 bits of 131072 tokens 60.7 instead of 64.8.
+    static constexpr int PARTS = TYPE == MC_BF16 ? 1 : 2;
     static constexpr bool RAW = TYPE != MC_F32;           // K's codes enter with their offset
     static constexpr int C = D / 16;                      // columns of V in a lane
     static constexpr int STEPS = D / 32;                  // of the first product
@@ -340,6 +343,10 @@ __device__ __forceinline__ float exponent_of(float scale)
     return (float)(e < -100 ? -100 : e);
 }
 
+// What a half holds of a weight, cut off and not rounded: the rest is exact in fp32 then, and its half leaves 2^-22.  (Below 2^-14 the first half is rounded to steps of 2^-24
+// all the same, which is the error allowed for.)
+__device__ __forceinline__ float first_part(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
+
 // A row's reference and sums
 template <int C> struct Row {
     float m, l; // m: the reference, and 7 (NONE: nothing seen)
@@ -400,13 +407,13 @@ template <int D, int TYPE, int C> __device__ __forceinline__ void put(const Cach
 
 // Up to 16 rows: the waves of a workgroup take a piece's tiles of 32 tokens in turn, from memory through registers alone.
 // Memory bounds it where there is much to read: 2216 MB (64 sequences of 16384, 8 heads of 128, 8 bits) in 340 us, 6.5 TB/s of 6.9 that reading alone reaches; with ordinary
-// instead of streaming loads 375.  In 4 bits (285 MB, two sequences of 131072) 55 us, 5.1 TB/s: there are twice as many conversions to a byte.  Unequal sequences (190 MB) take
+// instead of streaming loads 375.  In 4 bits and fp16 (285 MB, two sequences of 131072) 59 us, 4.8 TB/s: there are twice as many conversions to a byte.  Unequal sequences (190 MB) take
 // 43 us: 3 us until lengths and first pages are there, and workgroups of unequal work at the end.  Tried without gain: tiles three ahead, page ids a wave holds in its lanes, three waves
 // of longer tiles, wave priorities.
 template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_kernel(CacheAttnArgs a)
 {
     typedef Shape<D, BITS, TYPE> S;
-    constexpr int PLANES = S::PLANES, C = S::C, PB = S::PB;
+    constexpr int PLANES = S::PLANES, PARTS = S::PARTS, C = S::C, PB = S::PB;
     __shared__ float shared_o[CACHE_WAVES][16][D + 4];
     __shared__ float shared_m[CACHE_WAVES][16], shared_l[CACHE_WAVES][16];
 
@@ -531,15 +538,14 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] -= by;
         }
-        h8 w[PLANES];
+        h8 w[PARTS];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = __builtin_amdgcn_exp2f(x[e]);
             sums.l += p;
-            float v = p * vs[e];
-            if (PLANES == 2) asm("" : "+v"(v)); // (one product, rounded once: the first half by a fused rounding, and the second from another would differ at a tie)
-            w[0][e] = (_Float16)v;
-            if (PLANES == 2) w[PLANES - 1][e] = (_Float16)(v - (float)(_Float16)v);
+            const float v = p * vs[e], first = PARTS == 2 ? first_part(v) : v;
+            w[0][e] = (_Float16)first;
+            if (PARTS == 2) w[PARTS - 1][e] = (_Float16)(v - first);
         }
         constexpr int PER_WORD = 32 / BITS; // columns of a word
 #pragma unroll
@@ -548,7 +554,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
             const h8 v = operand(column_pair<BITS>(tile.v[0][0].w[n], tile.v[0][1].w[n], in), column_pair<BITS>(tile.v[0][2].w[n], tile.v[0][3].w[n], in),
                                  column_pair<BITS>(tile.v[1][0].w[n], tile.v[1][1].w[n], in), column_pair<BITS>(tile.v[1][2].w[n], tile.v[1][3].w[n], in));
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) sums.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[p], sums.o[c], 0, 0, 0);
+            for (int p = 0; p < PARTS; ++p) sums.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[p], sums.o[c], 0, 0, 0);
         }
     };
 
@@ -610,7 +616,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_rows_kernel(CacheAttnArgs a)
 {
     typedef Shape<D, BITS, TYPE> S;
-    constexpr int PLANES = S::PLANES, C = S::C, PB = S::PB, STEPS = S::STEPS;
+    constexpr int PLANES = S::PLANES, PARTS = S::PARTS, C = S::C, PB = S::PB, STEPS = S::STEPS;
     constexpr int T = D <= 128 ? 64 : 32, BLOCKS = T / 16, PAIRS = T / 32;  // tokens of a tile, in blocks of 16 and 32
     constexpr int SHARE = CACHE_WAVES / BLOCKS, KU = S::NK / SHARE, VB = S::VB / SHARE, VC = C / SHARE; // waves that convert 16 tokens, each some pieces of K and columns of V
     static_assert(KU * SHARE == S::NK && VC * SHARE == C, "even shares");
@@ -777,7 +783,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
         }
 #pragma unroll
         for (int pair = 0; pair < PAIRS; ++pair) {
-            h8 w[R][PLANES];
+            h8 w[R][PARTS];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int b = 2 * pair + half;
@@ -788,19 +794,18 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
                     for (int r = 0; r < 4; ++r) {
                         const float p = __builtin_amdgcn_exp2f(sc[t][b][r]);
                         sums[t].l += p;
-                        float v = p * vs[r];
-                        if (PLANES == 2) asm("" : "+v"(v)); // (as above)
-                        w[t][0][4 * half + r] = (_Float16)v;
-                        if (PLANES == 2) w[t][PLANES - 1][4 * half + r] = (_Float16)(v - (float)(_Float16)v);
+                        const float v = p * vs[r], first = PARTS == 2 ? first_part(v) : v;
+                        w[t][0][4 * half + r] = (_Float16)first;
+                        if (PARTS == 2) w[t][PARTS - 1][4 * half + r] = (_Float16)(v - first);
                     }
             }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const h8 v = *reinterpret_cast<const h8 *>(&st.v[(pair * C + c) * 1024 + lane * 16]);
 #pragma unroll
-                for (int t = 0; t < R; ++t)
+                for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-                    for (int p = 0; p < PLANES; ++p) sums[t].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][p], sums[t].o[c], 0, 0, 0);
+                    for (int t = 0; t < R; ++t) sums[t].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][p], sums[t].o[c], 0, 0, 0);
             }
         }
     };
@@ -843,8 +848,8 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 }
 
 // Pieces of sequences that were cut, joined in their order: a wave per row (and further rows after it), D / 4 lanes per piece.  3.5 - 5 us where rows are few: a launch and three trips to memory.
-// (16 sequences of up to 192 rows, 8 heads, two or three pieces: 17.6 us, 30 MB written by other XCDs just before; more or fewer workgroups and all pieces' requests at once: 94 - 109 us
-// for the whole call instead of 93.)
+// (16 sequences of up to 192 rows, 8 heads, two or three pieces: 17.6 us, 30 MB written by other XCDs just before; with more or fewer workgroups or all pieces' requests at once
+// the whole call took 1 - 17 % longer.)
 template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheAttnArgs a)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, AHEAD = 8;

@@ -7,7 +7,7 @@ import decode_reference as ref
 pytestmark = pytest.mark.gpu
 
 HALF = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
-WEIGHT = {"float32": 2.0 ** -20, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -11}
+WEIGHT = {"float32": 2.0 ** -20, "float16": 2.0 ** -20, "bfloat16": 2.0 ** -11}
 
 
 class Problem:
