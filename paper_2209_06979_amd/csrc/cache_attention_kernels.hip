@@ -343,8 +343,8 @@ __device__ __forceinline__ float exponent_of(float scale)
     return (float)(e < -100 ? -100 : e);
 }
 
-// What a half holds of a weight, cut off and not rounded: the rest is exact in fp32 then, and its half leaves 2^-22.  (Below 2^-14 the first half is rounded to steps of 2^-24
-// all the same, which is the error allowed for.)
+// What a half holds of a weight, cut off and not rounded: the rest is exact in fp32 then, and its half leaves 2^-22.  (Below 2^-14 both are rounded to steps of 2^-24: 2^-24
+// in all, 2^-31 of a row's largest.)
 __device__ __forceinline__ float first_part(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
 
 // A row's reference and sums

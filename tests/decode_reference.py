@@ -47,8 +47,8 @@ def attention(q, kc, vc, ks, vs, table, lengths, starts, tree=None, scale=None, 
       A (e^(2 d) - 1)     scores off by d: q c is summed over dk elements in fp32 (dk + 8 roundings of the sum of |q c|, 2^-24 each), and
                           q is held to 2^-22 of the row's largest at worst
       (keys + 16) 2^-23 A sums over the keys, the exponentials and the rescalings
-      2^-30 w sum |c|     weights are halves times a power of two such that the row's largest p 2^e, e the exponent of V's scale, lies between 2^7 and 2^15 (it is
-                          brought to 2^7 when it is beyond 2^15).  A half's step is never below 2^-24, so a weight is off by up to 2^-25, 2^-32 of that
+      2^-29 w sum |c|     weights are halves, or sums of two, times a power of two such that the row's largest p 2^e, e the exponent of V's scale, lies between 2^7 and 2^15 (it is
+                          brought to 2^7 when it is beyond 2^15).  A half's step is never below 2^-24, so each of up to two halves is off by up to 2^-25, a weight by 2^-31 of that
                           largest, and p 2^e is up to four times w, the largest p times scale: of one token (own_exponents), or, where several tokens share the
                           exponent of their largest scale, of any two of them
     """
@@ -88,5 +88,5 @@ def attention(q, kc, vc, ks, vs, table, lengths, starts, tree=None, scale=None, 
                 d = (((np.abs(kcode) @ np.abs(row)) * (dk + 8) * 2.0 ** -24 + np.abs(kcode).sum(1) * np.abs(row).max() * 2.0 ** -22) * k_s * abs(scale)).max()
                 out[s0 + i, h] = o
                 largest = (p * np.abs(v_s)).max() if own_exponents else p.max() * np.abs(v_s).max()
-                tol[s0 + i, h] = 2.0 ** -30 * largest * np.abs(vcode).sum(0) + half_step * np.abs(o) + spread * (weight_step + np.expm1(2 * d) + (len(at) + 16) * 2.0 ** -23) + 1e-30
+                tol[s0 + i, h] = 2.0 ** -29 * largest * np.abs(vcode).sum(0) + half_step * np.abs(o) + spread * (weight_step + np.expm1(2 * d) + (len(at) + 16) * 2.0 ** -23) + 1e-30
     return out, tol
