@@ -83,6 +83,14 @@ def test_chunks_of_unequal_lengths(dtype, bits):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("page", [16, 32, 128, 4096])
+@pytest.mark.parametrize("bits,dk", [(8, 128), (4, 128), (8, 256)])
+def test_chunks_on_pages_of_other_sizes(page, bits, dk):
+    """More than 64 rows, whose tokens are converted 64 (32) at a time: pages shorter, as long and longer than that, the largest among them."""
+    p = Problem([0, 70, 333], [33, 5, 40], kv_heads=2, group=3, dk=dk, bits=bits, page=page, dtype="bfloat16", seed=page, spare=1)
+    p.check(p.run())
+
+
 def _tree(rng, n):
     bits = []
     for i in range(n):
