@@ -4,7 +4,7 @@
 // registers: S^T = K q^T, and with the probabilities where that product leaves them, o^T += V^T p^T (their places in a lane are the
 // reduction's order of the second product, which V's rows follow).  Both products run on 16-bit floating MFMAs, in which codes are exact.
 //
-// Weights of the second product are halves (in fp16 and fp32 calls sums of two) of w = 2^(x - r) s^v, x the score in base 2 and r a reference of the row that follows the largest of x + e, e the
+// Weights of the second product are sums of two halves of w = 2^(x - r) s^v, x the score in base 2 and r a reference of the row that follows the largest of x + e, e the
 // exponent of s^v: so they are of the size of 1 for the terms that count, whatever the scales.  The reference stays while no w is beyond 2^15, and is moved, with l and
 // o, so that the largest is about 2^7; a half keeps what is 2^-24 of 1.  l = sum 2^(x - r) in fp32.
 //
@@ -253,9 +253,9 @@ __device__ __forceinline__ int64_t out_at(const CacheAttnArgs &a, const Sequence
 // the products with q, group g = l / 16 of the reduction.
 template <int D, int BITS, int TYPE> struct Shape {
     static constexpr int PLANES = TYPE == MC_F32 ? 2 : 1;  // halves that hold a value of q
-    // Halves that hold a weight.  One's rounding is as large as that of a result in fp16: with it results were 1.4 - 1.55 times as far from the formula's as rounded ones are,
-    // and trees (as below, fp16) took 93 instead of 106 us, 4 bits of 131072 tokens 60.7 instead of 64.8.
-    static constexpr int PARTS = TYPE == MC_BF16 ? 1 : 2;
+    // Halves that hold a weight, for every type.  With one, results in fp16 were 1.4 - 1.55 times as far from the formula's as rounded ones are, and every eighth of those in bf16 was
+    // not the rounded one (values that cancel lost up to 2^-12 of what they are summed from).
+    static constexpr int PARTS = 2;
     static constexpr bool RAW = TYPE != MC_F32;           // K's codes enter with their offset
     static constexpr int C = D / 16;                      // columns of V in a lane
     static constexpr int STEPS = D / 32;                  // of the first product
@@ -343,9 +343,16 @@ __device__ __forceinline__ float exponent_of(float scale)
     return (float)(e < -100 ? -100 : e);
 }
 
-// What a half holds of a weight, cut off and not rounded: the rest is exact in fp32 then, and its half leaves 2^-22.  (Below 2^-14 both are rounded to steps of 2^-24: 2^-24
-// in all, 2^-31 of a row's largest.)
-__device__ __forceinline__ float first_part(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
+// Two weights as sums of two halves each: what a half holds, cut off and not rounded, and the rest, which is exact in fp32 and whose half leaves 2^-22.  (Both are
+// rounded to steps of 2^-24 where they are small: 2^-25 in the end, 2^-32 of a row's largest.)
+__device__ __forceinline__ void put_parts(h8 (&w)[2], int e, float v0, float v1)
+{
+    const h2 first = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+    w[0][e] = first[0];
+    w[0][e + 1] = first[1];
+    w[1][e] = (_Float16)__builtin_fmaf((float)first[0], -1.f, v0);
+    w[1][e + 1] = (_Float16)__builtin_fmaf((float)first[1], -1.f, v1);
+}
 
 // A row's reference and sums
 template <int C> struct Row {
@@ -517,8 +524,7 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? x[e] : NONE;
         }
-        // The largest weight: by each token's exponent, or (one half to a weight) by that of the largest scale of a lane's eight, whose others keep their 11 bits
-        // while they are within 2^20 of it.
+        // The largest weight: by each token's exponent (fp32), or by that of the largest scale of a lane's eight.
         float top, most = fabsf(vs[0]);
         if (PLANES == 2) {
             top = x[0] + exponent_of(vs[0]);
@@ -540,12 +546,11 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
         }
         h8 w[PARTS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[e]);
-            sums.l += p;
-            const float v = p * vs[e], first = PARTS == 2 ? first_part(v) : v;
-            w[0][e] = (_Float16)first;
-            if (PARTS == 2) w[PARTS - 1][e] = (_Float16)(v - first);
+        for (int e = 0; e < 8; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(x[e]), p1 = __builtin_amdgcn_exp2f(x[e + 1]);
+            sums.l += p0;
+            sums.l += p1;
+            put_parts(w, e, p0 * vs[e], p1 * vs[e + 1]);
         }
         constexpr int PER_WORD = 32 / BITS; // columns of a word
 #pragma unroll
@@ -791,12 +796,11 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 #pragma unroll
                 for (int t = 0; t < R; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(sc[t][b][r]);
-                        sums[t].l += p;
-                        const float v = p * vs[r], first = PARTS == 2 ? first_part(v) : v;
-                        w[t][0][4 * half + r] = (_Float16)first;
-                        if (PARTS == 2) w[t][PARTS - 1][4 * half + r] = (_Float16)(v - first);
+                    for (int r = 0; r < 4; r += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(sc[t][b][r]), p1 = __builtin_amdgcn_exp2f(sc[t][b][r + 1]);
+                        sums[t].l += p0;
+                        sums[t].l += p1;
+                        put_parts(w[t], 4 * half + r, p0 * vs[r], p1 * vs[r + 1]);
                     }
             }
 #pragma unroll
