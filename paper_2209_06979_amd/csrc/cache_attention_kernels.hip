@@ -336,11 +336,11 @@ __device__ __forceinline__ int64_t place_of(const CacheAttnArgs &a, int page, in
     return (int64_t)((uint64_t)(is_page(a, page) ? (unsigned)page : 0u) * a.page_vectors + ((unsigned)head << a.page_shift) + ((unsigned)at & ((1u << a.page_shift) - 1)));
 }
 
-// The exponent of a scale: |scale| is below 2^exponent.  (At least -100: 2^(x - r) stays a number of fp32.)
+// The exponent of a scale: |scale| is below 2^exponent; at least -80, so that 2^(x - r) is at most 2^95 and 2^30 tokens' sum of it a number of fp32.  Zero has that lowest
+// exponent, too: a value of zeros counts in l and must not raise the reference above the weights that are there.
 __device__ __forceinline__ float exponent_of(float scale)
 {
-    const int e = __builtin_amdgcn_frexp_expf(scale);
-    return (float)(e < -100 ? -100 : e);
+    return (float)__builtin_amdgcn_frexp_expf(fmaxf(fabsf(scale), 0x1p-81f));
 }
 
 // Two weights as sums of two halves each: what a half holds, cut off and not rounded, and the rest, which is exact in fp32 and whose half leaves 2^-22.  (Both are
