@@ -584,7 +584,8 @@ typedef struct mc_rope_keys {
 
 /* Quantises keys and values into the cache: for every vector of dk elements
  *   scale = fp32(max |x| / qmax),  code = clamp(rint(x / scale), -qmax, qmax), ties to even, decided as in double precision; qmax = 127 or 7.
- * A vector of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has scale NaN and codes 0, so that it reads back as NaN.
+ * A vector of zeros has scale 0 and codes 0; one that holds an infinity or a NaN, or whose scale is beyond fp32 (a rotated key's can be), has scale NaN and codes 0, so that it
+ * reads back as NaN.
  *   k_dev, v_dev   tokens x kv_heads x dk, 16-byte aligned, strides whole 16-byte pieces
  *   slots_dev      tokens int64; a token whose slot is negative or beyond the cache is written nowhere (padding).  Other slots must differ: of
  *                  two tokens with one slot, each element of either may remain

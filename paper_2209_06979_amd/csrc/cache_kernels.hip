@@ -93,8 +93,7 @@ template <class REAL, int BITS, int LANES> __device__ __forceinline__ float code
     if (!finite) m = (REAL)__builtin_inf();
     if (!there) m = 0;
     m = max_of_lanes<LANES>(m);
-    const bool all_finite = m < (REAL)__builtin_inf();
-    const float scale = all_finite ? scale_of(m, (float)QMAX) : __builtin_nanf("");
+    const float ratio = scale_of(m, (float)QMAX), scale = ratio < __builtin_inff() ? ratio : __builtin_nanf(""); // (rotated keys can have finite maxima whose ratio is not)
     w[0] = w[1] = 0;
     auto put = [&](int e, unsigned code) {
         if (BITS == 8) w[e / 4] |= (code & 255u) << (8 * (e % 4));
@@ -110,7 +109,7 @@ template <class REAL, int BITS, int LANES> __device__ __forceinline__ float code
             code[e] = __builtin_bit_cast(unsigned, up);
             off = __builtin_fmaxf(off, __builtin_fabsf(r - (up - MAGIC)));
         }
-        if (off > 0.4999f) {
+        if (off > 0.4999f || m > (REAL)__FLT_MAX__) { // (a rotated key beyond fp32 has no fp32 quotient)
 #pragma unroll
             for (int e = 0; e < E; ++e) code[e] = (unsigned)(int)__builtin_rint((double)v[e] / (double)scale);
         }
