@@ -614,7 +614,7 @@ int mc_cache_read(const mc_cache *cache, const int64_t *slots_dev, int64_t token
  * Softmax over score_scale * (q . k), score_scale finite.  A row that sees nothing is zero; keys and values that a row does not see (an infinity or a NaN
  * among them) do not change it.  fp32 accumulation.  A weight, the probability times the value's scale, is off by at most
  * 2^-21 of itself or 2^-30 of the row's largest, whichever is more (tokens 4 or 8 at a time count with the largest of their scales here, scales below 2^-80 with 2^-80).  A key's or a value's scale that is no
- * number, or infinite, makes the rows that see it NaN or infinite.  Results do not
+ * number, or infinite, makes the rows that see it NaN.  Results do not
  * depend on what else is in the batch beyond the order of fp32 sums and of these roundings, and are the same from call to call.
  * The workspace (256-byte aligned, contents undefined before and after; calls that may overlap in time need one each) holds what pieces of long sequences
  * leave for each other.  mc_cache_attention_workspace gives the bytes for these sizes; 0 means that none is needed and NULL will do. */

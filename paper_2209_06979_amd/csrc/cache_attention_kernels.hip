@@ -518,7 +518,8 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float score = S::RAW ? __builtin_fmaf(sc[e / 4][e % 4], row_scale.scale, row_scale.offset) : sc[e / 4][e % 4] * row_scale.scale;
-            x[e] = __builtin_fmaf(score, tile.ks[e / 4][e % 4], to_add);
+            const float ks = tile.ks[e / 4][e % 4];
+            x[e] = __builtin_fmaf(score, ks, __builtin_fmaf(ks, 0.f, to_add)); // (NaN, and not -infinity, where a scale is infinite)
         }
         if (masked) {
 #pragma unroll
@@ -706,14 +707,14 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
                 make_uint2(column_pair<BITS>(t.v[0].w[n], t.v[1].w[n], in), column_pair<BITS>(t.v[2].w[n], t.v[3].w[n], in));
         }
         if (share == 0) {
-            // a scale of V that is not finite goes into the scores, from where it reaches the rows that see the token and no other
+            // scales that are not finite, V's too, go into the scores as NaN, from where they reach the rows that see the token and no other
             const bool finite = fabsf(t.v_scale) < __builtin_inff();
             const float v = finite ? t.v_scale : 0.f;
             float most = fabsf(v);
             most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0xB1, 0xF, 0xF, true))); // quad_perm 1 0 3 2
             most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0x4E, 0xF, 0xF, true))); // quad_perm 2 3 0 1
             if (g == 0) {
-                to.k_scale[16 * block + i] = finite ? t.k_scale : __builtin_nanf("");
+                to.k_scale[16 * block + i] = finite && fabsf(t.k_scale) < __builtin_inff() ? t.k_scale : __builtin_nanf("");
                 to.v_scale[16 * block + i] = v;
                 to.exponent[4 * block + i / 4] = exponent_of(most);
                 to.there[block] = (uint8_t)t.there;
