@@ -268,7 +268,8 @@ template <int D, int BITS, int TYPE> struct Shape {
     }
 };
 
-// A lane's row of q as operands of the first product, times a power of two that brings the row's largest into [1, 2); a score is sum * scale + offset then
+// A lane's row of q as operands of the first product, times a power of two that brings the row's largest into [2^14, 2^15), so that halves hold what is 2^-28 of it to their full
+// width (a nibble higher up: 2^-24); a score is sum * scale + offset then
 struct RowScale { float scale, offset; };
 template <class S, int BITS, int TYPE> __device__ __forceinline__ RowScale load_q(const CacheAttnArgs &a, int64_t at, int g, h8 (&q)[S::PLANES][S::STEPS])
 {
@@ -284,7 +285,7 @@ template <class S, int BITS, int TYPE> __device__ __forceinline__ RowScale load_
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[st][e]));
     }
     top = max_of_groups(top);
-    const int up = top > 0 && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
+    const int up = top > 0 && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
     float sum = 0;
 #pragma unroll
     for (int st = 0; st < S::STEPS; ++st)
