@@ -93,7 +93,7 @@ inline CacheAttnPlan cache_attention_plan(int kv_heads, int dk, int group, int b
     p.row_tiles = (p.rows + p.row_tile - 1) / p.row_tile;
     const int64_t sharers = (int64_t)kv_heads * (p.row_tiles > 0 ? p.row_tiles : 1);
     p.pieces = (int)(CACHE_PIECES / sharers > 1 ? CACHE_PIECES / sharers : 1);
-    p.cut = tiles > CACHE_MIN_PIECE && p.row_tiles > 0 && batch > 0;
+    p.cut = tiles > CACHE_MIN_PIECE && p.pieces > 1 && p.row_tiles > 0 && batch > 0; // (one piece to a head and tile of rows: all tokens together)
     // sequences that are cut have more than one piece, fewer than twice the pieces their share asks for; and every sequence adds one
     // that is not full
     p.slots = p.cut ? (2 * (int64_t)p.pieces < (int64_t)p.pieces + batch ? 2 * (int64_t)p.pieces : (int64_t)p.pieces + batch) : 0;
