@@ -374,6 +374,24 @@ class KVCache(_native.Cache):
         return cls(*codes, *(torch.zeros(shape, dtype=torch.float32, device=device) for _ in "kv"), bits=bits)
 
 
+class _RopeNode(torch.autograd.Function):
+    """rope of a tensor that requires grad: the gradient is the rotation by the angles reversed."""
+
+    @staticmethod
+    def forward(ctx, x, positions, inv_freq, interleaved, magnitude, inverse):
+        ctx.save_for_backward(positions, inv_freq)
+        ctx.turn = interleaved, magnitude, inverse
+        return rope(x, positions, inv_freq, interleaved, magnitude, inverse)
+
+    @staticmethod
+    def backward(ctx, dy):
+        interleaved, magnitude, inverse = ctx.turn
+        dx = rope(dy if dy.stride(-1) == 1 else dy.contiguous(), *ctx.saved_tensors, interleaved, magnitude, not inverse)
+        return dx, None, None, None, None, None
+
+
+_native._set_rope_node(_RopeNode.apply)
+
 ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 

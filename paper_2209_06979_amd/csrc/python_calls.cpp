@@ -13,6 +13,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/GradMode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -26,6 +27,7 @@
 namespace {
 
 PyObject *g_error_class = nullptr; // binding.MagicubeError
+PyObject *g_rope_node = nullptr;   // binding's autograd node of rope
 
 // ---- Matrix: the native part of binding.SparseMatrix -------------------------------------------------
 struct Matrix {
@@ -756,6 +758,18 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
         if (!(out = tensor(v[6]))) return nullptr;
         if (!(token_major(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->sizes() == x->sizes())) return assertion();
     }
+    if (c10::GradMode::is_enabled()) { // gradients are recorded, or the call is refused: never dropped
+        if (freq->requires_grad()) {
+            PyErr_SetString(PyExc_RuntimeError, "rope: inv_freq requires grad, for which there is no gradient");
+            return nullptr;
+        }
+        if (out && (x->requires_grad() || out->requires_grad())) {
+            PyErr_SetString(PyExc_RuntimeError, "rope: out= does not record gradients, and one of the tensors requires grad");
+            return nullptr;
+        }
+        if (x->requires_grad())
+            return PyObject_CallFunction(g_rope_node, "OOOOdO", v[0], v[1], v[2], interleaved ? Py_True : Py_False, (double)magnitude, inverse ? Py_True : Py_False);
+    }
     at::TensorBase made;
     int rc;
     {
@@ -939,9 +953,17 @@ PyObject *set_error_class(PyObject *, PyObject *cls)
     Py_RETURN_NONE;
 }
 
+PyObject *set_rope_node(PyObject *, PyObject *apply)
+{
+    Py_INCREF(apply);
+    Py_XSETREF(g_rope_node, apply);
+    Py_RETURN_NONE;
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL | METH_KEYWORDS
 PyMethodDef functions[] = {
     {"_set_error_class", set_error_class, METH_O, "the exception raised for a status of the library"},
+    {"_set_rope_node", set_rope_node, METH_O, "what rope calls for a tensor that requires grad: (x, positions, inv_freq, interleaved, magnitude, inverse)"},
     {"spmm", FAST(spmm),
      "spmm(A, B, prec, out=None, lhs_unsigned=False, rhs_unsigned=False, options=None)\n--\n\n"
      "C = A * B (int32, M x N).  B: device tensor (K, N) int8, (K, N/2) uint8 for R4, (K, N) int16 for R16.\n"
@@ -990,7 +1012,8 @@ PyMethodDef functions[] = {
      "rope(x, positions, inv_freq, interleaved=False, magnitude=1.0, inverse=False, out=None)\n--\n\n"
      "Rotary positions: x (tokens, heads, dim) fp32, fp16 or bf16 with any strides, positions (tokens,) int64, inv_freq (rot/2,) float64\n"
      "(see rope_frequencies).  Pairs (j, j + rot/2), or (2j, 2j + 1) if interleaved; elements from rot on are copied.  out may be x.\n"
-     "inverse: the angles reversed, which makes the call the gradient (no autograd node is recorded)."},
+     "inverse: the angles reversed, which makes the call the gradient.  Autograd records it where x requires grad (out must be None then;\n"
+     "there is no gradient for inv_freq)."},
     {"cache_write", FAST(cache_write),
      "cache_write(cache, k, v, slots, positions=None, inv_freq=None, interleaved=False, magnitude=1.0)\n--\n\n"
      "Quantises k and v (tokens, kv_heads, dk; fp32, fp16 or bf16) into the cache, one scale per vector; slots (tokens,) int64 = page *\n"
@@ -1004,7 +1027,8 @@ PyMethodDef functions[] = {
      "Attention of new tokens over the cache that holds their keys and values already.  q: (total new tokens, heads, dk); page_table\n"
      "(batch, pages) int32; lengths (batch,) int32, the new tokens included.  starts (batch + 1,) int32: the rows of each sequence, at most\n"
      "max_new each (None: the same number for all).  tree (total,) int64: bit j of a row lets it see the sequence's new token j (None: all\n"
-     "up to itself).  scale: None is 1 / sqrt(dk).  See mc_cache_attention in magicube.h for what out-of-range values do."},
+     "up to itself).  scale: None is 1 / sqrt(dk).  See mc_cache_attention in magicube.h for what out-of-range values do.  Rows of no\n"
+     "sequence stay as `out` has them, and have no defined value without it.  For inference: no gradient is recorded."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};
