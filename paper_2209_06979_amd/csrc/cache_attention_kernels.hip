@@ -65,19 +65,6 @@ __device__ __forceinline__ Sequence sequence(const CacheAttnArgs &a, int b)
     return s;
 }
 __device__ __forceinline__ int tiles_of(const Sequence &s) { return s.n == 0 ? 0 : s.length <= 0 ? 1 : (s.length - 1) / CACHE_TILE + 1; }
-// Tiles that a piece should have, for this many tiles in all
-__device__ __forceinline__ int piece_tiles(const CacheAttnArgs &a, int total)
-{
-    const int t = (total + a.pieces - 1) / a.pieces;
-    return t < CACHE_MIN_PIECE ? CACHE_MIN_PIECE : t;
-}
-// Pieces of a sequence: one while it has up to a quarter more than that (a remnant costs more than it relieves the others of)
-__device__ __forceinline__ int pieces_of(int tiles, int each)
-{
-    if (tiles == 0) return 0;
-    const int n = (tiles - 1 + each - each / 4) / each;
-    return n < 1 ? 1 : n;
-}
 
 __device__ __forceinline__ int scan(int v) // inclusive, over the wave: within rows of 16 lanes, then their last lanes' sums into the rows behind
 {
@@ -105,12 +92,12 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
         total = at_lane(scan(t), 63);
         for (int b = 64; b < a.batch; b += 64) total += at_lane(scan(tiles_of(b + lane < a.batch ? sequence(a, b + lane) : none)), 63);
     }
-    int each = a.partial ? piece_tiles(a, total) : 0x40000000;
-    if (a.partial && a.batch <= 64 && a.batch < a.pieces) { // (the whole pieces are more than asked for: longer ones, until they run at once)
-        for (int i = 0; i < 6; ++i) {
-            const int n = at_lane(scan(pieces_of(t, each)), 63);
+    int each = a.partial ? cache_piece_tiles(total, a.pieces) : CACHE_WHOLE;
+    if (a.partial && cache_pieces_lengthened(a.batch, a.pieces)) {
+        for (int i = 0; i < CACHE_LENGTHENINGS; ++i) {
+            const int n = at_lane(scan(cache_pieces_of(t, each)), 63);
             if (n <= a.pieces) break;
-            each += (int)((int64_t)each * (n - a.pieces) / (2 * a.pieces)) + 1;
+            each = cache_longer_piece(each, n, a.pieces);
         }
     }
     Cut c = {-1, 0, 0, 0, 0, none};
@@ -120,15 +107,14 @@ template <bool BY_PIECE> __device__ __forceinline__ Cut cut_of(const CacheAttnAr
             s = b + lane < a.batch ? sequence(a, b + lane) : none;
             t = tiles_of(s);
         }
-        const int pieces = pieces_of(t, each), up_to = scan(pieces), cut_up_to = scan(pieces > 1 ? pieces : 0);
+        const int pieces = cache_pieces_of(t, each), up_to = scan(pieces), cut_up_to = scan(pieces > 1 ? pieces : 0);
         const bool here = BY_PIECE ? before + up_to - pieces <= number && number < before + up_to : b + lane == number;
         const unsigned long long who = __ballot(here);
         if (who) {
             const int l = __builtin_ctzll(who);
             c.b = b + l;
             c.pieces = at_lane(pieces, l);
-            // equal pieces, but for whole rounds of the waves
-            c.each = (at_lane(t, l) + c.pieces * CACHE_WAVES - 1) / (c.pieces * CACHE_WAVES) * CACHE_WAVES;
+            c.each = cache_each_of(at_lane(t, l), c.pieces);
             c.slot = slots + at_lane(cut_up_to, l) - (c.pieces > 1 ? c.pieces : 0);
             c.index = number - before - at_lane(up_to, l) + c.pieces;
             c.of = {at_lane(s.start, l), at_lane(s.n, l), at_lane(s.length, l), at_lane(s.held, l)};

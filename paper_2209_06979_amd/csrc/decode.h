@@ -100,3 +100,26 @@ inline CacheAttnPlan cache_attention_plan(int kv_heads, int dk, int group, int b
     p.lines = p.slots * kv_heads * p.rows;
     return p;
 }
+
+// How sequences are cut, for both sides: the kernels follow these from the lengths, and the plan above has to hold what comes of it.
+#define CACHE_RULE __host__ __device__ __forceinline__
+constexpr int CACHE_WHOLE = 0x40000000; // tiles of a piece where nothing is cut
+// Tiles that a piece should have, for this many tiles in all
+CACHE_RULE int cache_piece_tiles(int total, int pieces)
+{
+    const int t = (total + pieces - 1) / pieces;
+    return t < CACHE_MIN_PIECE ? CACHE_MIN_PIECE : t;
+}
+// Pieces of a sequence: one while it has up to a quarter more than that (a remnant costs more than it relieves the others of)
+CACHE_RULE int cache_pieces_of(int tiles, int each)
+{
+    if (tiles == 0) return 0;
+    const int n = (tiles - 1 + each - each / 4) / each;
+    return n < 1 ? 1 : n;
+}
+// Where the sequences' pieces are more than asked for: longer ones, some times at most, until they run at once (batches that one wave looks over)
+constexpr int CACHE_LENGTHENINGS = 6;
+CACHE_RULE bool cache_pieces_lengthened(int batch, int pieces) { return batch <= 64 && batch < pieces; }
+CACHE_RULE int cache_longer_piece(int each, int n, int pieces) { return each + (int)((int64_t)each * (n - pieces) / (2 * pieces)) + 1; }
+// Tiles of each of a sequence's pieces: equal ones, but for whole rounds of the waves
+CACHE_RULE int cache_each_of(int tiles, int pieces) { return (tiles + pieces * CACHE_WAVES - 1) / (pieces * CACHE_WAVES) * CACHE_WAVES; }
