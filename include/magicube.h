@@ -553,8 +553,8 @@ int mc_rope_frequencies(int rot, double base, mc_rope_scaling scaling, double fa
  * it the call is the gradient, dx from dy.  Angles are products in double precision, so far positions keep their phase; the rest is fp32.
  *   x_dev, y_dev        tokens x heads x dim; y_dev may be x_dev with the same strides, else the two must not overlap
  *   positions_dev       tokens int64, any values;  inv_freq_dev  rot / 2 doubles
- * Any alignment; tensors whose pointers, strides and rot / 2 elements make whole 16-byte pieces are faster.  rot even, 0 <= rot <= dim;
- * tokens = 0 is accepted. */
+ * Any alignment; tensors whose pointers, strides and rot / 2 elements make whole 16-byte pieces are faster.  rot even, 0 <= rot <= dim <= 65536, heads at most 65535,
+ * tokens * heads * ceil(dim / 2) at most 2^31 - 256; tokens = 0 is accepted. */
 int mc_rope(const void *x_dev, mc_type type, int64_t tokens, int heads, int dim, int64_t x_token_stride, int64_t x_head_stride,
             const int64_t *positions_dev, const double *inv_freq_dev, int rot, int interleaved, float magnitude, int inverse,
             void *y_dev, int64_t y_token_stride, int64_t y_head_stride, void *stream);
@@ -590,7 +590,7 @@ typedef struct mc_rope_keys {
  *   slots_dev      tokens int64; a token whose slot is negative or beyond the cache is written nowhere (padding).  Other slots must differ: of
  *                  two tokens with one slot, each element of either may remain
  *   rope           NULL: keys as they are
- * All else in the cache stays as it was. */
+ * tokens * kv_heads is at most 33554428, here and in mc_cache_read.  All else in the cache stays as it was. */
 int mc_cache_write(const mc_cache *cache, const void *k_dev, const void *v_dev, mc_type type, int64_t tokens, int64_t k_token_stride,
                    int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots_dev, const mc_rope_keys *rope,
                    void *stream);
@@ -612,9 +612,9 @@ int mc_cache_read(const mc_cache *cache, const int64_t *slots_dev, int64_t token
  *                  token j where bit j of its word is set (its own bit included, or not); max_new <= 64 then
  * batch is at most 65535, max_new * heads / kv_heads at most 262140, and (batch + 512) * kv_heads for each 128 rows of that at most some 8 million.
  * Softmax over score_scale * (q . k), score_scale finite.  A row that sees nothing is zero; keys and values that a row does not see (an infinity or a NaN
- * among them) do not change it.  fp32 accumulation.  A weight, the probability times the value's scale, is off by at most
- * 2^-21 of itself or 2^-30 of the row's largest, whichever is more (tokens 4 or 8 at a time count with the largest of their scales here, scales below 2^-80 with 2^-80).  A key's or a value's scale that is no
- * number, or infinite, makes the rows that see it NaN.  Results do not
+ * among them) do not change it.  fp32 accumulation.  q enters as halves (fp32 tensors: as sums of two, 22 bits), whole for elements down to 2^-24 of their row's largest.  A weight, the
+ * probability times the value's scale, is off by at most 2^-21 of itself or 2^-30 of the row's largest, whichever is more (tokens 4 or 8 at a time count with the largest of their scales
+ * here, scales below 2^-80 with 2^-80).  A key's or a value's scale that is no number, or infinite, makes the rows that see it NaN.  Results do not
  * depend on what else is in the batch beyond the order of fp32 sums and of these roundings, and are the same from call to call.
  * The workspace (256-byte aligned, contents undefined before and after; calls that may overlap in time need one each) holds what pieces of long sequences
  * leave for each other.  mc_cache_attention_workspace gives the bytes for these sizes; 0 means that none is needed and NULL will do. */

@@ -400,9 +400,9 @@ template <int D, int TYPE, int C> __device__ __forceinline__ void put(const Cach
 }
 
 // Up to 16 rows: the waves of a workgroup take a piece's tiles of 32 tokens in turn, from memory through registers alone.
-// Memory bounds it where there is much to read: 2216 MB (64 sequences of 16384, 8 heads of 128, 8 bits) in 340 us, 6.5 TB/s of 6.9 that reading alone reaches; with ordinary
+// Memory bounds it where there is much to read: 2216 MB (64 sequences of 16384, 8 heads of 128, 8 bits) in 341 us, 6.5 TB/s of 6.9 that reading alone reaches; with ordinary
 // instead of streaming loads 375.  In 4 bits and fp16 (285 MB, two sequences of 131072) 59 us, 4.8 TB/s: there are twice as many conversions to a byte.  Unequal sequences (190 MB) take
-// 43 us: 3 us until lengths and first pages are there, and workgroups of unequal work at the end.  Tried without gain: tiles three ahead, page ids a wave holds in its lanes, three waves
+// 44 us: 3 us until lengths and first pages are there, and workgroups of unequal work at the end.  Tried without gain: tiles three ahead, page ids a wave holds in its lanes, three waves
 // of longer tiles, wave priorities.
 template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_kernel(CacheAttnArgs a)
 {
@@ -602,10 +602,12 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 
 // More rows: each wave has R tiles of 16 rows, and the workgroup converts a piece's tokens, 64 at a time (32 for D = 256), once for all of them.  The operands lie in LDS as
 // the MFMAs take them, 16 bytes a lane side by side, two tiles of tokens in turn; beside them their scales.
-// What bounds it is the issue of what is not a matrix product: 4 sequences of 512 new tokens over 4096, 32 heads of 128, 133 Gflop in 205 us (650 Tflop/s; a library's bf16 product of 8192^3 reaches 1216), the
-// matrix unit busy 25 % and the vector unit 51 % of the cycles, LDS conflicts 3 %.  Of 314 vector instructions a wave and tile (R = 2), 82 convert, 74 make scores, 46 find the largest weight, and 112,
-// 32 of them exponentials at a quarter of the rate, make weights.  Codes that each wave converted for itself took 595 us.  Tried without gain: weights made first and the largest sought only
-// where they do not fit (registers spill: 527 - 710 us), weights by one mixed multiply-add (212), wave priorities, 32 tokens at a time.
+// What bounds it is the issue of what is not a matrix product: 4 sequences of 512 new tokens over 4096, 32 heads of 128, bf16, 133 Gflop in 250 us (530 Tflop/s; a library's bf16 product of 8192^3 reaches
+// 1200), the vector unit busy 50 % of the cycles and the matrix unit 31 %, a third of it with the weights' second halves (one half: 205 us), LDS conflicts 3 %.  A wave and tile (R = 2) counts 96 matrix and
+// 446 other vector instructions: in the loop 82 convert, 74 make scores, 46 find the largest weight, 144, 32 of them exponentials at a quarter of the rate, make weights, and some 30 are
+// pages, addresses and scales; the others, about 70 to each of a wave's 31 tiles, are before and behind the loop (the piece, q's operands, results).  Two registers of the instance spill, 12 bytes a lane.
+// In fp16 251 us, fp32 295, 4 bits 238 (fp32 275), dk 64 182, dk 192 and 256 793 (one wave a SIMD, and a tile of 256 columns for both).  Before any of this, codes that each wave converted for itself took 595 us.
+// Tried without gain: weights made first and the largest sought only where they do not fit (registers spill: 527 - 710 us), wave priorities, 32 tokens at a time.
 template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_rows_kernel(CacheAttnArgs a)
 {
     typedef Shape<D, BITS, TYPE> S;
@@ -840,7 +842,7 @@ template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_W
 }
 
 // Pieces of sequences that were cut, joined in their order: a wave per row (and further rows after it), D / 4 lanes per piece.  3.5 - 5 us where rows are few: a launch and three trips to memory.
-// (16 sequences of up to 192 rows, 8 heads, two or three pieces: 17.6 us, 30 MB written by other XCDs just before; with more or fewer workgroups or all pieces' requests at once
+// (16 sequences of up to 192 rows, 8 heads, two or three pieces: 17.5 us, 30 MB written by other XCDs just before; with more or fewer workgroups or all pieces' requests at once
 // the whole call took 1 - 17 % longer.)
 template <int D, int TYPE> __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheAttnArgs a)
 {

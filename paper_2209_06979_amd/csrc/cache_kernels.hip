@@ -3,8 +3,8 @@
 // for each vector of dk elements (a token's head).  Both directions stream: 8 elements a lane, a vector's lanes side by side.
 // A code is decided as in double precision, from the key as it is after its rotation, which is carried in double precision, too: what lies next to
 // a border of rounding goes by the definition and not by a sine's last bit.
-// Memory bounds both.  16384 tokens of 8 heads of 128 fp16: read 102 MB in 20.8 us (4.9 TB/s, what a large copy reaches), written in 33.8 with keys rotated
-// (the rotation and the quotients in double precision were 172 us for both before sines were shared and quotients decided in fp32), in 30 without.
+// Memory bounds both.  16384 tokens of 8 heads of 128 fp16: read 102 MB in 20.4 us (4.9 TB/s, what a large copy reaches), written in 33.6 with keys rotated
+// (the rotation and the quotients in double precision were 172 us for both before sines were shared and quotients decided in fp32), in 30 without, 3.4 TB/s.
 #include "decode.h"
 #include "rope.h"
 

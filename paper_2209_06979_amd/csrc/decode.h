@@ -72,10 +72,11 @@ hipError_t launch_cache_attention(const CacheAttnArgs &a, mc_type type, int bits
 
 constexpr int CACHE_TILE = 32;         // tokens that a wave takes at a time
 constexpr int CACHE_WAVES = 4;         // waves of a workgroup, which share a piece
-// Tiles of the shortest piece: two a wave.  (Sixteen: one sequence of 1024 tokens, 8 heads of 128, 13.6 us instead of 12.0, from 8192 on the same.)
+// Tiles of the shortest piece: two a wave.  (Sixteen: one sequence of 1024 tokens, 8 heads of 128, 15.3 us instead of 13.1; from 32768 tokens on 3 % more to 3 % less.)
 constexpr int CACHE_MIN_PIECE = 8;
-// Pieces asked for, over all heads of the cache and row tiles: as many as run at once, two workgroups a compute unit.  256, 512 and 1024 at 8 heads of 128, four query heads each: one sequence of
-// 65536 tokens 34.9, 34.1, 40.3 us; 8 of 4096 23.0, 21.2, 26.7; 32 of 4096 54.2, 54.8, 59.5; 64 of 8192 179.8, 180.4, 184.9.
+// Pieces asked for, over all heads of the cache and row tiles: as many as run at once, two workgroups a compute unit.  256, 512 and 1024 at 8 heads of 128, four query heads each, bf16: one sequence of
+// 65536 tokens 38.9, 37.9, 45.4 us; 8 of 4096 25.5, 24.8, 30.7; 32 of 4096 58.5, 58.6, 65.5; 64 of 8192 185.5, 192.7, 191.9.  Of 500 .. 8192 tokens each: 16 sequences 37.1, 30.4, 34.9;
+// 32 60.5, 50.2, 51.7; 48 94.6, 79.1, 72.6; 64 115.9, 94.0, 88.5; 128 193.9, 180.8, 163.2 (there more pieces than run at once even out the end, which the rule does not know).
 constexpr int CACHE_PIECES = 512;
 
 // What the launch and its workspace are made for: pieces per head asked for, tiles of rows, whether a sequence can be cut at all, and the
@@ -87,8 +88,8 @@ inline CacheAttnPlan cache_attention_plan(int kv_heads, int dk, int group, int b
     const int64_t tiles = (most_tokens + CACHE_TILE - 1) / CACHE_TILE;
     p.rows = max_new * group;
     p.width = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
-    // Tiles of 16, 64 and 128 rows for one another, 8 sequences of 4096 tokens, 8 heads of 128 (us): 16 rows 22.8, 25.4, 30.9; 20 30.1, 27.5, 30.8; 64 46.7, 33.9, 38.8;
-    // 68 71.8, 47.1, 39.6; 128 71.1, 51.2, 49.9; 192 101, 84.9, 66.7
+    // Tiles of 16, 64 and 128 rows for one another, 8 sequences of 4096 tokens, 8 heads of 128, bf16 (us): 16 rows 26.4, 30.9, 39.3; 20 35.1, 35.0, 40.3; 64 54.8, 42.0, 52.2;
+    // 68 75.5, 57.1, 52.8; 128 78.1, 62.4, 61.3; 192 127, 99.6, 87.9
     p.row_tile = p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.row_tile - 1) / p.row_tile;
     const int64_t sharers = (int64_t)kv_heads * (p.row_tiles > 0 ? p.row_tiles : 1);
