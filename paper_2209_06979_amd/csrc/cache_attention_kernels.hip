@@ -604,8 +604,9 @@ template <int D, int BITS, int TYPE> __global__ __launch_bounds__(CACHE_WAVES * 
 // the MFMAs take them, 16 bytes a lane side by side, two tiles of tokens in turn; beside them their scales.
 // What bounds it is the issue of what is not a matrix product: 4 sequences of 512 new tokens over 4096, 32 heads of 128, bf16, 133 Gflop in 250 us (530 Tflop/s; a library's bf16 product of 8192^3 reaches
 // 1200), the vector unit busy 50 % of the cycles and the matrix unit 31 %, a third of it with the weights' second halves (one half: 205 us), LDS conflicts 3 %.  A wave and tile (R = 2) counts 96 matrix and
-// 446 other vector instructions: in the loop 82 convert, 74 make scores, 46 find the largest weight, 144, 32 of them exponentials at a quarter of the rate, make weights, and some 30 are
-// pages, addresses and scales; the others, about 70 to each of a wave's 31 tiles, are before and behind the loop (the piece, q's operands, results).  Two registers of the instance spill, 12 bytes a lane.
+// 446 other vector instructions: in the loop 82 convert, 74 make scores, 46 find the largest weight, 144, 32 of them exponentials at a quarter of the rate, make weights, and 47 are
+// maxima over lanes, pages and scales; the others, 53 to each of a wave's 31 tiles, are masks, moved references, and what is before and behind the loop (the piece, q's operands, results).  Two
+// registers of the instance spill, 12 bytes a lane.
 // In fp16 251 us, fp32 295, 4 bits 238 (fp32 275), dk 64 182, dk 192 and 256 793 (one wave a SIMD, and a tile of 256 columns for both).  Before any of this, codes that each wave converted for itself took 595 us.
 // Tried without gain: weights made first and the largest sought only where they do not fit (registers spill: 527 - 710 us), wave priorities, 32 tokens at a time.
 template <int D, int BITS, int TYPE, int R> __global__ __launch_bounds__(CACHE_WAVES * 64, D <= 128 ? 2 : 1) void cache_attention_rows_kernel(CacheAttnArgs a)
