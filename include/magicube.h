@@ -626,6 +626,102 @@ int mc_cache_attention(const mc_cache *cache, const void *q_dev, mc_type type, i
                        void *stream);
 
 /* ------------------------------------------------------------------------------------
+ * The rest of a decoder around its attention, for serving and for training: norms with a block's gate and residual connection,
+ * the gated feed-forward block, log probabilities of tokens; each with its gradient.
+ * Tensors are rows of elements with unit stride, of mc_type, at any alignment; strides are those of rows, in ELEMENTS.  fp32 arithmetic, rounded once
+ * at the end where nothing else is said.  No result depends on the order in which workgroups run.
+ * ---------------------------------------------------------------------------------- */
+typedef enum { MC_NORM_NONE = 0, MC_NORM_RMS = 1, MC_NORM_LAYER = 2 } mc_norm_kind;
+
+/* The norms after a block and before the next one, for `rows` rows of `dim` elements:
+ *   a = post(x),   y = residual_scale * residual + branch_scale * gate * a,   n = pre(y)   (from the unrounded y)
+ *   MC_NORM_RMS    v / sqrt(mean v^2 + eps) * weight + bias
+ *   MC_NORM_LAYER  (v - mean v) / sqrt(mean (v - mean v)^2 + eps) * weight + bias
+ *   MC_NORM_NONE   post: a = x;  pre: there is no n
+ *   x_dev          the block's output, of `type`, as n is;  residual_dev  of residual_type, as y is (`type` or MC_F32); NULL: none, its scale is not looked at
+ *   weight_dev, bias_dev, post_weight_dev, post_bias_dev   dim elements of param_type (`type` or MC_F32); NULL: ones, zeros.  Not given for a norm that there is not
+ *   gate_dev       gate_groups rows of param_type; rows / gate_groups consecutive rows share one (gate_groups divides rows; 1: one for all).  NULL: ones, gate_groups 0
+ * 1 <= dim <= 16384, rows up to 2^31 - 1, eps >= 0, scales finite.  A row that holds an infinity or a NaN becomes NaN in part or whole, and no other does.  Squares
+ * are fp32: a row with elements beyond 2^63 is 0 or NaN. */
+typedef struct mc_block_norm_args {
+    int64_t rows;
+    int dim;
+    mc_type type, residual_type, param_type;
+    mc_norm_kind pre, post;
+    const void *x_dev; int64_t x_stride;
+    const void *residual_dev; int64_t residual_stride;
+    const void *weight_dev, *bias_dev, *post_weight_dev, *post_bias_dev;
+    const void *gate_dev; int64_t gate_groups, gate_stride;
+    float branch_scale, residual_scale, eps;
+} mc_block_norm_args;
+/* y_dev may be NULL (not written) or the residual itself with its stride, n_dev NULL without `pre`; either may be x with its stride and type.  Otherwise nothing overlaps. */
+int mc_block_norm(const mc_block_norm_args *args, void *y_dev, int64_t y_stride, void *n_dev, int64_t n_stride, void *stream);
+
+/* Gradients, from dy (of residual_type; NULL: zeros) and dn (of `type`; NULL: zeros) and the same arguments as the forward call's (nothing is kept from it).
+ *   dx_dev, dresidual_dev        of x's and of the residual's type;  dgate_dev  gate_groups rows of param_type, dgate_stride apart
+ *   dweight_dev .. dpost_bias_dev  dim elements of param_type: sums over all rows in fp32
+ * Any may be NULL: not computed.  Gradients of what was not given are NULL.  Outputs overlap nothing.
+ * The workspace (256-byte aligned, contents undefined before and after; calls that may overlap in time need one each) holds sums of rows. */
+typedef struct mc_block_norm_grads {
+    void *dx_dev; int64_t dx_stride;
+    void *dresidual_dev; int64_t dresidual_stride;
+    void *dgate_dev; int64_t dgate_stride;
+    void *dweight_dev, *dbias_dev, *dpost_weight_dev, *dpost_bias_dev;
+} mc_block_norm_grads;
+size_t mc_block_norm_backward_workspace(int64_t rows, int dim);
+int mc_block_norm_backward(const mc_block_norm_args *args, const void *dy_dev, int64_t dy_stride, const void *dn_dev, int64_t dn_stride,
+                           const mc_block_norm_grads *grads, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* The gated feed-forward block: h = act(x Wg^T) * (x Wu^T), rows x dim against two hidden x dim weights, and its gradient
+ *   dg = dh * u * act'(g),  du = dh * act(g)  (g = x Wg^T, u = x Wu^T),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
+ * Products of 16-bit types take whole elements and add in fp32, those of fp32 are fp32 throughout; h comes from the unrounded g and u.  For the gradient g and u
+ * are kept rounded to the type, and dg and du are rounded to it before the products.
+ *   MC_ACT_SILU v sigmoid(v), MC_ACT_GELU v Phi(v), MC_ACT_GELU_TANH v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2, MC_ACT_RELU max(v, 0) (slope 0 at 0), MC_ACT_SIGMOID
+ * 1 <= dim, hidden <= 2^20, rows up to 2^21 (0 is accepted: the weights' gradients are zeros then), all products of two of these at most 2^34; rows of x and of the weights
+ * are less than 16 MiB apart. */
+typedef enum { MC_ACT_SILU = 0, MC_ACT_GELU = 1, MC_ACT_GELU_TANH = 2, MC_ACT_RELU = 3, MC_ACT_SIGMOID = 4 } mc_activation;
+typedef struct mc_gated_ffn_args {
+    int64_t rows;
+    int dim, hidden;
+    mc_type type;
+    mc_activation activation;
+    const void *x_dev; int64_t x_stride;
+    const void *gate_dev; int64_t gate_stride;   /* Wg */
+    const void *up_dev; int64_t up_stride;       /* Wu */
+} mc_gated_ffn_args;
+/* g_dev and u_dev: what the gradient needs, rows x hidden of `type` each with saved_stride, or both NULL.  Outputs overlap nothing.
+ * The workspace is as for mc_block_norm_backward (more than a few rows whose pointers, strides or `dim` do not make whole 16-byte pieces: copies that do); the
+ * function gives its bytes for these arguments, 0: none is needed. */
+size_t mc_gated_ffn_workspace(const mc_gated_ffn_args *args);
+int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t h_stride, void *g_dev, void *u_dev, int64_t saved_stride, void *workspace_dev,
+                 size_t workspace_bytes, void *stream);
+/* dx_dev (rows x dim), dgate_dev and dup_dev (hidden x dim): any may be NULL (not computed); they overlap nothing. */
+size_t mc_gated_ffn_backward_workspace(const mc_gated_ffn_args *args);
+int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int64_t dh_stride, const void *g_dev, const void *u_dev, int64_t saved_stride,
+                          void *dx_dev, int64_t dx_stride, void *dgate_dev, int64_t dgate_stride, void *dup_dev, int64_t dup_stride,
+                          void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens: for each row of `vocab` logits, z = scale * logits,
+ *   logprobs[row] = z[token] - log sum e^z,   entropy[row] = - sum p log p,   and the `top` largest logits in order (equal ones: the lower index first)
+ * with their log probabilities.  All fp32 (tokens int64).
+ *   tokens_dev   rows int64; a token that is not 0 .. vocab - 1 is none: its log probability is 0
+ *   top          0 (top_logprobs_dev and top_tokens_dev may be NULL then) .. 64, at most vocab
+ *   sums_dev     rows x 2 floats for the gradient (a row's largest logit, log of its sum), or NULL
+ * A logit of -infinity has probability 0 (log probability -infinity).  A row of nothing else has log probabilities of -infinity and entropy 0.  A row that holds a NaN or +infinity has
+ * NaN for all of them; its top tokens are in order, NaN above all.  1 <= vocab <= 2^30, scale > 0 and finite; rows * ceil(vocab / 4096) at most 8 million.
+ * The workspace is as for mc_block_norm_backward; mc_token_logprobs_workspace gives its bytes, 0: none is needed. */
+size_t mc_token_logprobs_workspace(int64_t rows, int vocab, mc_type type, int top);
+int mc_token_logprobs(const void *logits_dev, mc_type type, int64_t rows, int vocab, int64_t stride, const int64_t *tokens_dev, float scale, int top,
+                      float *logprobs_dev, float *entropy_dev, float *top_logprobs_dev, int64_t *top_tokens_dev, float *sums_dev,
+                      void *workspace_dev, size_t workspace_bytes, void *stream);
+/* The logits' gradient (of their type) from those of the log probabilities, the entropies and the top log probabilities (NULL: zeros), with sums_dev, entropy_dev and
+ * top_tokens_dev of the forward call:  scale * (sum of the gradients of what names j - p_j (G + dentropy (log p_j + entropy))), G the sum of a row's gradients of
+ * log probabilities.  Zeros for a row of nothing but -infinity; tokens that are none take no part.  dlogits_dev may be logits_dev with its stride if dtop_dev is NULL; otherwise nothing overlaps. */
+int mc_token_logprobs_backward(const void *logits_dev, mc_type type, int64_t rows, int vocab, int64_t stride, const int64_t *tokens_dev, float scale, int top,
+                               const int64_t *top_tokens_dev, const float *sums_dev, const float *entropy_dev, const float *dlogprobs_dev,
+                               const float *dentropy_dev, const float *dtop_dev, void *dlogits_dev, int64_t dlogits_stride, void *stream);
+
+/* ------------------------------------------------------------------------------------
  * One-knob setters kept for existing callers, tests and measurements.  Each changes one field of
  * the CALLING THREAD's default options (see mc_set_thread_options); none is needed for
  * correctness, and none affects other threads or the ..._ex entry points.

@@ -1,0 +1,125 @@
+// Internal declarations of the operators of a decoder around its attention: norms with gate and residual, the gated feed-forward
+// block, log probabilities of tokens.
+#pragma once
+
+#include "decode.h"
+
+// ---- norms (block_norm_kernels.hip) -------------------------------------------------------------------------------------
+struct NormArgs {
+    const void *x, *r;             // block's output, residual (null: none)
+    int64_t x_stride, r_stride;    // elements, as all strides here
+    const void *weight, *bias, *post_weight, *post_bias; // null: ones, zeros
+    const void *gate;              // null: ones
+    int64_t gate_stride, gate_rows, gate_groups; // rows that share a row of the gate, rows of the gate
+    int64_t rows;
+    int dim, type, r_type, p_type; // mc_type of x and n, of r and y, of the parameters
+    int pre, post;                 // mc_norm_kind
+    float branch_scale, residual_scale, eps;
+    void *y, *n;                   // null: not written
+    int64_t y_stride, n_stride;
+    // backward
+    const void *dy, *dn;           // null: zeros
+    int64_t dy_stride, dn_stride;
+    void *dx, *dr;                 // null: not written
+    int64_t dx_stride, dr_stride;
+    void *grads[5];                // gate, weight, bias, post weight, post bias; null: not asked for
+    int64_t dgate_stride;
+    int64_t per;                   // rows of a workgroup (filled by the launcher)
+    int workgroups;
+    float *partial;                // workgroups x (2 for the gate, 4) x dim
+};
+constexpr int NORM_MOST_DIM = 16384;
+// Workgroups that a backward pass is cut into, at most (rows of up to 1024 elements: workgroups of one wave)
+inline int norm_workgroups(int64_t rows, int dim)
+{
+    const int most = dim <= 1024 ? 2048 : 512;
+    return (int)(rows < most ? rows : most);
+}
+hipError_t launch_block_norm(const NormArgs &a, hipStream_t s);
+hipError_t launch_block_norm_backward(NormArgs a, hipStream_t s);
+
+// ---- log probabilities (logprob_kernels.hip) -----------------------------------------------------------------------------
+struct LogprobArgs {
+    const void *logits;
+    int64_t stride;
+    int type;
+    int64_t rows;
+    int vocab, top;
+    float scale;
+    const int64_t *tokens;
+    float *logprobs, *entropy, *top_logprobs, *sums; // sums: (maximum, log of the sum) of each row, null: not written
+    int64_t *top_tokens;
+    int pieces;                    // pieces of a row
+    int piece_vectors;             // vectors of 16 bytes of a piece
+    float *partial;                // pieces of all rows x LOGPROB_PARTIAL
+    // backward
+    const float *dlogprobs, *dentropy, *dtop; // null: zeros
+    const int64_t *chosen;         // rows x top
+    void *dlogits;
+    int64_t dstride;
+};
+constexpr int LOGPROB_MOST_TOP = 64;
+// A piece's maximum, sum and weighted sum (and one float more), and its keys
+constexpr int logprob_partial(int top) { return 4 + 2 * top; }
+constexpr int LOGPROB_GROUPS_WANTED = 1024; // workgroups that all rows together are cut into, where they are fewer
+constexpr int LOGPROB_LEAST_VECTORS = 512; // vectors of a piece: two a thread
+struct LogprobPlan { int pieces, piece_vectors; };
+inline LogprobPlan logprob_plan(int64_t rows, int vocab, int type)
+{
+    const int per = type == MC_F32 ? 4 : 8, vectors = (vocab + per - 1) / per;
+    int64_t pieces = (LOGPROB_GROUPS_WANTED + rows - 1) / (rows > 0 ? rows : 1);
+    const int most = (vectors + LOGPROB_LEAST_VECTORS - 1) / LOGPROB_LEAST_VECTORS;
+    if (pieces > most) pieces = most;
+    if (pieces > 64) pieces = 64;
+    if (pieces < 1) pieces = 1;
+    const int each = (int)((vectors + pieces - 1) / pieces);
+    return {(int)((vectors + each - 1) / (each > 0 ? each : 1)), each};
+}
+hipError_t launch_token_logprobs(const LogprobArgs &a, hipStream_t s);
+hipError_t launch_token_logprobs_backward(const LogprobArgs &a, hipStream_t s);
+
+// ---- the gated feed-forward block (gated_ffn_kernels.hip) ------------------------------------------------------------------
+// A product of two operands whose rows run along the reduction: C[m][n] = sum over k of A[m][k] B[n][k].  Rows begin at multiples of 16 bytes
+// and k is whole pieces of 16 bytes.
+struct ProductArgs {
+    const void *a;
+    const void *b[2];              // gated: gate and up weights; else b[0]
+    int64_t a_stride, b_stride[2]; // bytes
+    int m, n, k;
+    // gated: h, and g and u if they are kept (null: not)
+    void *h, *g, *u;
+    int64_t h_stride, saved_stride; // elements
+    int activation;
+    // plain: products side by side, A's rows a_batch bytes apart, each with an output of its own
+    int batch;
+    int64_t a_batch;
+    void *c[2];
+    int64_t c_stride[2];           // elements
+    // filled by the launcher
+    int tiles_m, tiles_n;
+};
+struct FewRowsArgs { // a few rows of x against both weights
+    const void *x, *gate, *up;
+    int64_t x_stride, gate_stride, up_stride; // elements
+    int rows, dim, hidden, activation;
+    void *h, *g, *u;
+    int64_t h_stride, saved_stride;
+};
+struct GatedGradArgs { // dg and du from dh, g and u, as rows and as columns
+    const void *dh, *g, *u;
+    int64_t dh_stride, saved_stride; // elements
+    int64_t rows;
+    int hidden, activation;
+    void *d, *dt;                  // rows x 2 padded hidden; 2 padded hidden x padded rows
+    int padded_hidden;
+    int64_t padded_rows;
+};
+constexpr int FEW_ROWS = 64;
+hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_product(const ProductArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s);
+hipError_t launch_gated_grad(const GatedGradArgs &a, mc_type type, hipStream_t s);
+// rows of `width` elements (`size` bytes each) into rows of `padded` elements, zeros behind them
+hipError_t launch_pad_rows(const void *from, int64_t from_stride, int64_t rows, int width, void *to, int padded, int size, hipStream_t s);
+// to[c][r] = from[r][c] for c < columns, r < rows; zeros up to r < padded
+hipError_t launch_transpose(const void *from, int64_t from_stride, int64_t rows, int columns, void *to, int64_t to_stride, int64_t padded, int size, hipStream_t s);

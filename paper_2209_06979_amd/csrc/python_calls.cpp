@@ -946,6 +946,432 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, P
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the rest of a decoder around its attention ---------------------------------------------------------
+PyObject *g_layer_nodes[3] = {}; // binding's autograd nodes of block_norm, gated_ffn and token_logprobs
+
+// rows of elements on the device, unit stride along them
+inline bool rows_of(const at::Tensor &t) { return t.is_cuda() && t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1 || t.numel() == 0); }
+inline bool rows_like(const at::Tensor &t, const at::Tensor &x, at::ScalarType type)
+{
+    return rows_of(t) && t.device() == x.device() && t.scalar_type() == type && t.size(0) == x.size(0) && t.size(1) == x.size(1);
+}
+inline int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); } // (a single row's stride says nothing)
+// An optional tensor: null and true where it is not given
+inline bool optional(PyObject *o, const at::Tensor **t) { return !given(o) || (*t = tensor(o)); }
+inline void *data(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+inline PyObject *wrap_or_none(at::TensorBase &&t)
+{
+    if (t.defined()) return wrap(std::move(t));
+    Py_RETURN_NONE;
+}
+// A tuple of tensors, None for those that are not defined
+template <size_t N> PyObject *tuple_of(at::TensorBase (&t)[N])
+{
+    PyObject *all = PyTuple_New(N);
+    for (size_t i = 0; all && i < N; ++i) {
+        PyObject *o = wrap_or_none(std::move(t[i]));
+        if (!o) Py_CLEAR(all);
+        else PyTuple_SET_ITEM(all, i, o);
+    }
+    return all;
+}
+// Whether gradients are recorded for one of these.
+template <size_t N> bool recorded(const at::Tensor *const (&t)[N])
+{
+    if (c10::GradMode::is_enabled())
+        for (const at::Tensor *x : t)
+            if (x && x->requires_grad()) return true;
+    return false;
+}
+PyObject *no_out_gradient(const char *what)
+{
+    PyErr_Format(PyExc_RuntimeError, "%s: out= does not record gradients, and one of the tensors requires grad", what);
+    return nullptr;
+}
+template <int N> bool one_of(PyObject *o, const char *const (&names)[N], int *which)
+{
+    for (int i = 0; i < N; ++i)
+        if (names[i] ? o && PyUnicode_Check(o) && PyUnicode_CompareWithASCIIString(o, names[i]) == 0 : !given(o)) {
+            *which = i;
+            return true;
+        }
+    PyErr_SetObject(PyExc_KeyError, o ? o : Py_None);
+    return false;
+}
+
+// What block_norm and its gradient share: v = x, residual, pre, post, weight, bias, post_weight, post_bias, gate, branch_scale, residual_scale, eps
+struct NormCall {
+    const at::Tensor *x = nullptr, *residual = nullptr, *weight = nullptr, *bias = nullptr, *post_weight = nullptr, *post_bias = nullptr, *gate = nullptr;
+    at::ScalarType stream_type, param_type;
+    mc_block_norm_args args = {};
+    bool trivial = false; // y is x
+    bool read(PyObject *const *v, bool pre_default)
+    {
+        if (!(x = tensor(v[0])) || !optional(v[1], &residual) || !optional(v[4], &weight) || !optional(v[5], &bias) || !optional(v[6], &post_weight) || !optional(v[7], &post_bias) ||
+            !optional(v[8], &gate))
+            return false;
+        static const char *const kinds[3] = {nullptr, "rms", "layer"};
+        int pre = MC_NORM_RMS, post = MC_NORM_NONE;
+        if ((!(pre_default && !v[2]) && !one_of(v[2], kinds, &pre)) || !one_of(v[3], kinds, &post)) return false;
+        args.branch_scale = args.residual_scale = 1;
+        args.eps = 1e-6f;
+        if ((v[9] && !number(v[9], &args.branch_scale)) || (v[10] && !number(v[10], &args.residual_scale)) || (v[11] && !number(v[11], &args.eps))) return false;
+        if (!(rows_of(*x) && real_type(x->scalar_type(), &args.type) && current(*x) && x->size(1) <= 0x7fffffff)) return assertion();
+        stream_type = residual ? residual->scalar_type() : x->scalar_type();
+        if (!real_type(stream_type, &args.residual_type) || (residual && !rows_like(*residual, *x, stream_type))) return assertion();
+        const at::Tensor *params[5] = {weight, bias, post_weight, post_bias, gate};
+        param_type = x->scalar_type();
+        for (const at::Tensor *p : params)
+            if (p) param_type = p->scalar_type();
+        if (!real_type(param_type, &args.param_type)) return assertion();
+        for (int i = 0; i < 4; ++i)
+            if (params[i] && !array(*params[i], param_type, x->size(1), *x)) return assertion();
+        if (gate) {
+            if (!(gate->is_cuda() && gate->device() == x->device() && gate->scalar_type() == param_type && (gate->dim() == 1 || gate->dim() == 2) && gate->size(-1) == x->size(1) &&
+                  (gate->stride(-1) == 1 || gate->size(-1) <= 1)))
+                return assertion();
+            args.gate_groups = gate->dim() == 2 ? gate->size(0) : 1;
+            args.gate_stride = gate->dim() == 2 ? row_stride(*gate) : gate->size(0);
+        }
+        args.rows = x->size(0);
+        args.dim = (int)x->size(1);
+        args.pre = (mc_norm_kind)pre;
+        args.post = (mc_norm_kind)post;
+        args.x_dev = x->data_ptr(); args.x_stride = row_stride(*x);
+        if (residual) args.residual_dev = residual->data_ptr(), args.residual_stride = row_stride(*residual);
+        args.weight_dev = data(weight); args.bias_dev = data(bias); args.post_weight_dev = data(post_weight); args.post_bias_dev = data(post_bias); args.gate_dev = data(gate);
+        trivial = !residual && !gate && !post && args.branch_scale == 1;
+        return true;
+    }
+    static bool assertion()
+    {
+        ::assertion();
+        return false;
+    }
+};
+
+Params<13> p_block_norm = {"block_norm", 1, {"x", "residual", "pre", "post", "weight", "bias", "post_weight", "post_bias", "gate", "branch_scale", "residual_scale", "eps", "out"}, {}};
+
+PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[13];
+    if (!p_block_norm.parse(args, nargs, kwnames, v)) return nullptr;
+    NormCall c;
+    if (!c.read(v, true)) return nullptr;
+    const at::Tensor *y = nullptr, *n = nullptr;
+    const bool out = given(v[12]);
+    if (out) {
+        if (!PyTuple_Check(v[12]) || PyTuple_GET_SIZE(v[12]) != 2) return assertion();
+        if (!optional(PyTuple_GET_ITEM(v[12], 0), &y) || !optional(PyTuple_GET_ITEM(v[12], 1), &n)) return nullptr;
+        if ((y && !rows_like(*y, *c.x, c.stream_type)) || !n != !c.args.pre || (n && !rows_like(*n, *c.x, c.x->scalar_type()))) return assertion();
+    }
+    if (recorded({c.x, c.residual, c.weight, c.bias, c.post_weight, c.post_bias, c.gate, y, n})) {
+        if (out) return no_out_gradient("block_norm");
+        PyObject *all[12];
+        PyObject *scales[3] = {PyFloat_FromDouble(c.args.branch_scale), PyFloat_FromDouble(c.args.residual_scale), PyFloat_FromDouble(c.args.eps)};
+        static const char *const kinds[3] = {nullptr, "rms", "layer"};
+        PyObject *pre = c.args.pre ? PyUnicode_FromString(kinds[c.args.pre]) : same(Py_None);
+        for (int i = 0; i < 9; ++i) all[i] = v[i] ? v[i] : Py_None;
+        all[2] = pre;
+        for (int i = 0; i < 3; ++i) all[9 + i] = scales[i];
+        PyObject *r = pre && scales[0] && scales[1] && scales[2] ? PyObject_Vectorcall(g_layer_nodes[0], all, 12, nullptr) : nullptr;
+        for (PyObject *o : scales) Py_XDECREF(o);
+        Py_XDECREF(pre);
+        return r;
+    }
+    at::TensorBase made[2];
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        if (!out && !c.trivial) made[0] = empty(c.x->sizes(), c.stream_type, *c.x);
+        if (!out && c.args.pre) made[1] = empty(c.x->sizes(), c.x->scalar_type(), *c.x);
+        const int64_t dim = c.x->size(1);
+        void *to_y = out ? data(y) : made[0].defined() ? made[0].data_ptr() : nullptr, *to_n = out ? data(n) : made[1].defined() ? made[1].data_ptr() : nullptr;
+        rc = !to_y && !c.args.pre && c.trivial ? MC_OK : mc_block_norm(&c.args, to_y, y ? row_stride(*y) : dim, to_n, n ? row_stride(*n) : dim, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_block_norm");
+    if (out) return same(v[12]);
+    PyObject *a = c.trivial ? same(v[0]) : wrap(std::move(made[0])), *b = wrap_or_none(std::move(made[1])), *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+Params<15> p_block_norm_backward = {"_block_norm_backward", 15, {"x", "residual", "pre", "post", "weight", "bias", "post_weight", "post_bias", "gate", "branch_scale", "residual_scale", "eps",
+                                                                 "dy", "dn", "wanted"}, {}};
+
+// Gradients of x, residual, weight, bias, post_weight, post_bias, gate; bit i of `wanted`: the i-th is asked for
+PyObject *block_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[15];
+    if (!p_block_norm_backward.parse(args, nargs, kwnames, v)) return nullptr;
+    NormCall c;
+    if (!c.read(v, false)) return nullptr;
+    const at::Tensor *dy = nullptr, *dn = nullptr;
+    int wanted;
+    if (!optional(v[12], &dy) || !optional(v[13], &dn) || !integer(v[14], 0, &wanted)) return nullptr;
+    if ((dy && !rows_like(*dy, *c.x, c.stream_type)) || (dn && !rows_like(*dn, *c.x, c.x->scalar_type()))) return assertion();
+    at::TensorBase made[7], scratch;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        const at::Tensor *of[7] = {c.x, c.residual, c.weight, c.bias, c.post_weight, c.post_bias, c.gate};
+        void *to[7] = {};
+        for (int i = 0; i < 7; ++i)
+            if (of[i] && (wanted >> i & 1)) {
+                made[i] = empty(of[i]->sizes(), of[i]->scalar_type(), *c.x);
+                to[i] = made[i].data_ptr();
+            }
+        mc_block_norm_grads g = {};
+        g.dx_dev = to[0]; g.dx_stride = c.x->size(1); g.dresidual_dev = to[1]; g.dresidual_stride = c.x->size(1); g.dgate_dev = to[6]; g.dgate_stride = c.x->size(1);
+        g.dweight_dev = to[2]; g.dbias_dev = to[3]; g.dpost_weight_dev = to[4]; g.dpost_bias_dev = to[5];
+        const size_t bytes = mc_block_norm_backward_workspace(c.args.rows, c.args.dim);
+        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *c.x);
+        rc = mc_block_norm_backward(&c.args, data(dy), dy ? row_stride(*dy) : 0, data(dn), dn ? row_stride(*dn) : 0, &g, bytes ? scratch.data_ptr() : nullptr, bytes, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_block_norm_backward");
+    return tuple_of(made);
+    END_HANDLE_TH_ERRORS
+}
+
+const char *const ACTIVATIONS[5] = {"silu", "gelu", "gelu_tanh", "relu", "sigmoid"};
+
+bool ffn_args(PyObject *const *v, const at::Tensor **x, const at::Tensor **gate, const at::Tensor **up, mc_gated_ffn_args *f)
+{
+    if (!(*x = tensor(v[0])) || !(*gate = tensor(v[1])) || !(*up = tensor(v[2]))) return false;
+    int act = 0;
+    if (v[3] && !one_of(v[3], ACTIVATIONS, &act)) return false;
+    if (!(rows_of(**x) && real_type((*x)->scalar_type(), &f->type) && current(**x) && rows_of(**gate) && rows_like(**up, **gate, (*x)->scalar_type()) &&
+          (*gate)->device() == (*x)->device() && (*gate)->scalar_type() == (*x)->scalar_type() && (*gate)->size(1) == (*x)->size(1) && (*x)->size(1) <= 0x7fffffff &&
+          (*gate)->size(0) <= 0x7fffffff)) {
+        assertion();
+        return false;
+    }
+    f->rows = (*x)->size(0); f->dim = (int)(*x)->size(1); f->hidden = (int)(*gate)->size(0); f->activation = (mc_activation)act;
+    f->x_dev = (*x)->data_ptr(); f->x_stride = row_stride(**x);
+    f->gate_dev = (*gate)->data_ptr(); f->gate_stride = row_stride(**gate);
+    f->up_dev = (*up)->data_ptr(); f->up_stride = row_stride(**up);
+    return true;
+}
+
+Params<6> p_gated_ffn = {"gated_ffn", 3, {"x", "w_gate", "w_up", "activation", "out", "workspace"}, {}};
+
+// keep: h, g and u
+PyObject *gated_ffn_call(PyObject *const *v, bool keep)
+{
+    const at::Tensor *x, *gate, *up, *out = nullptr, *ws = nullptr;
+    mc_gated_ffn_args f = {};
+    if (!ffn_args(v, &x, &gate, &up, &f) || !optional(v[4], &out) || !optional(v[5], &ws)) return nullptr;
+    if (out && !(rows_of(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->size(0) == x->size(0) && out->size(1) == gate->size(0)))
+        return assertion();
+    if (ws && !(ws->is_cuda() && ws->device() == x->device() && ws->is_contiguous())) return assertion();
+    if (!keep && recorded({x, gate, up, out})) {
+        if (out) return no_out_gradient("gated_ffn");
+        PyObject *all[4] = {v[0], v[1], v[2], v[3]}, *silu = nullptr;
+        if (!all[3]) all[3] = silu = PyUnicode_FromString("silu");
+        PyObject *r = all[3] ? PyObject_Vectorcall(g_layer_nodes[1], all, 4, nullptr) : nullptr;
+        Py_XDECREF(silu);
+        return r;
+    }
+    at::TensorBase made[3], scratch;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        const int64_t hidden = gate->size(0);
+        for (int i = 0; i < 3; ++i)
+            if (i ? keep : !out) made[i] = empty({x->size(0), hidden}, x->scalar_type(), *x);
+        void *w = nullptr;
+        size_t bytes = 0;
+        if (ws) {
+            w = ws->data_ptr();
+            bytes = (size_t)ws->numel() * ws->element_size();
+        } else if ((bytes = mc_gated_ffn_workspace(&f)) > 0) {
+            scratch = empty({(int64_t)bytes}, at::kByte, *x);
+            w = scratch.data_ptr();
+        }
+        rc = mc_gated_ffn(&f, out ? out->data_ptr() : made[0].data_ptr(), out ? row_stride(*out) : hidden, keep ? made[1].data_ptr() : nullptr,
+                          keep ? made[2].data_ptr() : nullptr, hidden, w, bytes, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_gated_ffn");
+    if (keep) return tuple_of(made);
+    return out ? same(v[4]) : wrap(std::move(made[0]));
+}
+
+PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[6];
+    if (!p_gated_ffn.parse(args, nargs, kwnames, v)) return nullptr;
+    return gated_ffn_call(v, false);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *gated_ffn_kept(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[6];
+    if (!p_gated_ffn.parse(args, nargs, kwnames, v)) return nullptr;
+    if (given(v[4])) return assertion();
+    return gated_ffn_call(v, true);
+    END_HANDLE_TH_ERRORS
+}
+
+Params<8> p_gated_ffn_backward = {"_gated_ffn_backward", 8, {"x", "w_gate", "w_up", "activation", "dh", "g", "u", "wanted"}, {}};
+
+// Gradients of x, w_gate, w_up; bit i of `wanted`: the i-th is asked for
+PyObject *gated_ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[8];
+    if (!p_gated_ffn_backward.parse(args, nargs, kwnames, v)) return nullptr;
+    const at::Tensor *x, *gate, *up, *dh, *g, *u;
+    mc_gated_ffn_args f = {};
+    int wanted;
+    if (!ffn_args(v, &x, &gate, &up, &f) || !(dh = tensor(v[4])) || !(g = tensor(v[5])) || !(u = tensor(v[6])) || !integer(v[7], 0, &wanted)) return nullptr;
+    for (const at::Tensor *t : {dh, g, u})
+        if (!(rows_of(*t) && t->device() == x->device() && t->scalar_type() == x->scalar_type() && t->size(0) == x->size(0) && t->size(1) == gate->size(0))) return assertion();
+    if (row_stride(*g) != row_stride(*u)) return assertion();
+    at::TensorBase made[3], scratch;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        const at::Tensor *of[3] = {x, gate, up};
+        void *to[3] = {};
+        for (int i = 0; i < 3; ++i)
+            if (wanted >> i & 1) {
+                made[i] = empty(of[i]->sizes(), x->scalar_type(), *x);
+                to[i] = made[i].data_ptr();
+            }
+        const size_t bytes = mc_gated_ffn_backward_workspace(&f);
+        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *x);
+        rc = mc_gated_ffn_backward(&f, dh->data_ptr(), row_stride(*dh), g->data_ptr(), u->data_ptr(), row_stride(*g), to[0], f.dim, to[1], f.dim, to[2], f.dim,
+                                   bytes ? scratch.data_ptr() : nullptr, bytes, stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_gated_ffn_backward");
+    return tuple_of(made);
+    END_HANDLE_TH_ERRORS
+}
+
+Params<5> p_token_logprobs = {"token_logprobs", 2, {"logits", "tokens", "top", "scale", "workspace"}, {}};
+
+// keep: the sums for the gradient too
+PyObject *token_logprobs_call(PyObject *const *v, bool keep)
+{
+    const at::Tensor *x = tensor(v[0]), *tokens = x ? tensor(v[1]) : nullptr, *ws = nullptr;
+    int top;
+    float scale = 1;
+    if (!tokens || !integer(v[2], 0, &top) || (v[3] && !number(v[3], &scale)) || !optional(v[4], &ws)) return nullptr;
+    mc_type type;
+    if (!(rows_of(*x) && real_type(x->scalar_type(), &type) && current(*x) && x->size(1) <= 0x7fffffff && array(*tokens, at::kLong, x->size(0), *x))) return assertion();
+    if (ws && !(ws->is_cuda() && ws->device() == x->device() && ws->is_contiguous())) return assertion();
+    if (!keep && recorded({x})) {
+        PyObject *count = PyLong_FromLong(top), *factor = PyFloat_FromDouble(scale), *all[4] = {v[0], v[1], count, factor};
+        PyObject *r = count && factor ? PyObject_Vectorcall(g_layer_nodes[2], all, 4, nullptr) : nullptr;
+        Py_XDECREF(count);
+        Py_XDECREF(factor);
+        return r;
+    }
+    const int64_t rows = x->size(0), most = top > 0 ? top : 0;
+    at::TensorBase made[5], scratch;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        if (top <= x->size(1)) { // (refused below otherwise)
+            made[0] = empty({rows}, at::kFloat, *x);
+            made[1] = empty({rows}, at::kFloat, *x);
+            made[2] = empty({rows, most}, at::kFloat, *x);
+            made[3] = empty({rows, most}, at::kLong, *x);
+            if (keep) made[4] = empty({rows, 2}, at::kFloat, *x);
+            void *w = nullptr;
+            size_t bytes = 0;
+            if (ws) {
+                w = ws->data_ptr();
+                bytes = (size_t)ws->numel() * ws->element_size();
+            } else if ((bytes = mc_token_logprobs_workspace(rows, (int)x->size(1), type, top)) > 0) {
+                scratch = empty({(int64_t)bytes}, at::kByte, *x);
+                w = scratch.data_ptr();
+            }
+            rc = mc_token_logprobs(x->data_ptr(), type, rows, (int)x->size(1), row_stride(*x), static_cast<const int64_t *>(tokens->data_ptr()), scale, top,
+                                   static_cast<float *>(made[0].data_ptr()), static_cast<float *>(made[1].data_ptr()), static_cast<float *>(made[2].data_ptr()),
+                                   static_cast<int64_t *>(made[3].data_ptr()), keep ? static_cast<float *>(made[4].data_ptr()) : nullptr, w, bytes, stream());
+        } else {
+            rc = MC_EINVAL;
+        }
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_token_logprobs");
+    if (keep) return tuple_of(made);
+    at::TensorBase four[4];
+    for (int i = 0; i < 4; ++i) four[i] = std::move(made[i]);
+    return tuple_of(four);
+}
+
+PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[5];
+    if (!p_token_logprobs.parse(args, nargs, kwnames, v)) return nullptr;
+    return token_logprobs_call(v, false);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *token_logprobs_kept(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[5];
+    if (!p_token_logprobs.parse(args, nargs, kwnames, v)) return nullptr;
+    return token_logprobs_call(v, true);
+    END_HANDLE_TH_ERRORS
+}
+
+Params<9> p_token_logprobs_backward = {"_token_logprobs_backward", 9, {"logits", "tokens", "scale", "top_tokens", "sums", "entropy", "dlogprobs", "dentropy", "dtop"}, {}};
+
+PyObject *token_logprobs_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    HANDLE_TH_ERRORS
+    PyObject *v[9];
+    if (!p_token_logprobs_backward.parse(args, nargs, kwnames, v)) return nullptr;
+    const at::Tensor *x = tensor(v[0]), *tokens = x ? tensor(v[1]) : nullptr, *chosen = tokens ? tensor(v[3]) : nullptr, *sums = chosen ? tensor(v[4]) : nullptr,
+                     *entropy = sums ? tensor(v[5]) : nullptr, *dl = nullptr, *dh = nullptr, *dt = nullptr;
+    float scale;
+    if (!entropy || !number(v[2], &scale) || !optional(v[6], &dl) || !optional(v[7], &dh) || !optional(v[8], &dt)) return nullptr;
+    mc_type type;
+    const int64_t rows = x->dim() == 2 ? x->size(0) : 0;
+    if (!(rows_of(*x) && real_type(x->scalar_type(), &type) && current(*x) && x->size(1) <= 0x7fffffff && array(*tokens, at::kLong, rows, *x) && array(*entropy, at::kFloat, rows, *x) &&
+          (!dl || array(*dl, at::kFloat, rows, *x)) && (!dh || array(*dh, at::kFloat, rows, *x))))
+        return assertion();
+    for (const at::Tensor *t : {chosen, sums, dt})
+        if (t && !(t->is_cuda() && t->device() == x->device() && t->dim() == 2 && t->size(0) == rows && t->is_contiguous())) return assertion();
+    if (!(chosen->scalar_type() == at::kLong && sums->scalar_type() == at::kFloat && sums->size(1) == 2 && (!dt || (dt->scalar_type() == at::kFloat && dt->size(1) == chosen->size(1)))))
+        return assertion();
+    at::TensorBase made;
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        made = empty(x->sizes(), x->scalar_type(), *x);
+        rc = mc_token_logprobs_backward(x->data_ptr(), type, rows, (int)x->size(1), row_stride(*x), static_cast<const int64_t *>(tokens->data_ptr()), scale, (int)chosen->size(1),
+                                        static_cast<const int64_t *>(chosen->data_ptr()), static_cast<const float *>(sums->data_ptr()), static_cast<const float *>(entropy->data_ptr()),
+                                        static_cast<const float *>(data(dl)), static_cast<const float *>(data(dh)), static_cast<const float *>(data(dt)), made.data_ptr(), x->size(1),
+                                        stream());
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_token_logprobs_backward");
+    return wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *set_layer_nodes(PyObject *, PyObject *args)
+{
+    PyObject *node[3];
+    if (!PyArg_ParseTuple(args, "OOO", &node[0], &node[1], &node[2])) return nullptr;
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(node[i]);
+        Py_XSETREF(g_layer_nodes[i], node[i]);
+    }
+    Py_RETURN_NONE;
+}
+
 PyObject *set_error_class(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -1029,6 +1455,29 @@ PyMethodDef functions[] = {
      "max_new each (None: the same number for all).  tree (total,) int64: bit j of a row lets it see the sequence's new token j (None: all\n"
      "up to itself).  scale: None is 1 / sqrt(dk).  See mc_cache_attention in magicube.h for what out-of-range values do.  Rows of no\n"
      "sequence stay as `out` has them, and have no defined value without it.  For inference: no gradient is recorded."},
+    {"block_norm", FAST(block_norm),
+     "block_norm(x, residual=None, pre='rms', post=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None,\n"
+     "           branch_scale=1.0, residual_scale=1.0, eps=1e-6, out=None)\n--\n\n"
+     "The norms after a block and before the next one: a = post(x), y = residual_scale * residual + branch_scale * gate * a, n = pre(y);\n"
+     "returns (y, n).  x (rows, dim) fp32, fp16 or bf16, residual the same or fp32 (y has its type); pre and post 'rms', 'layer' or None (n is\n"
+     "None without pre); weights and biases (dim,), gate (dim,) or (groups, dim), each row for rows / groups consecutive rows, all of one\n"
+     "type (x's or fp32).  y is x itself where there is nothing to add or to scale.  out: a tuple (y or None, n) to write to; y may be the\n"
+     "residual, or either may be x.  Autograd records it (out must be None then)."},
+    {"gated_ffn", FAST(gated_ffn),
+     "gated_ffn(x, w_gate, w_up, activation='silu', out=None, workspace=None)\n--\n\n"
+     "act(x w_gate^T) * (x w_up^T): x (rows, dim), weights (hidden, dim), all fp32, fp16 or bf16; activation 'silu', 'gelu',\n"
+     "'gelu_tanh', 'relu' or 'sigmoid'.  Autograd records it (out must be None then)."},
+    {"token_logprobs", FAST(token_logprobs),
+     "token_logprobs(logits, tokens, top=0, scale=1.0, workspace=None)\n--\n\n"
+     "(log probabilities of the tokens, entropies, log probabilities of the `top` most likely tokens, these tokens) of rows of\n"
+     "scale * logits (rows, vocab) fp32, fp16 or bf16: (rows,), (rows,), (rows, top) fp32 and (rows, top) int64.  tokens (rows,) int64, those\n"
+     "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three."},
+    {"_set_layer_nodes", set_layer_nodes, METH_VARARGS, "what block_norm, gated_ffn and token_logprobs call for tensors that require grad"},
+    {"_block_norm_backward", FAST(block_norm_backward), "gradients of block_norm's tensors (see mc_block_norm_backward)"},
+    {"_gated_ffn_kept", FAST(gated_ffn_kept), "gated_ffn with what its gradient needs: (h, g, u)"},
+    {"_gated_ffn_backward", FAST(gated_ffn_backward), "gradients of gated_ffn's tensors (see mc_gated_ffn_backward)"},
+    {"_token_logprobs_kept", FAST(token_logprobs_kept), "token_logprobs with what its gradient needs: its results and the sums"},
+    {"_token_logprobs_backward", FAST(token_logprobs_backward), "the gradient of token_logprobs' logits (see mc_token_logprobs_backward)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};
@@ -1056,6 +1505,7 @@ PyMODINIT_FUNC PyInit__native(void)
     CacheType.tp_new = PyType_GenericNew;
     if (PyType_Ready(&CacheType) < 0) return nullptr;
     p_rope.intern(); p_cache_write.intern(); p_cache_read.intern(); p_cache_attention.intern();
+    p_block_norm.intern(); p_block_norm_backward.intern(); p_gated_ffn.intern(); p_gated_ffn_backward.intern(); p_token_logprobs.intern(); p_token_logprobs_backward.intern();
     PyObject *m = PyModule_Create(&module_def);
     if (!m) return nullptr;
     Py_INCREF(&MatrixType);
