@@ -675,7 +675,7 @@ int mc_block_norm_backward(const mc_block_norm_args *args, const void *dy_dev, i
 /* The gated feed-forward block: h = act(x Wg^T) * (x Wu^T), rows x dim against two hidden x dim weights, and its gradient
  *   dg = dh * u * act'(g),  du = dh * act(g)  (g = x Wg^T, u = x Wu^T),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
  * Products of 16-bit types take whole elements and add in fp32, those of fp32 are fp32 throughout; h comes from the unrounded g and u.  For the gradient g and u
- * are kept rounded to the type, and dg and du are rounded to it before the products.
+ * are kept in fp32; dg and du are rounded to the type, once, before the products.
  *   MC_ACT_SILU v sigmoid(v), MC_ACT_GELU v Phi(v), MC_ACT_GELU_TANH v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2, MC_ACT_RELU max(v, 0) (slope 0 at 0), MC_ACT_SIGMOID
  * 1 <= dim, hidden <= 2^20, rows up to 2^21 (0 is accepted: the weights' gradients are zeros then), all products of two of these at most 2^34; rows of x and of the weights
  * are less than 16 MiB apart. */
@@ -689,15 +689,15 @@ typedef struct mc_gated_ffn_args {
     const void *gate_dev; int64_t gate_stride;   /* Wg */
     const void *up_dev; int64_t up_stride;       /* Wu */
 } mc_gated_ffn_args;
-/* g_dev and u_dev: what the gradient needs, rows x hidden of `type` each with saved_stride, or both NULL.  Outputs overlap nothing.
+/* g_dev and u_dev: what the gradient needs, rows x hidden floats each with saved_stride, or both NULL.  Outputs overlap nothing.
  * The workspace is as for mc_block_norm_backward (more than a few rows whose pointers, strides or `dim` do not make whole 16-byte pieces: copies that do); the
  * function gives its bytes for these arguments, 0: none is needed. */
 size_t mc_gated_ffn_workspace(const mc_gated_ffn_args *args);
-int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t h_stride, void *g_dev, void *u_dev, int64_t saved_stride, void *workspace_dev,
+int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t h_stride, float *g_dev, float *u_dev, int64_t saved_stride, void *workspace_dev,
                  size_t workspace_bytes, void *stream);
 /* dx_dev (rows x dim), dgate_dev and dup_dev (hidden x dim): any may be NULL (not computed); they overlap nothing. */
 size_t mc_gated_ffn_backward_workspace(const mc_gated_ffn_args *args);
-int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int64_t dh_stride, const void *g_dev, const void *u_dev, int64_t saved_stride,
+int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int64_t dh_stride, const float *g_dev, const float *u_dev, int64_t saved_stride,
                           void *dx_dev, int64_t dx_stride, void *dgate_dev, int64_t dgate_stride, void *dup_dev, int64_t dup_stride,
                           void *workspace_dev, size_t workspace_bytes, void *stream);
 

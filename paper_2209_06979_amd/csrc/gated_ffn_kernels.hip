@@ -1,6 +1,7 @@
 // The gated feed-forward block, h = act(x Wg^T) (x Wu^T), and its gradient
 //   dg = dh u act'(g),   du = dh act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
-// All products have the form C[m][n] = sum of A[m][k] B[n][k] with k along the rows of both (the gradient's operands that lie the other way are written transposed first).
+// Three products of matrices, of one tiled kernel: for the first k lies along the rows of both operands, for dx along those of dg and du alone, for dWg and dWu along
+// none; operands that have a row for each k are transposed on their way from LDS into registers.
 #include "layer.h"
 
 #include "lds_async.h"
@@ -73,33 +74,101 @@ template <int TYPE> __device__ __forceinline__ v4f multiply(const v4i &a, const 
     }
 }
 
-// Four neighbouring elements, `n` of them.
-template <class T> __device__ __forceinline__ void store4(T *to, const float (&v)[4], int n)
+// RUN neighbouring elements, `n` of them.
+template <class T, int RUN> __device__ __forceinline__ void store_run(T *to, const float (&v)[RUN], int n)
 {
-    T h[4];
+    T h[RUN];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = (T)v[e];
-    if (n >= 4) return (void)__builtin_memcpy(to, h, 4 * sizeof(T));
+    for (int e = 0; e < RUN; ++e) h[e] = (T)v[e];
+    if (n >= RUN) return (void)__builtin_memcpy(to, h, RUN * sizeof(T));
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < RUN; ++e)
         if (e < n) to[e] = h[e];
 }
 
 // ---- the tiled product ------------------------------------------------------------------------------------------------------
 __device__ const v4i zeros[1] = {};
 
-constexpr int STEP = 128;           // bytes of a row that a step takes: eight pieces of 16
+constexpr int STEP = 128;           // bytes of k that a step takes
 constexpr int TOGETHER = 8;         // tiles of rows that follow one another for the same columns
+enum { PLAIN, GATED, PARTIAL };     // what becomes of a tile: C, act(g) u, or fp32 sums of a piece of k
 
-// BM x BN tiles, WM x WN waves.  GATED: the rows of B are half gate's, half up's, such that each wave has both of its columns.
-// Pieces lie in LDS at place (piece ^ row % 8) of their row: the rows that a read addresses at once have different banks.
-template <int TYPE, int BM, int BN, int WM, int WN, bool GATED> __global__ __launch_bounds__(64 * WM *WN) void product_kernel(ProductArgs a)
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+
+// One operand's share of the kernel: X of its rows (m or n) to a tile, of which a wave multiplies X / SHARES in FRAGMENTS of 16.
+// ROWS false: k along rows.  LDS holds a row's eight pieces of 16 bytes at places (piece ^ row % 8), so that what a read addresses at once has different banks.
+// ROWS true: a row for each k.  LDS holds the rows, in units of 16 elements at places (unit ^ turned(row)), for the same reason.
+template <int TYPE, int X, int SHARES, int WAVES, bool ROWS> struct Operand {
+    typedef typename RealOf<TYPE>::type T;
+    static constexpr int SIZE = sizeof(T), PER = 16 / SIZE, KS = STEP / SIZE, COPIES = X / 8 / WAVES, FRAGMENTS = X / SHARES / 16;
+    static constexpr int LINE = X * SIZE, LANES = LINE / 16, UNITS = X / 16; // of a row of the second form
+    static_assert(COPIES * 8 * WAVES == X && FRAGMENTS * 16 * SHARES == X, "whole copies and fragments");
+    unsigned from[COPIES];  // of the lane's pieces, behind the step's address
+    unsigned at[FRAGMENTS]; // of the lane's fragments, behind the stage's address
+
+    static __device__ __forceinline__ int turned(int row) { return (SIZE == 4 ? row >> 2 & 3 : (row & 3) | (row >> 3 & 1) << 2) & (UNITS - 1); }
+    static __device__ __forceinline__ int row_of(int copy, int lane) { return ROWS ? copy * (64 / LANES) + lane / LANES : copy * 8 + (lane >> 3); }
+    // the tile's rows from `first` on of `count`; the wave's share
+    __device__ __forceinline__ void set(int first, int count, int64_t stride, int w, int share, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int row = row_of(w * COPIES + i, lane);
+            if constexpr (ROWS) {
+                const int place = lane % LANES, column = (place / SIZE ^ turned(row)) * 16 + place % SIZE * PER;
+                from[i] = (unsigned)(row * stride) + (first + column < count ? column * SIZE : 0); // (columns beyond the last are never stored)
+            } else {
+                from[i] = (unsigned)((min(first + row, count - 1) - first) * stride) + piece(lane) * 16;
+            }
+        }
+        fragments(share, lane);
+    }
+    static __device__ __forceinline__ int piece(int lane) { return (lane & 7) ^ (lane >> 3); }
+    __device__ __forceinline__ void fragments(int share, int lane)
+    {
+        const int i = lane & 15, q = lane >> 4;
+#pragma unroll
+        for (int f = 0; f < FRAGMENTS; ++f) {
+            const int unit = share * FRAGMENTS + f;
+            if constexpr (!ROWS) at[f] = (unit * 16 + i) * STEP;
+            else if constexpr (SIZE == 4) at[f] = 4 * q * LINE + (unit ^ (q & (UNITS - 1))) * 64 + i * 4;
+            else at[f] = (8 * q + (i >> 2)) * LINE + (unit ^ turned(8 * q + (i >> 2))) * 32 + (i & 3) * 8;
+        }
+    }
+    // what the lane's piece of copy i begins with along k, of the step's
+    static __device__ __forceinline__ int begins(int copy, int lane) { return ROWS ? row_of(copy, lane) : piece(lane) * PER; }
+    // Half `h` of a step.
+    __device__ __forceinline__ v4i read(const char *stage, int f, int h, int lane) const
+    {
+        if constexpr (!ROWS) {
+            return *reinterpret_cast<const v4i *>(stage + at[f] + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
+        } else if constexpr (SIZE == 4) {
+            v4i v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int *>(stage + at[f] + (h * 16 + e) * LINE);
+            return v;
+        } else { // four rows of 16 elements become four elements of 16 rows, twice
+            const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(stage + at[f] + h * 32 * LINE));
+            const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(stage + at[f] + (h * 32 + 4) * LINE));
+            return __builtin_bit_cast(v4i, (__attribute__((ext_vector_type(8))) short){a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w});
+        }
+    }
+};
+
+// BM x BN tiles, WM x WN waves, NS stages.  GATED: the rows of B are half gate's, half up's, such that each wave has both of its columns; where it has 32 of
+// them, a lane's eight neighbouring ones.
+template <int TYPE, int BM, int BN, int WM, int WN, int NS, bool AR, bool BR, int MODE> __global__ __launch_bounds__(64 * WM *WN) void product_kernel(ProductArgs a)
 {
     typedef typename RealOf<TYPE>::type T;
-    constexpr int W = WM * WN, RM = BM / WM, RN = BN / WN, MF = RM / 16, NF = RN / 16, CA = BM / 8 / W, CB = BN / 8 / W, STAGE = (BM + BN) * STEP;
-    constexpr int PER = 16 / sizeof(T), COLUMNS = GATED ? BN / 2 : BN;
-    static_assert(CA * 8 * W == BM && CB * 8 * W == BN && RN % 32 == 0, "whole copies");
-    __shared__ __attribute__((aligned(1024))) char lds[2][STAGE];
+    constexpr int W = WM * WN, RM = BM / WM, RN = BN / WN, MF = RM / 16, NF = RN / 16, STAGE = (BM + BN) * STEP;
+    constexpr int KS = STEP / sizeof(T), COLUMNS = MODE == GATED ? BN / 2 : BN;
+    constexpr bool EIGHT = MODE == GATED && RN % 64 == 0;
+    typedef Operand<TYPE, BM, WM, W, AR> A;
+    typedef Operand<TYPE, BN, WN, W, BR> B;
+    constexpr int COPIES = A::COPIES + B::COPIES;
+    static_assert(MODE != GATED || (!AR && !BR), "weights lie with k along their rows");
+    __shared__ __attribute__((aligned(1024))) char lds[NS][STAGE];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
 
     // Workgroups go to the eight XCDs round-robin: each gets a run of tiles, in blocks of TOGETHER tiles of rows.
@@ -108,43 +177,56 @@ template <int TYPE, int BM, int BN, int WM, int WN, bool GATED> __global__ __lau
     const int block = t / (TOGETHER * a.tiles_n), high = min(TOGETHER, a.tiles_m - block * TOGETHER), in = t - block * TOGETHER * a.tiles_n;
     const int m0 = (block * TOGETHER + in % high) * BM, n0 = in / high * COLUMNS, z = blockIdx.y;
 
-    const int piece = (lane & 7) ^ (lane >> 3);
-    const char *const pa = static_cast<const char *>(a.a) + z * a.a_batch + m0 * a.a_stride;
-    const char *pb[CB];
-    unsigned oa[CA], ob[CB];
+    A oa;
+    B ob;
+    oa.set(m0, a.m, a.a_stride, w, wm, lane);
+    const char *pa[2], *pb[2]; // of the products of a sum
+    const int64_t a_ahead = AR ? KS * a.a_stride : STEP, b_ahead = BR ? KS * a.b_stride[0] : STEP;
+    pa[0] = static_cast<const char *>(z ? a.a[1] : a.a[0]) + (AR ? m0 * (int64_t)sizeof(T) : m0 * a.a_stride);
+    pa[1] = static_cast<const char *>(a.a[1]) + (AR ? m0 * (int64_t)sizeof(T) : m0 * a.a_stride);
+    const char *gated[B::COPIES];
+    if constexpr (MODE == GATED) {
 #pragma unroll
-    for (int i = 0; i < CA; ++i) {
-        const int row = (w * CA + i) * 8 + (lane >> 3);
-        oa[i] = (unsigned)((min(m0 + row, a.m - 1) - m0) * a.a_stride) + piece * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < CB; ++i) {
-        const int first = (w * CB + i) * 8;
-        int row = first + (lane >> 3), which = 0;
-        if constexpr (GATED) {
-            which = first % RN >= RN / 2;
-            row = first / RN * (RN / 2) + first % (RN / 2) + (lane >> 3);
+        for (int i = 0; i < B::COPIES; ++i) {
+            const int first = (w * B::COPIES + i) * 8, which = first % RN >= RN / 2, in = first % (RN / 2) + (lane >> 3);
+            // (row 16 f + 4 q + e of 32 holds column 8 q + 4 f + e)
+            const int column = first / RN * (RN / 2) + (EIGHT ? (in & ~31) + (in >> 2 & 3) * 8 + (in >> 4 & 1) * 4 + (in & 3) : in);
+            const int64_t stride = which ? a.b_stride[1] : a.b_stride[0];
+            gated[i] = static_cast<const char *>(which ? a.b[1] : a.b[0]) + n0 * stride;
+            ob.from[i] = (unsigned)((min(n0 + column, a.n - 1) - n0) * stride) + B::piece(lane) * 16;
         }
-        const int64_t stride = GATED && which ? a.b_stride[1] : a.b_stride[0];
-        pb[i] = static_cast<const char *>(GATED && which ? a.b[1] : a.b[0]) + n0 * stride;
-        ob[i] = (unsigned)((min(n0 + row, a.n - 1) - n0) * stride) + piece * 16;
+        ob.fragments(wn, lane);
+    } else {
+        ob.set(n0, a.n, a.b_stride[0], w, wn, lane);
+        pb[0] = static_cast<const char *>(a.b[0]) + (BR ? n0 * (int64_t)sizeof(T) : n0 * a.b_stride[0]);
+        pb[1] = static_cast<const char *>(a.b[1]) + (BR ? n0 * (int64_t)sizeof(T) : n0 * a.b_stride[0]);
     }
     const unsigned base = mcu::lds_addr_uniform(lds);
-    const int steps = (a.k + 8 * PER - 1) / (8 * PER);
-    auto request = [&](int step, int buffer) {
-        const int64_t at = (int64_t)step * STEP;
-        const unsigned to = base + buffer * STAGE;
-        if ((step + 1) * 8 * PER <= a.k) {
+    const int each = (a.k + KS - 1) / KS, all = MODE == GATED ? each : each * a.sum;
+    int first = 0, steps = all;
+    if constexpr (MODE == PARTIAL) {
+        first = (int)((int64_t)all * blockIdx.z / a.splits);
+        steps = (int)((int64_t)all * (blockIdx.z + 1) / a.splits) - first;
+    }
+    auto request = [&](int s) { // step s of this workgroup's
+        const int step = first + s, second = MODE != GATED && step >= each, own = second ? step - each : step;
+        const unsigned to = base + s % NS * STAGE;
+        const char *const ca = (second ? pa[1] : pa[0]) + own * a_ahead;
+        if ((own + 1) * KS <= a.k) {
 #pragma unroll
-            for (int i = 0; i < CA; ++i) mcu::copy16_to_lds(pa + at, oa[i], to + (w * CA + i) * 1024);
+            for (int i = 0; i < A::COPIES; ++i) mcu::copy16_to_lds(ca, oa.from[i], to + (w * A::COPIES + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < CB; ++i) mcu::copy16_to_lds(pb[i] + at, ob[i], to + BM * STEP + (w * CB + i) * 1024);
-        } else { // pieces beyond k are zeros of both operands
-            const bool there = step * 8 * PER + piece * PER < a.k;
+            for (int i = 0; i < B::COPIES; ++i)
+                mcu::copy16_to_lds((MODE == GATED ? gated[i] : second ? pb[1] : pb[0]) + own * b_ahead, ob.from[i], to + BM * STEP + (w * B::COPIES + i) * 1024);
+        } else { // what lies beyond k is zeros of both operands
+            const int left = a.k - own * KS;
 #pragma unroll
-            for (int i = 0; i < CA; ++i) mcu::copy16_to_lds(there ? (const void *)(pa + at + oa[i]) : zeros, to + (w * CA + i) * 1024);
+            for (int i = 0; i < A::COPIES; ++i)
+                mcu::copy16_to_lds(A::begins(w * A::COPIES + i, lane) < left ? (const void *)(ca + oa.from[i]) : zeros, to + (w * A::COPIES + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < CB; ++i) mcu::copy16_to_lds(there ? (const void *)(pb[i] + at + ob[i]) : zeros, to + BM * STEP + (w * CB + i) * 1024);
+            for (int i = 0; i < B::COPIES; ++i)
+                mcu::copy16_to_lds(B::begins(w * B::COPIES + i, lane) < left ? (const void *)((MODE == GATED ? gated[i] : second ? pb[1] : pb[0]) + own * b_ahead + ob.from[i]) : zeros,
+                                   to + BM * STEP + (w * B::COPIES + i) * 1024);
         }
     };
 
@@ -153,49 +235,51 @@ template <int TYPE, int BM, int BN, int WM, int WN, bool GATED> __global__ __lau
     for (int n = 0; n < NF; ++n)
 #pragma unroll
         for (int m = 0; m < MF; ++m) acc[n][m] = (v4f){0, 0, 0, 0};
-    if (steps > 0) request(0, 0);
-    mcu::vm_wait<0>();
-    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+        if (s < steps) request(s);
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) request(s + 1, (s + 1) & 1); // (its readers passed the last barrier)
-        const char *const la = lds[s & 1] + (wm * RM + (lane & 15)) * STEP, *const lb = lds[s & 1] + (BM + wn * RN + (lane & 15)) * STEP;
+        if (s + NS - 1 <= steps) mcu::vm_wait<(NS - 2) * COPIES>(); // (step s has come: that many copies were asked for behind it)
+        else mcu::vm_wait<0>();
+        asm volatile("s_barrier" ::: "memory"); // for all waves, whose reads of the stage that is written next have returned, too
+        if (s + NS - 1 < steps) request(s + NS - 1);
+        const char *const la = lds[s % NS], *const lb = lds[s % NS] + BM * STEP;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int at = ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16;
             v4i fa[MF], fb[NF];
 #pragma unroll
-            for (int m = 0; m < MF; ++m) fa[m] = *reinterpret_cast<const v4i *>(la + at + m * 16 * STEP);
+            for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
 #pragma unroll
-            for (int n = 0; n < NF; ++n) fb[n] = *reinterpret_cast<const v4i *>(lb + at + n * 16 * STEP);
+            for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
 #pragma unroll
             for (int n = 0; n < NF; ++n)
 #pragma unroll
                 for (int m = 0; m < MF; ++m) acc[n][m] = multiply<TYPE>(fb[n], fa[m], acc[n][m]);
         }
-        mcu::vm_wait<0>();
-        __syncthreads();
+        mcu::lgkm_wait();
     }
 
 #pragma unroll
     for (int m = 0; m < MF; ++m) {
         const int row = m0 + wm * RM + m * 16 + (lane & 15);
         if (row >= a.m) continue;
-        if constexpr (GATED) {
+        if constexpr (MODE == GATED) {
+            constexpr int RUN = EIGHT ? 8 : 4, FS = RUN / 4;
 #pragma unroll
-            for (int n = 0; n < NF / 2; ++n) {
-                const int column = n0 + wn * (RN / 2) + n * 16 + 4 * (lane >> 4), count = a.n - column;
+            for (int n = 0; n < NF / 2; n += FS) {
+                const int column = n0 + wn * (RN / 2) + n * 16 + RUN * (lane >> 4), count = a.n - column;
                 if (count <= 0) continue;
-                float h[4], g[4], u[4];
+                float h[RUN], g[RUN], u[RUN];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    g[e] = acc[n][m][e];
-                    u[e] = acc[NF / 2 + n][m][e];
+                for (int e = 0; e < RUN; ++e) {
+                    g[e] = acc[n + e / 4][m][e % 4];
+                    u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
                     h[e] = activated(g[e], a.activation) * u[e];
                 }
-                store4(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
+                store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
                 if (a.g) {
-                    store4(static_cast<T *>(a.g) + row * a.saved_stride + column, g, count);
-                    store4(static_cast<T *>(a.u) + row * a.saved_stride + column, u, count);
+                    store_run(a.g + row * a.saved_stride + column, g, count);
+                    store_run(a.u + row * a.saved_stride + column, u, count);
                 }
             }
         } else {
@@ -204,10 +288,29 @@ template <int TYPE, int BM, int BN, int WM, int WN, bool GATED> __global__ __lau
                 const int column = n0 + wn * RN + n * 16 + 4 * (lane >> 4), count = a.n - column;
                 if (count <= 0) continue;
                 const float v[4] = {acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3]};
-                store4(static_cast<T *>(z ? a.c[1] : a.c[0]) + row * (z ? a.c_stride[1] : a.c_stride[0]) + column, v, count);
+                if constexpr (MODE == PARTIAL) store_run(a.partial + ((int64_t)(blockIdx.z * a.batch + z) * a.m + row) * a.n + column, v, count);
+                else store_run(static_cast<T *>(z ? a.c[1] : a.c[0]) + row * (z ? a.c_stride[1] : a.c_stride[0]) + column, v, count);
             }
         }
     }
+}
+
+// The pieces' sums, four columns to a thread, in the order of the pieces.
+template <int TYPE> __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a)
+{
+    typedef typename RealOf<TYPE>::type T;
+    const int quads = (a.n + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.m * quads;
+    if (id >= all * a.batch) return;
+    const int z = id >= all;
+    const int64_t row = (id - z * all) / quads;
+    const int column = (int)(id - z * all - row * quads) * 4, count = a.n - column;
+    const float *from = a.partial + ((int64_t)z * a.m + row) * a.n + column;
+    float v[4] = {0, 0, 0, 0};
+    for (int s = 0; s < a.splits; ++s, from += (int64_t)a.batch * a.m * a.n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += e < count ? from[e] : 0;
+    store_run(static_cast<T *>(z ? a.c[1] : a.c[0]) + row * (z ? a.c_stride[1] : a.c_stride[0]) + column, v, count);
 }
 
 // ---- a few rows --------------------------------------------------------------------------------------------------------------
@@ -288,40 +391,51 @@ template <int TYPE, int MT> __global__ __launch_bounds__(64 * FEW_WAVES) void fe
             us[e] = su[e];
             h[e] = activated(gs[e], a.activation) * us[e];
         }
-        store4(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
+        store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
         if (a.g) {
-            store4(static_cast<T *>(a.g) + row * a.saved_stride + column, gs, count);
-            store4(static_cast<T *>(a.u) + row * a.saved_stride + column, us, count);
+            store_run(a.g + row * a.saved_stride + column, gs, count);
+            store_run(a.u + row * a.saved_stride + column, us, count);
         }
     }
 }
 
 // ---- the gradient's operands ---------------------------------------------------------------------------------------------------
-constexpr int TILE = 64;
-// A tile of 64 x 64 elements, of which rows x columns are there: written to `to` transposed, with zeros for missing rows up to `padded`
-// of them.  Four threads to a line.
-template <class T> __device__ __forceinline__ void write_transposed(const T (&tile)[TILE][TILE + 2], T *to, int64_t stride, int columns, int padded)
+// dg and du, rounded to the type that the products take: once each, half a step, whose signs the products' sums even out.  Eight elements to a thread; columns from
+// hidden to padded_hidden are zeros.
+template <int TYPE> __global__ __launch_bounds__(256) void gated_grad_kernel(GatedGradArgs a)
 {
-    const int c = threadIdx.x / 4;
-    if (c >= columns) return;
+    typedef typename RealOf<TYPE>::type T;
+    const int octs = (a.padded_hidden + 7) / 8;
+    const int64_t all = a.rows * octs;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+        const int64_t row = id / octs;
+        const int column = (int)(id - row * octs) * 8, count = a.hidden - column;
+        const T *dh = static_cast<const T *>(a.dh) + row * a.dh_stride + column;
+        const float *g = a.g + row * a.saved_stride + column, *u = a.u + row * a.saved_stride + column;
+        T d[8];
+        float gs[8], us[8], dg[8], du[8];
+        if (count >= 8) {
+            __builtin_memcpy(d, dh, sizeof d);
+            __builtin_memcpy(gs, g, 32);
+            __builtin_memcpy(us, u, 32);
+        } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = threadIdx.x % 4 * 16 + i;
-        if (r < padded) to[c * stride + r] = tile[r][c];
+            for (int e = 0; e < 8; ++e) {
+                d[e] = e < count ? dh[e] : (T)0;
+                gs[e] = e < count ? g[e] : 0;
+                us[e] = e < count ? u[e] : 0;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float slope;
+            const float act = activated(gs[e], a.activation, slope);
+            du[e] = (float)d[e] * act;
+            dg[e] = (float)d[e] * us[e] * slope;
+        }
+        store_run(static_cast<T *>(a.dg) + row * a.padded_hidden + column, dg, a.padded_hidden - column);
+        store_run(static_cast<T *>(a.du) + row * a.padded_hidden + column, du, a.padded_hidden - column);
     }
-}
-
-template <class T> __global__ __launch_bounds__(256) void transpose_kernel(const T *from, int64_t from_stride, int64_t rows, int columns, T *to, int64_t to_stride, int64_t padded)
-{
-    __shared__ T tile[TILE][TILE + 2];
-    const int64_t r0 = (int64_t)blockIdx.y * TILE;
-    const int c0 = blockIdx.x * TILE, here = min(TILE, columns - c0);
-    for (int i = threadIdx.x; i < TILE * TILE; i += 256) {
-        const int r = i / TILE, c = i % TILE;
-        tile[r][c] = r0 + r < rows && c < here ? from[(r0 + r) * from_stride + c0 + c] : (T)0;
-    }
-    __syncthreads();
-    write_transposed(tile, to + c0 * to_stride + r0, to_stride, here, (int)min((int64_t)TILE, padded - r0));
 }
 
 template <class T> __global__ __launch_bounds__(256) void pad_rows_kernel(const T *from, int64_t from_stride, int64_t rows, int width, T *to, int padded)
@@ -333,54 +447,31 @@ template <class T> __global__ __launch_bounds__(256) void pad_rows_kernel(const 
     }
 }
 
-// dg and du (rounded to the type that the products take: half a step of each, whose signs the sums over rows and columns even out), written as rows and
-// as columns.  What lies between a matrix's end and its padded end is zero.
-template <int TYPE> __global__ __launch_bounds__(256) void gated_grad_kernel(GatedGradArgs a)
-{
-    typedef typename RealOf<TYPE>::type T;
-    __shared__ T tg[TILE][TILE + 2], tu[TILE][TILE + 2];
-    const int64_t r0 = (int64_t)blockIdx.y * TILE;
-    const int c0 = blockIdx.x * TILE;
-    const int64_t width = 2 * (int64_t)a.padded_hidden;
-    for (int i = threadIdx.x; i < TILE * TILE; i += 256) {
-        const int r = i / TILE, c = i % TILE;
-        T dg = (T)0, du = (T)0;
-        if (r0 + r < a.rows && c0 + c < a.hidden) {
-            const float dh = (float)static_cast<const T *>(a.dh)[(r0 + r) * a.dh_stride + c0 + c];
-            const float g = (float)static_cast<const T *>(a.g)[(r0 + r) * a.saved_stride + c0 + c], u = (float)static_cast<const T *>(a.u)[(r0 + r) * a.saved_stride + c0 + c];
-            float slope;
-            du = (T)(dh * activated(g, a.activation, slope));
-            dg = (T)(dh * u * slope);
-        }
-        tg[r][c] = dg;
-        tu[r][c] = du;
-        if (a.d && r0 + r < a.rows && c0 + c < a.padded_hidden) {
-            T *to = static_cast<T *>(a.d) + (r0 + r) * width + c0 + c;
-            to[0] = dg;
-            to[a.padded_hidden] = du;
-        }
-    }
-    if (!a.dt) return;
-    __syncthreads();
-    const int columns = min(TILE, a.padded_hidden - c0), padded = (int)min((int64_t)TILE, a.padded_rows - r0);
-    T *to = static_cast<T *>(a.dt) + c0 * a.padded_rows + r0;
-    write_transposed(tg, to, a.padded_rows, columns, padded);
-    write_transposed(tu, to + a.padded_hidden * a.padded_rows, a.padded_rows, columns, padded);
-}
-
 // ---- launches --------------------------------------------------------------------------------------------------------------------
-template <int TYPE, int BM, int BN, int WM, int WN, bool GATED> hipError_t product(ProductArgs a, hipStream_t s)
+template <int TYPE, int BM, int BN, int WM, int WN, int NS, bool AR, bool BR, int MODE> hipError_t product(ProductArgs a, hipStream_t s)
 {
+    constexpr int COLUMNS = MODE == GATED ? BN / 2 : BN;
     a.tiles_m = (a.m + BM - 1) / BM;
-    a.tiles_n = (a.n + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
-    return launch_kernel((product_kernel<TYPE, BM, BN, WM, WN, GATED>), dim3((unsigned)((a.tiles_m * a.tiles_n + 7) / 8 * 8), GATED ? 1 : a.batch), dim3(64 * WM * WN), 0, s, a);
+    a.tiles_n = (a.n + COLUMNS - 1) / COLUMNS;
+    const dim3 grid((unsigned)((a.tiles_m * a.tiles_n + 7) / 8 * 8), MODE == GATED ? 1 : a.batch, MODE == PARTIAL ? a.splits : 1);
+    return launch_kernel((product_kernel<TYPE, BM, BN, WM, WN, NS, AR, BR, MODE>), grid, dim3(64 * WM * WN), 0, s, a);
 }
 
-template <int TYPE, bool GATED> hipError_t product_of(const ProductArgs &a, hipStream_t s)
+template <int TYPE, bool AR, bool BR, int MODE> hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t s)
 {
-    const int64_t tiles = (int64_t)((a.m + 255) / 256) * ((a.n + (GATED ? 127 : 255)) / (GATED ? 128 : 256)) * (GATED ? 1 : a.batch);
-    if (tiles >= 192) return product<TYPE, 256, 256, 2, 4, GATED>(a, s);
-    return product<TYPE, 128, 128, 2, 2, GATED>(a, s);
+    if (tile == 256) return product<TYPE, 256, 256, 2, 4, 2, AR, BR, MODE>(a, s);
+    if (tile == 128) return product<TYPE, 128, 128, 2, 2, 2, AR, BR, MODE>(a, s);
+    return product<TYPE, 64, 64, 2, 2, 3, AR, BR, MODE>(a, s);
+}
+
+template <int TYPE, bool AR> hipError_t product_plain(ProductArgs a, ProductPlan p, hipStream_t s)
+{
+    a.splits = p.splits;
+    if (p.splits == 1) return product_tile<TYPE, AR, true, PLAIN>(a, p.tile, s);
+    const hipError_t e = product_tile<TYPE, AR, true, PARTIAL>(a, p.tile, s);
+    if (e != hipSuccess) return e;
+    const int64_t threads = (int64_t)a.batch * a.m * ((a.n + 3) / 4);
+    return launch_kernel(product_join_kernel<TYPE>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
 }
 
 template <int TYPE, int MT> hipError_t few_rows(const FewRowsArgs &a, hipStream_t s)
@@ -396,13 +487,37 @@ template <int TYPE> hipError_t few_rows_of(const FewRowsArgs &a, hipStream_t s)
 
 } // namespace
 
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type type, bool gated)
+{
+    // What a compute unit takes for a step of 128 bytes of each tile, and workgroups that it runs at once
+    struct Shape { int tile; double cost; };
+    const Shape shapes[3] = {{256, type == MC_F32 ? 16.0 : 16.0}, {128, type == MC_F32 ? 4.0 : 4.8}, {64, type == MC_F32 ? 1.05 : 1.8}};
+    const int64_t size = type == MC_F32 ? 4 : 2, steps = (k * size + STEP - 1) / STEP;
+    ProductPlan best = {256, 1};
+    double least = 1e30;
+    for (const Shape &s : shapes) {
+        const int64_t tiles = (m + s.tile - 1) / s.tile * ((n * (gated ? 2 : 1) + s.tile - 1) / s.tile) * batch;
+        for (int splits = 1; splits <= (gated ? 1 : 16); ++splits) {
+            if (splits > 1 && (steps / splits < 8 || tiles * splits > 4096)) break;
+            const double rounds = (double)((tiles * splits + 255) / 256);
+            double cost = rounds * s.cost * ((double)(steps + splits - 1) / splits + 3);
+            if (splits > 1) cost += 12 + (splits + 1) * (double)(m * n * batch) * 4 / 4e5; // (the join: a launch, and its bytes)
+            if (cost < least) least = cost, best = {s.tile, splits};
+        }
+    }
+    return best;
+}
+
 hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s)
 {
-    return type == MC_F32 ? product_of<MC_F32, true>(a, s) : type == MC_F16 ? product_of<MC_F16, true>(a, s) : product_of<MC_BF16, true>(a, s);
+    const int tile = product_plan(a.m, a.n, a.k, 1, type, true).tile;
+    return type == MC_F32 ? product_tile<MC_F32, false, false, GATED>(a, tile, s)
+         : type == MC_F16 ? product_tile<MC_F16, false, false, GATED>(a, tile, s) : product_tile<MC_BF16, false, false, GATED>(a, tile, s);
 }
-hipError_t launch_product(const ProductArgs &a, mc_type type, hipStream_t s)
+hipError_t launch_product(const ProductArgs &a, ProductPlan p, bool a_rows, mc_type type, hipStream_t s)
 {
-    return type == MC_F32 ? product_of<MC_F32, false>(a, s) : type == MC_F16 ? product_of<MC_F16, false>(a, s) : product_of<MC_BF16, false>(a, s);
+    if (a_rows) return type == MC_F32 ? product_plain<MC_F32, true>(a, p, s) : type == MC_F16 ? product_plain<MC_F16, true>(a, p, s) : product_plain<MC_BF16, true>(a, p, s);
+    return type == MC_F32 ? product_plain<MC_F32, false>(a, p, s) : type == MC_F16 ? product_plain<MC_F16, false>(a, p, s) : product_plain<MC_BF16, false>(a, p, s);
 }
 hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s)
 {
@@ -410,7 +525,8 @@ hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s)
 }
 hipError_t launch_gated_grad(const GatedGradArgs &a, mc_type type, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.padded_hidden + TILE - 1) / TILE), (unsigned)((a.padded_rows + TILE - 1) / TILE)), block(256);
+    const int64_t blocks = (a.rows * ((a.padded_hidden + 7) / 8) + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384)), block(256);
     return type == MC_F32 ? launch_kernel(gated_grad_kernel<MC_F32>, grid, block, 0, s, a)
          : type == MC_F16 ? launch_kernel(gated_grad_kernel<MC_F16>, grid, block, 0, s, a) : launch_kernel(gated_grad_kernel<MC_BF16>, grid, block, 0, s, a);
 }
@@ -420,10 +536,4 @@ hipError_t launch_pad_rows(const void *from, int64_t from_stride, int64_t rows, 
     const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(256);
     if (size == 4) return launch_kernel(pad_rows_kernel<uint32_t>, grid, block, 0, s, static_cast<const uint32_t *>(from), from_stride, rows, width, static_cast<uint32_t *>(to), padded);
     return launch_kernel(pad_rows_kernel<uint16_t>, grid, block, 0, s, static_cast<const uint16_t *>(from), from_stride, rows, width, static_cast<uint16_t *>(to), padded);
-}
-hipError_t launch_transpose(const void *from, int64_t from_stride, int64_t rows, int columns, void *to, int64_t to_stride, int64_t padded, int size, hipStream_t s)
-{
-    const dim3 grid((unsigned)((columns + TILE - 1) / TILE), (unsigned)((padded + TILE - 1) / TILE)), block(256);
-    if (size == 4) return launch_kernel(transpose_kernel<uint32_t>, grid, block, 0, s, static_cast<const uint32_t *>(from), from_stride, rows, columns, static_cast<uint32_t *>(to), to_stride, padded);
-    return launch_kernel(transpose_kernel<uint16_t>, grid, block, 0, s, static_cast<const uint16_t *>(from), from_stride, rows, columns, static_cast<uint16_t *>(to), to_stride, padded);
 }

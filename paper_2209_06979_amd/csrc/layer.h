@@ -79,47 +79,51 @@ hipError_t launch_token_logprobs(const LogprobArgs &a, hipStream_t s);
 hipError_t launch_token_logprobs_backward(const LogprobArgs &a, hipStream_t s);
 
 // ---- the gated feed-forward block (gated_ffn_kernels.hip) ------------------------------------------------------------------
-// A product of two operands whose rows run along the reduction: C[m][n] = sum over k of A[m][k] B[n][k].  Rows begin at multiples of 16 bytes
-// and k is whole pieces of 16 bytes.
+// C[m][n] = sum over k of A(m, k) B(n, k).  An operand lies with k along its rows (a row for each m or n), or with a row for each k
+// (the gradient's); rows begin at multiples of 16 bytes, and their elements are whole pieces of 16 bytes, zeros behind k where it runs along them.
 struct ProductArgs {
-    const void *a;
-    const void *b[2];              // gated: gate and up weights; else b[0]
+    const void *a[2], *b[2];       // gated: x, and gate and up weights.  Else: one, or a sum of two products
     int64_t a_stride, b_stride[2]; // bytes
-    int m, n, k;
-    // gated: h, and g and u if they are kept (null: not)
-    void *h, *g, *u;
+    int m, n, k;                   // k of each of the products of a sum
+    // gated: h, and g and u in fp32 if they are kept (null: not)
+    void *h;
+    float *g, *u;
     int64_t h_stride, saved_stride; // elements
     int activation;
-    // plain: products side by side, A's rows a_batch bytes apart, each with an output of its own
-    int batch;
-    int64_t a_batch;
+    // else
+    int sum;                       // products of a sum, 1 or 2
+    int batch;                     // or 2 products side by side: of a[0] and a[1] with b[0], into c[0] and c[1]
     void *c[2];
     int64_t c_stride[2];           // elements
+    float *partial;                // splits x batch x m x n, of products that are cut along k
     // filled by the launcher
-    int tiles_m, tiles_n;
+    int tiles_m, tiles_n, splits;
 };
 struct FewRowsArgs { // a few rows of x against both weights
     const void *x, *gate, *up;
     int64_t x_stride, gate_stride, up_stride; // elements
     int rows, dim, hidden, activation;
-    void *h, *g, *u;
+    void *h;
+    float *g, *u;
     int64_t h_stride, saved_stride;
 };
-struct GatedGradArgs { // dg and du from dh, g and u, as rows and as columns
-    const void *dh, *g, *u;
+struct GatedGradArgs { // dg and du from dh, g and u
+    const void *dh;
+    const float *g, *u;
     int64_t dh_stride, saved_stride; // elements
     int64_t rows;
     int hidden, activation;
-    void *d, *dt;                  // rows x 2 padded hidden; 2 padded hidden x padded rows
+    void *dg, *du;                 // rows x padded hidden, zeros behind hidden
     int padded_hidden;
-    int64_t padded_rows;
 };
 constexpr int FEW_ROWS = 64;
 hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s);
-hipError_t launch_product(const ProductArgs &a, mc_type type, hipStream_t s);
+// Shapes of a product's tiles, and pieces along k
+struct ProductPlan { int tile, splits; };
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type type, bool gated);
+// B has a row for each k, and so has A if a_rows
+hipError_t launch_product(const ProductArgs &a, ProductPlan p, bool a_rows, mc_type type, hipStream_t s);
 hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s);
 hipError_t launch_gated_grad(const GatedGradArgs &a, mc_type type, hipStream_t s);
 // rows of `width` elements (`size` bytes each) into rows of `padded` elements, zeros behind them
 hipError_t launch_pad_rows(const void *from, int64_t from_stride, int64_t rows, int width, void *to, int padded, int size, hipStream_t s);
-// to[c][r] = from[r][c] for c < columns, r < rows; zeros up to r < padded
-hipError_t launch_transpose(const void *from, int64_t from_stride, int64_t rows, int columns, void *to, int64_t to_stride, int64_t padded, int size, hipStream_t s);

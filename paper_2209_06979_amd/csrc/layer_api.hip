@@ -106,17 +106,31 @@ FfnPlan ffn_plan(const mc_gated_ffn_args *f)
     return p;
 }
 
-struct FfnGradPlan { int hidden, rows; size_t d, dt, wt, xt, bytes; }; // padded sizes, offsets
+// The gradient's operands and copies: offsets, and the products' plans
+struct FfnGradPlan {
+    int hidden;                    // padded
+    ProductPlan dx, dw;
+    bool pad_x, pad_gate, pad_up;
+    size_t dg, du, x, gate, up, partial, bytes;
+};
 FfnGradPlan ffn_grad_plan(const mc_gated_ffn_args *f)
 {
     FfnGradPlan p = {};
-    const size_t size = size_of(f->type);
+    const size_t size = size_of(f->type), line = (size_t)pieces_up(f->dim, f->type) * size;
     p.hidden = pieces_up(f->hidden, f->type);
-    p.rows = pieces_up(f->rows, f->type);
-    p.dt = rounded(2 * (size_t)p.hidden * f->rows * size);
-    p.wt = p.dt + rounded(2 * (size_t)p.hidden * p.rows * size);
-    p.xt = p.wt + rounded(2 * (size_t)p.hidden * f->dim * size);
-    p.bytes = p.xt + rounded((size_t)f->dim * p.rows * size);
+    p.pad_x = !in_pieces(f->x_dev, f->x_stride, f->rows, f->dim, f->type);
+    p.pad_gate = !in_pieces(f->gate_dev, f->gate_stride, f->hidden, f->dim, f->type);
+    p.pad_up = !in_pieces(f->up_dev, f->up_stride, f->hidden, f->dim, f->type) || p.pad_gate || (f->hidden > 1 && f->up_stride != f->gate_stride);
+    p.pad_gate = p.pad_up;         // (both halves of a sum have one stride)
+    p.dx = product_plan(f->rows, f->dim, 2 * (int64_t)f->hidden, 1, f->type, false);
+    p.dw = product_plan(f->hidden, f->dim, f->rows, 2, f->type, false);
+    p.du = p.dg + rounded((size_t)p.hidden * f->rows * size);
+    p.x = p.du + rounded((size_t)p.hidden * f->rows * size);
+    p.gate = p.x + (p.pad_x ? rounded(f->rows * line) : 0);
+    p.up = p.gate + (p.pad_gate ? rounded(f->hidden * line) : 0);
+    p.partial = p.up + (p.pad_up ? rounded(f->hidden * line) : 0);
+    const size_t of_dx = p.dx.splits > 1 ? sizeof(float) * p.dx.splits * f->rows * f->dim : 0, of_dw = p.dw.splits > 1 ? sizeof(float) * 2 * p.dw.splits * f->hidden * f->dim : 0;
+    p.bytes = p.partial + rounded(of_dx > of_dw ? of_dx : of_dw);
     return p;
 }
 
@@ -171,14 +185,14 @@ extern "C" int mc_block_norm_backward(const mc_block_norm_args *args, const void
 
 extern "C" size_t mc_gated_ffn_workspace(const mc_gated_ffn_args *args) { return check_ffn(args) == MC_OK ? ffn_plan(args).bytes : 0; }
 
-extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t h_stride, void *g_dev, void *u_dev, int64_t saved_stride, void *workspace_dev,
+extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t h_stride, float *g_dev, float *u_dev, int64_t saved_stride, void *workspace_dev,
                             size_t workspace_bytes, void *stream)
 {
     if (const int rc = check_ffn(args)) return rc;
     const mc_gated_ffn_args &f = *args;
     if (f.rows == 0) return MC_OK;
     if (!rows_ok(h_dev, h_stride, f.rows, f.hidden, f.type) || !g_dev != !u_dev ||
-        (g_dev && (!rows_ok(g_dev, saved_stride, f.rows, f.hidden, f.type) || !rows_ok(u_dev, saved_stride, f.rows, f.hidden, f.type))))
+        (g_dev && (!rows_ok(g_dev, saved_stride, f.rows, f.hidden, MC_F32) || !rows_ok(u_dev, saved_stride, f.rows, f.hidden, MC_F32))))
         return MC_EINVAL;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const FfnPlan p = ffn_plan(args);
@@ -195,11 +209,11 @@ extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t 
     char *const ws = static_cast<char *>(workspace_dev);
     const int size = size_of(f.type), padded = pieces_up(f.dim, f.type);
     ProductArgs a = {};
-    a.a = f.x_dev; a.b[0] = f.gate_dev; a.b[1] = f.up_dev;
+    a.a[0] = f.x_dev; a.b[0] = f.gate_dev; a.b[1] = f.up_dev;
     a.a_stride = f.x_stride * size; a.b_stride[0] = f.gate_stride * size; a.b_stride[1] = f.up_stride * size;
     if (p.pad_x) {
         MC_HIP(launch_pad_rows(f.x_dev, f.x_stride, f.rows, f.dim, ws + p.x, padded, size, s));
-        a.a = ws + p.x; a.a_stride = (int64_t)padded * size;
+        a.a[0] = ws + p.x; a.a_stride = (int64_t)padded * size;
     }
     if (p.pad_gate) {
         MC_HIP(launch_pad_rows(f.gate_dev, f.gate_stride, f.hidden, f.dim, ws + p.gate, padded, size, s));
@@ -209,7 +223,7 @@ extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t 
         MC_HIP(launch_pad_rows(f.up_dev, f.up_stride, f.hidden, f.dim, ws + p.up, padded, size, s));
         a.b[1] = ws + p.up; a.b_stride[1] = (int64_t)padded * size;
     }
-    a.m = (int)f.rows; a.n = f.hidden; a.k = padded;
+    a.m = (int)f.rows; a.n = f.hidden; a.k = f.dim;
     a.h = h_dev; a.g = g_dev; a.u = u_dev; a.h_stride = h_stride; a.saved_stride = saved_stride; a.activation = f.activation;
     MC_HIP(launch_gated_product(a, f.type, s));
     return MC_OK;
@@ -217,14 +231,14 @@ extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t 
 
 extern "C" size_t mc_gated_ffn_backward_workspace(const mc_gated_ffn_args *args) { return check_ffn(args) == MC_OK ? ffn_grad_plan(args).bytes : 0; }
 
-extern "C" int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int64_t dh_stride, const void *g_dev, const void *u_dev, int64_t saved_stride,
+extern "C" int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int64_t dh_stride, const float *g_dev, const float *u_dev, int64_t saved_stride,
                                      void *dx_dev, int64_t dx_stride, void *dgate_dev, int64_t dgate_stride, void *dup_dev, int64_t dup_stride,
                                      void *workspace_dev, size_t workspace_bytes, void *stream)
 {
     if (const int rc = check_ffn(args)) return rc;
     const mc_gated_ffn_args &f = *args;
-    if ((f.rows > 0 && (!rows_ok(dh_dev, dh_stride, f.rows, f.hidden, f.type) || !rows_ok(g_dev, saved_stride, f.rows, f.hidden, f.type) ||
-                        !rows_ok(u_dev, saved_stride, f.rows, f.hidden, f.type))) ||
+    if ((f.rows > 0 && (!rows_ok(dh_dev, dh_stride, f.rows, f.hidden, f.type) || !rows_ok(g_dev, saved_stride, f.rows, f.hidden, MC_F32) ||
+                        !rows_ok(u_dev, saved_stride, f.rows, f.hidden, MC_F32))) ||
         (dx_dev && !rows_ok(dx_dev, dx_stride, f.rows, f.dim, f.type)) || (dgate_dev && !rows_ok(dgate_dev, dgate_stride, f.hidden, f.dim, f.type)) ||
         (dup_dev && !rows_ok(dup_dev, dup_stride, f.hidden, f.dim, f.type)))
         return MC_EINVAL;
@@ -233,32 +247,39 @@ extern "C" int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *
     const hipStream_t s = static_cast<hipStream_t>(stream);
     char *const ws = static_cast<char *>(workspace_dev);
     const int size = size_of(f.type);
-    const int64_t line = 2 * (int64_t)p.hidden; // elements of a row of d and of the weights' transpose
+    const int padded = pieces_up(f.dim, f.type);
     const bool weights = dgate_dev || dup_dev;
     if (f.rows > 0) {
         GatedGradArgs a = {};
         a.dh = dh_dev; a.g = g_dev; a.u = u_dev; a.dh_stride = dh_stride; a.saved_stride = saved_stride;
         a.rows = f.rows; a.hidden = f.hidden; a.activation = f.activation;
-        a.d = dx_dev ? ws + p.d : nullptr; a.dt = weights ? ws + p.dt : nullptr;
-        a.padded_hidden = p.hidden; a.padded_rows = p.rows;
+        a.dg = ws + p.dg; a.du = ws + p.du; a.padded_hidden = p.hidden;
         MC_HIP(launch_gated_grad(a, f.type, s));
     }
-    if (dx_dev && f.rows > 0) {
-        MC_HIP(launch_transpose(f.gate_dev, f.gate_stride, f.hidden, f.dim, ws + p.wt, line, p.hidden, size, s));
-        MC_HIP(launch_transpose(f.up_dev, f.up_stride, f.hidden, f.dim, ws + p.wt + (size_t)p.hidden * size, line, p.hidden, size, s));
-        ProductArgs a = {};
-        a.a = ws + p.d; a.b[0] = ws + p.wt; a.a_stride = a.b_stride[0] = line * size;
-        a.m = (int)f.rows; a.n = f.dim; a.k = (int)line; a.batch = 1;
+    ProductArgs a = {};
+    a.a[0] = ws + p.dg; a.a[1] = ws + p.du; a.a_stride = (int64_t)p.hidden * size;
+    a.n = f.dim; a.partial = reinterpret_cast<float *>(ws + p.partial);
+    if (dx_dev && f.rows > 0) { // a sum of two products; the weights have a row for each k
+        a.b[0] = f.gate_dev; a.b[1] = f.up_dev; a.b_stride[0] = f.gate_stride * size;
+        if (p.pad_gate) {
+            MC_HIP(launch_pad_rows(f.gate_dev, f.gate_stride, f.hidden, f.dim, ws + p.gate, padded, size, s));
+            MC_HIP(launch_pad_rows(f.up_dev, f.up_stride, f.hidden, f.dim, ws + p.up, padded, size, s));
+            a.b[0] = ws + p.gate; a.b[1] = ws + p.up; a.b_stride[0] = (int64_t)padded * size;
+        }
+        a.m = (int)f.rows; a.k = f.hidden; a.sum = 2; a.batch = 1;
         a.c[0] = dx_dev; a.c_stride[0] = dx_stride;
-        MC_HIP(launch_product(a, f.type, s));
+        MC_HIP(launch_product(a, p.dx, false, f.type, s));
     }
-    if (weights) {
-        if (f.rows > 0) MC_HIP(launch_transpose(f.x_dev, f.x_stride, f.rows, f.dim, ws + p.xt, p.rows, p.rows, size, s));
-        ProductArgs a = {};
-        a.a = ws + p.dt + (dgate_dev ? 0 : (size_t)p.hidden * p.rows * size); a.b[0] = ws + p.xt; a.a_stride = a.b_stride[0] = (int64_t)p.rows * size;
-        a.m = f.hidden; a.n = f.dim; a.k = p.rows; a.batch = dgate_dev && dup_dev ? 2 : 1; a.a_batch = (int64_t)p.hidden * p.rows * size;
+    if (weights) { // two products with x; rows of both operands are k
+        a.b[0] = f.x_dev; a.b_stride[0] = f.x_stride * size;
+        if (p.pad_x && f.rows > 0) {
+            MC_HIP(launch_pad_rows(f.x_dev, f.x_stride, f.rows, f.dim, ws + p.x, padded, size, s));
+            a.b[0] = ws + p.x; a.b_stride[0] = (int64_t)padded * size;
+        }
+        if (!dgate_dev) a.a[0] = a.a[1];
+        a.m = f.hidden; a.k = (int)f.rows; a.sum = 1; a.batch = dgate_dev && dup_dev ? 2 : 1;
         a.c[0] = dgate_dev ? dgate_dev : dup_dev; a.c_stride[0] = dgate_dev ? dgate_stride : dup_stride; a.c[1] = dup_dev; a.c_stride[1] = dup_stride;
-        MC_HIP(launch_product(a, f.type, s));
+        MC_HIP(launch_product(a, p.dw, true, f.type, s));
     }
     return MC_OK;
 }

@@ -1182,7 +1182,7 @@ PyObject *gated_ffn_call(PyObject *const *v, bool keep)
         pybind11::gil_scoped_release nogil;
         const int64_t hidden = gate->size(0);
         for (int i = 0; i < 3; ++i)
-            if (i ? keep : !out) made[i] = empty({x->size(0), hidden}, x->scalar_type(), *x);
+            if (i ? keep : !out) made[i] = empty({x->size(0), hidden}, i ? at::kFloat : x->scalar_type(), *x);
         void *w = nullptr;
         size_t bytes = 0;
         if (ws) {
@@ -1192,8 +1192,8 @@ PyObject *gated_ffn_call(PyObject *const *v, bool keep)
             scratch = empty({(int64_t)bytes}, at::kByte, *x);
             w = scratch.data_ptr();
         }
-        rc = mc_gated_ffn(&f, out ? out->data_ptr() : made[0].data_ptr(), out ? row_stride(*out) : hidden, keep ? made[1].data_ptr() : nullptr,
-                          keep ? made[2].data_ptr() : nullptr, hidden, w, bytes, stream());
+        rc = mc_gated_ffn(&f, out ? out->data_ptr() : made[0].data_ptr(), out ? row_stride(*out) : hidden, keep ? static_cast<float *>(made[1].data_ptr()) : nullptr,
+                          keep ? static_cast<float *>(made[2].data_ptr()) : nullptr, hidden, w, bytes, stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_gated_ffn");
     if (keep) return tuple_of(made);
@@ -1232,7 +1232,8 @@ PyObject *gated_ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
     int wanted;
     if (!ffn_args(v, &x, &gate, &up, &f) || !(dh = tensor(v[4])) || !(g = tensor(v[5])) || !(u = tensor(v[6])) || !integer(v[7], 0, &wanted)) return nullptr;
     for (const at::Tensor *t : {dh, g, u})
-        if (!(rows_of(*t) && t->device() == x->device() && t->scalar_type() == x->scalar_type() && t->size(0) == x->size(0) && t->size(1) == gate->size(0))) return assertion();
+        if (!(rows_of(*t) && t->device() == x->device() && t->scalar_type() == (t == dh ? x->scalar_type() : at::kFloat) && t->size(0) == x->size(0) && t->size(1) == gate->size(0)))
+            return assertion();
     if (row_stride(*g) != row_stride(*u)) return assertion();
     at::TensorBase made[3], scratch;
     int rc;
@@ -1247,7 +1248,7 @@ PyObject *gated_ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
             }
         const size_t bytes = mc_gated_ffn_backward_workspace(&f);
         if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *x);
-        rc = mc_gated_ffn_backward(&f, dh->data_ptr(), row_stride(*dh), g->data_ptr(), u->data_ptr(), row_stride(*g), to[0], f.dim, to[1], f.dim, to[2], f.dim,
+        rc = mc_gated_ffn_backward(&f, dh->data_ptr(), row_stride(*dh), static_cast<const float *>(g->data_ptr()), static_cast<const float *>(u->data_ptr()), row_stride(*g), to[0], f.dim, to[1], f.dim, to[2], f.dim,
                                    bytes ? scratch.data_ptr() : nullptr, bytes, stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_gated_ffn_backward");

@@ -139,8 +139,8 @@ def gated_ffn(x, w_gate, w_up, act, dh=None):
     if dh is None:
         return out
     dh = dh.detach().double().cpu()
-    # g and u are kept rounded, dg and du are rounded before the products
-    keptg, keptu = offg + half * (g.abs() + offg) + TINY[kind], offu + half * (u.abs() + offu) + TINY[kind]
+    # dg and du are rounded before the products
+    keptg, keptu = offg, offu
     offs = 1.1 * keptg + 16 * F * (1 + g.abs())
     if act == "relu":
         offs = (g.abs() <= keptg).double()                          # the slope's step
