@@ -15,62 +15,75 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 // ---- activations ----------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + expf(-g)); }
+// The hardware's exponential and reciprocal, each within a step or two: of a sigmoid some |g| 2^-23 of itself where it is small.  (With the
+// library's exponential and quotient the activation of a 256 x 128 tile took as long as a seventh of its products.)
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)); }
 constexpr float GELU_A = 0.7978845608028654f, GELU_B = 0.044715f;
 
-__device__ __forceinline__ float activated(float g, int kind)
+template <int KIND> __device__ __forceinline__ float activated(float g)
 {
-    switch (kind) {
-    case MC_ACT_SILU: return g / (1.0f + expf(-g));
-    case MC_ACT_GELU: return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
-    case MC_ACT_GELU_TANH: return 0.5f * g * (1.0f + tanhf(GELU_A * (g + GELU_B * g * g * g)));
-    case MC_ACT_RELU: return g > 0 ? g : g != g ? g : 0;
-    default: return sigmoid(g);
-    }
+    if constexpr (KIND == MC_ACT_SILU) return g * sigmoid(g);
+    else if constexpr (KIND == MC_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
+    else if constexpr (KIND == MC_ACT_GELU_TANH) return g * sigmoid(2.0f * GELU_A * (g + GELU_B * g * g * g)); // ((1 + tanh v) / 2 is sigmoid 2 v)
+    else if constexpr (KIND == MC_ACT_RELU) return g > 0 ? g : g != g ? g : 0;
+    else return sigmoid(g);
 }
 // act(g), and its slope
-__device__ __forceinline__ float activated(float g, int kind, float &slope)
+template <int KIND> __device__ __forceinline__ float activated(float g, float &slope)
 {
-    switch (kind) {
-    case MC_ACT_SILU: {
+    if constexpr (KIND == MC_ACT_SILU) {
         const float p = sigmoid(g);
         slope = p * (1.0f + g * (1.0f - p));
         return g * p;
-    }
-    case MC_ACT_GELU: {
+    } else if constexpr (KIND == MC_ACT_GELU) {
         const float c = 0.5f * (1.0f + erff(g * 0.7071067811865476f));
-        slope = c + g * expf(-0.5f * g * g) * 0.3989422804014327f;
+        slope = c + g * __builtin_amdgcn_exp2f(g * g * -0.7213475204444817f) * 0.3989422804014327f;
         return g * c;
-    }
-    case MC_ACT_GELU_TANH: {
-        const float t = tanhf(GELU_A * (g + GELU_B * g * g * g));
-        slope = 0.5f * (1.0f + t) + 0.5f * g * (1.0f - t * t) * GELU_A * (1.0f + 3.0f * GELU_B * g * g);
-        return 0.5f * g * (1.0f + t);
-    }
-    case MC_ACT_RELU:
+    } else if constexpr (KIND == MC_ACT_GELU_TANH) {
+        const float p = sigmoid(2.0f * GELU_A * (g + GELU_B * g * g * g));
+        slope = p + p * (1.0f - p) * 2.0f * GELU_A * (g + 3.0f * GELU_B * g * g * g);
+        return g * p;
+    } else if constexpr (KIND == MC_ACT_RELU) {
         slope = g > 0 ? 1 : g != g ? g : 0;
         return g > 0 ? g : g != g ? g : 0;
-    default: {
+    } else {
         const float p = sigmoid(g);
         slope = p * (1.0f - p);
         return p;
     }
+}
+// f with the activation as a constant
+template <class F> __device__ __forceinline__ void with_activation(int kind, F &&f)
+{
+    switch (kind) {
+    case MC_ACT_SILU: return f(std::integral_constant<int, MC_ACT_SILU>{});
+    case MC_ACT_GELU: return f(std::integral_constant<int, MC_ACT_GELU>{});
+    case MC_ACT_GELU_TANH: return f(std::integral_constant<int, MC_ACT_GELU_TANH>{});
+    case MC_ACT_RELU: return f(std::integral_constant<int, MC_ACT_RELU>{});
+    default: return f(std::integral_constant<int, MC_ACT_SIGMOID>{});
     }
 }
 
 // ---- matrix instructions ----------------------------------------------------------------------------------------------------
 // 16 rows of either operand, 16 bytes of each along k: a lane holds piece lane / 16 of row lane % 16.  (fp32: element e of the four pieces are
 // the four k of instruction e.)  The result has 4 rows of the first, 4 (lane / 16) + i, for row lane % 16 of the second.
-template <int TYPE> __device__ __forceinline__ v4f multiply(const v4i &a, const v4i &b, v4f c)
+template <int TYPE, int N, int M> __device__ __forceinline__ void multiply(const v4i (&a)[N], const v4i (&b)[M], v4f (&c)[N][M])
 {
     if constexpr (TYPE == MC_F32) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[e]), __int_as_float(b[e]), c, 0, 0, 0);
-        return c;
-    } else if constexpr (TYPE == MC_F16) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) // (an instruction's sum is the next one's after all others)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int m = 0; m < M; ++m) c[n][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[n][e]), __int_as_float(b[m][e]), c[n][m], 0, 0, 0);
     } else {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                if constexpr (TYPE == MC_F16) c[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a[n]), __builtin_bit_cast(v8h, b[m]), c[n][m], 0, 0, 0);
+                else c[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a[n]), __builtin_bit_cast(v8bf, b[m]), c[n][m], 0, 0, 0);
+            }
     }
 }
 
@@ -251,38 +264,42 @@ template <int TYPE, int BM, int BN, int WM, int WN, int NS, bool AR, bool BR, in
             for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
 #pragma unroll
             for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
-#pragma unroll
-            for (int n = 0; n < NF; ++n)
-#pragma unroll
-                for (int m = 0; m < MF; ++m) acc[n][m] = multiply<TYPE>(fb[n], fa[m], acc[n][m]);
+            multiply<TYPE>(fb, fa, acc);
         }
         mcu::lgkm_wait();
     }
 
+    if constexpr (MODE == GATED) {
+        constexpr int RUN = EIGHT ? 8 : 4, FS = RUN / 4;
+        with_activation(a.activation, [&](auto kind) {
 #pragma unroll
-    for (int m = 0; m < MF; ++m) {
-        const int row = m0 + wm * RM + m * 16 + (lane & 15);
-        if (row >= a.m) continue;
-        if constexpr (MODE == GATED) {
-            constexpr int RUN = EIGHT ? 8 : 4, FS = RUN / 4;
+            for (int m = 0; m < MF; ++m) {
+                const int row = m0 + wm * RM + m * 16 + (lane & 15);
+                if (row >= a.m) continue;
 #pragma unroll
-            for (int n = 0; n < NF / 2; n += FS) {
-                const int column = n0 + wn * (RN / 2) + n * 16 + RUN * (lane >> 4), count = a.n - column;
-                if (count <= 0) continue;
-                float h[RUN], g[RUN], u[RUN];
+                for (int n = 0; n < NF / 2; n += FS) {
+                    const int column = n0 + wn * (RN / 2) + n * 16 + RUN * (lane >> 4), count = a.n - column;
+                    if (count <= 0) continue;
+                    float h[RUN], g[RUN], u[RUN];
 #pragma unroll
-                for (int e = 0; e < RUN; ++e) {
-                    g[e] = acc[n + e / 4][m][e % 4];
-                    u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
-                    h[e] = activated(g[e], a.activation) * u[e];
-                }
-                store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
-                if (a.g) {
-                    store_run(a.g + row * a.saved_stride + column, g, count);
-                    store_run(a.u + row * a.saved_stride + column, u, count);
+                    for (int e = 0; e < RUN; ++e) {
+                        g[e] = acc[n + e / 4][m][e % 4];
+                        u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
+                        h[e] = activated<decltype(kind)::value>(g[e]) * u[e];
+                    }
+                    store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
+                    if (a.g) {
+                        store_run(a.g + row * a.saved_stride + column, g, count);
+                        store_run(a.u + row * a.saved_stride + column, u, count);
+                    }
                 }
             }
-        } else {
+        });
+    } else {
+#pragma unroll
+        for (int m = 0; m < MF; ++m) {
+            const int row = m0 + wm * RM + m * 16 + (lane & 15);
+            if (row >= a.m) continue;
 #pragma unroll
             for (int n = 0; n < NF; ++n) {
                 const int column = n0 + wn * RN + n * 16 + 4 * (lane >> 4), count = a.n - column;
@@ -343,40 +360,36 @@ template <int TYPE, int MT> __global__ __launch_bounds__(64 * FEW_WAVES) void fe
     const T *px[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) px[m] = static_cast<const T *>(a.x) + (int64_t)min(m * 16 + r, a.rows - 1) * a.x_stride;
-    v4f g[MT], u[MT];
+    v4f acc[2][MT]; // of gate and up
 #pragma unroll
-    for (int m = 0; m < MT; ++m) g[m] = u[m] = (v4f){0, 0, 0, 0};
+    for (int m = 0; m < MT; ++m) acc[0][m] = acc[1][m] = (v4f){0, 0, 0, 0};
     int k = w * TAKE * UNROLL;
     for (; k + TAKE * UNROLL <= a.dim; k += FEW_WAVES * TAKE * UNROLL) {
-        v4i fg[UNROLL], fu[UNROLL];
+        v4i fw[UNROLL][2];
 #pragma unroll
         for (int i = 0; i < UNROLL; ++i) {
-            __builtin_memcpy(&fg[i], pg + k + i * TAKE + q * PER, 16);
-            __builtin_memcpy(&fu[i], pu + k + i * TAKE + q * PER, 16);
+            __builtin_memcpy(&fw[i][0], pg + k + i * TAKE + q * PER, 16);
+            __builtin_memcpy(&fw[i][1], pu + k + i * TAKE + q * PER, 16);
         }
 #pragma unroll
-        for (int i = 0; i < UNROLL; ++i)
+        for (int i = 0; i < UNROLL; ++i) {
+            v4i fx[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                v4i fx;
-                __builtin_memcpy(&fx, px[m] + k + i * TAKE + q * PER, 16);
-                g[m] = multiply<TYPE>(fg[i], fx, g[m]);
-                u[m] = multiply<TYPE>(fu[i], fx, u[m]);
-            }
+            for (int m = 0; m < MT; ++m) __builtin_memcpy(&fx[m], px[m] + k + i * TAKE + q * PER, 16);
+            multiply<TYPE>(fw[i], fx, acc);
+        }
     }
     for (int i = 0; i < UNROLL && k + i * TAKE < a.dim; ++i) { // what is left, fewer than UNROLL
         const int at = k + i * TAKE + q * PER, count = a.dim - at;
-        const v4i fg = load_piece(pg + at, count), fu = load_piece(pu + at, count);
+        const v4i fw[2] = {load_piece(pg + at, count), load_piece(pu + at, count)};
+        v4i fx[MT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const v4i fx = load_piece(px[m] + at, count);
-            g[m] = multiply<TYPE>(fg, fx, g[m]);
-            u[m] = multiply<TYPE>(fu, fx, u[m]);
-        }
+        for (int m = 0; m < MT; ++m) fx[m] = load_piece(px[m] + at, count);
+        multiply<TYPE>(fw, fx, acc);
     }
     __shared__ v4f sums[FEW_WAVES][2][MT][64];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) sums[w][0][m][lane] = g[m], sums[w][1][m][lane] = u[m];
+    for (int m = 0; m < MT; ++m) sums[w][0][m][lane] = acc[0][m], sums[w][1][m][lane] = acc[1][m];
     __syncthreads();
     for (int m = w; m < MT; m += FEW_WAVES) {
         v4f sg = sums[0][0][m][lane], su = sums[0][1][m][lane];
@@ -386,11 +399,11 @@ template <int TYPE, int MT> __global__ __launch_bounds__(64 * FEW_WAVES) void fe
         if (row >= a.rows || count <= 0) continue;
         float h[4], gs[4], us[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            gs[e] = sg[e];
-            us[e] = su[e];
-            h[e] = activated(gs[e], a.activation) * us[e];
-        }
+        for (int e = 0; e < 4; ++e) gs[e] = sg[e], us[e] = su[e];
+        with_activation(a.activation, [&](auto kind) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = activated<decltype(kind)::value>(gs[e]) * us[e];
+        });
         store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
         if (a.g) {
             store_run(a.g + row * a.saved_stride + column, gs, count);
@@ -426,24 +439,32 @@ template <int TYPE> __global__ __launch_bounds__(256) void gated_grad_kernel(Gat
                 us[e] = e < count ? u[e] : 0;
             }
         }
+        with_activation(a.activation, [&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float slope;
-            const float act = activated(gs[e], a.activation, slope);
-            du[e] = (float)d[e] * act;
-            dg[e] = (float)d[e] * us[e] * slope;
-        }
+            for (int e = 0; e < 8; ++e) {
+                float slope;
+                const float act = activated<decltype(kind)::value>(gs[e], slope);
+                du[e] = (float)d[e] * act;
+                dg[e] = (float)d[e] * us[e] * slope;
+            }
+        });
         store_run(static_cast<T *>(a.dg) + row * a.padded_hidden + column, dg, a.padded_hidden - column);
         store_run(static_cast<T *>(a.du) + row * a.padded_hidden + column, du, a.padded_hidden - column);
     }
 }
 
-template <class T> __global__ __launch_bounds__(256) void pad_rows_kernel(const T *from, int64_t from_stride, int64_t rows, int width, T *to, int padded)
+// Matrices whose rows are no whole pieces of 16 bytes, copied into such that are: a piece to a thread.
+template <class T> __global__ __launch_bounds__(256) void pad_rows_kernel(PadRowsArgs a)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * padded; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / padded;
-        const int c = (int)(i - r * padded);
-        to[i] = c < width ? from[r * from_stride + c] : (T)0;
+    constexpr int PER = 16 / sizeof(T);
+    const PadRowsArgs::Matrix &m = a.matrix[blockIdx.y];
+    const unsigned pieces = a.padded / PER, stride = gridDim.x * 256;
+    const int64_t all = m.rows * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += stride) {
+        const int64_t row = all < 0xffffffffll ? (int64_t)((unsigned)i / pieces) : i / pieces;
+        const int column = (int)(i - row * pieces) * PER;
+        const v4i v = load_piece(static_cast<const T *>(m.from) + row * m.stride + column, a.width - column);
+        __builtin_memcpy(static_cast<T *>(m.to) + row * a.padded + column, &v, 16);
     }
 }
 
@@ -530,10 +551,11 @@ hipError_t launch_gated_grad(const GatedGradArgs &a, mc_type type, hipStream_t s
     return type == MC_F32 ? launch_kernel(gated_grad_kernel<MC_F32>, grid, block, 0, s, a)
          : type == MC_F16 ? launch_kernel(gated_grad_kernel<MC_F16>, grid, block, 0, s, a) : launch_kernel(gated_grad_kernel<MC_BF16>, grid, block, 0, s, a);
 }
-hipError_t launch_pad_rows(const void *from, int64_t from_stride, int64_t rows, int width, void *to, int padded, int size, hipStream_t s)
+hipError_t launch_pad_rows(const PadRowsArgs &a, mc_type type, hipStream_t s)
 {
-    const int64_t blocks = (rows * padded + 1023) / 1024;
-    const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(256);
-    if (size == 4) return launch_kernel(pad_rows_kernel<uint32_t>, grid, block, 0, s, static_cast<const uint32_t *>(from), from_stride, rows, width, static_cast<uint32_t *>(to), padded);
-    return launch_kernel(pad_rows_kernel<uint16_t>, grid, block, 0, s, static_cast<const uint16_t *>(from), from_stride, rows, width, static_cast<uint16_t *>(to), padded);
+    int64_t most = 0;
+    for (int i = 0; i < a.count; ++i) most = a.matrix[i].rows > most ? a.matrix[i].rows : most;
+    const int64_t blocks = (most * (a.padded / (type == MC_F32 ? 4 : 8)) + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096), a.count), block(256);
+    return type == MC_F32 ? launch_kernel(pad_rows_kernel<uint32_t>, grid, block, 0, s, a) : launch_kernel(pad_rows_kernel<uint16_t>, grid, block, 0, s, a);
 }

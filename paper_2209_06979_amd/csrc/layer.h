@@ -116,6 +116,10 @@ struct GatedGradArgs { // dg and du from dh, g and u
     void *dg, *du;                 // rows x padded hidden, zeros behind hidden
     int padded_hidden;
 };
+struct PadRowsArgs { // rows of `width` elements into rows of `padded`, zeros behind them; up to three matrices
+    struct Matrix { const void *from; int64_t stride, rows; void *to; } matrix[3];
+    int count, width, padded;
+};
 constexpr int FEW_ROWS = 64;
 hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s);
 // Shapes of a product's tiles, and pieces along k
@@ -125,5 +129,4 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type typ
 hipError_t launch_product(const ProductArgs &a, ProductPlan p, bool a_rows, mc_type type, hipStream_t s);
 hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s);
 hipError_t launch_gated_grad(const GatedGradArgs &a, mc_type type, hipStream_t s);
-// rows of `width` elements (`size` bytes each) into rows of `padded` elements, zeros behind them
-hipError_t launch_pad_rows(const void *from, int64_t from_stride, int64_t rows, int width, void *to, int padded, int size, hipStream_t s);
+hipError_t launch_pad_rows(const PadRowsArgs &a, mc_type type, hipStream_t s);

@@ -90,6 +90,13 @@ inline bool in_pieces(const void *p, int64_t stride, int64_t rows, int width, in
     return aligned(p, 16) && (rows <= 1 || stride * size_of(type) % 16 == 0) && width * size_of(type) % 16 == 0;
 }
 
+// One more matrix to be copied
+void *padded_copy(PadRowsArgs &a, const void *from, int64_t stride, int64_t rows, void *to)
+{
+    a.matrix[a.count++] = {from, stride, rows, to};
+    return to;
+}
+
 struct FfnPlan { bool few, pad_x, pad_gate, pad_up; size_t x, gate, up, bytes; }; // offsets of the copies
 FfnPlan ffn_plan(const mc_gated_ffn_args *f)
 {
@@ -211,18 +218,12 @@ extern "C" int mc_gated_ffn(const mc_gated_ffn_args *args, void *h_dev, int64_t 
     ProductArgs a = {};
     a.a[0] = f.x_dev; a.b[0] = f.gate_dev; a.b[1] = f.up_dev;
     a.a_stride = f.x_stride * size; a.b_stride[0] = f.gate_stride * size; a.b_stride[1] = f.up_stride * size;
-    if (p.pad_x) {
-        MC_HIP(launch_pad_rows(f.x_dev, f.x_stride, f.rows, f.dim, ws + p.x, padded, size, s));
-        a.a[0] = ws + p.x; a.a_stride = (int64_t)padded * size;
-    }
-    if (p.pad_gate) {
-        MC_HIP(launch_pad_rows(f.gate_dev, f.gate_stride, f.hidden, f.dim, ws + p.gate, padded, size, s));
-        a.b[0] = ws + p.gate; a.b_stride[0] = (int64_t)padded * size;
-    }
-    if (p.pad_up) {
-        MC_HIP(launch_pad_rows(f.up_dev, f.up_stride, f.hidden, f.dim, ws + p.up, padded, size, s));
-        a.b[1] = ws + p.up; a.b_stride[1] = (int64_t)padded * size;
-    }
+    PadRowsArgs pads = {};
+    if (p.pad_x) a.a[0] = padded_copy(pads, f.x_dev, f.x_stride, f.rows, ws + p.x), a.a_stride = (int64_t)padded * size;
+    if (p.pad_gate) a.b[0] = padded_copy(pads, f.gate_dev, f.gate_stride, f.hidden, ws + p.gate), a.b_stride[0] = (int64_t)padded * size;
+    if (p.pad_up) a.b[1] = padded_copy(pads, f.up_dev, f.up_stride, f.hidden, ws + p.up), a.b_stride[1] = (int64_t)padded * size;
+    pads.width = f.dim; pads.padded = padded;
+    if (pads.count) MC_HIP(launch_pad_rows(pads, f.type, s));
     a.m = (int)f.rows; a.n = f.hidden; a.k = f.dim;
     a.h = h_dev; a.g = g_dev; a.u = u_dev; a.h_stride = h_stride; a.saved_stride = saved_stride; a.activation = f.activation;
     MC_HIP(launch_gated_product(a, f.type, s));
@@ -259,23 +260,23 @@ extern "C" int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *
     ProductArgs a = {};
     a.a[0] = ws + p.dg; a.a[1] = ws + p.du; a.a_stride = (int64_t)p.hidden * size;
     a.n = f.dim; a.partial = reinterpret_cast<float *>(ws + p.partial);
+    PadRowsArgs pads = {};
+    const void *x = f.x_dev, *gate = f.gate_dev, *up = f.up_dev;
+    if (weights && p.pad_x && f.rows > 0) x = padded_copy(pads, x, f.x_stride, f.rows, ws + p.x);
+    if (dx_dev && p.pad_gate && f.rows > 0) {
+        gate = padded_copy(pads, gate, f.gate_stride, f.hidden, ws + p.gate);
+        up = padded_copy(pads, up, f.up_stride, f.hidden, ws + p.up);
+    }
+    pads.width = f.dim; pads.padded = padded;
+    if (pads.count) MC_HIP(launch_pad_rows(pads, f.type, s));
     if (dx_dev && f.rows > 0) { // a sum of two products; the weights have a row for each k
-        a.b[0] = f.gate_dev; a.b[1] = f.up_dev; a.b_stride[0] = f.gate_stride * size;
-        if (p.pad_gate) {
-            MC_HIP(launch_pad_rows(f.gate_dev, f.gate_stride, f.hidden, f.dim, ws + p.gate, padded, size, s));
-            MC_HIP(launch_pad_rows(f.up_dev, f.up_stride, f.hidden, f.dim, ws + p.up, padded, size, s));
-            a.b[0] = ws + p.gate; a.b[1] = ws + p.up; a.b_stride[0] = (int64_t)padded * size;
-        }
+        a.b[0] = gate; a.b[1] = up; a.b_stride[0] = (p.pad_gate ? padded : f.gate_stride) * size;
         a.m = (int)f.rows; a.k = f.hidden; a.sum = 2; a.batch = 1;
         a.c[0] = dx_dev; a.c_stride[0] = dx_stride;
         MC_HIP(launch_product(a, p.dx, false, f.type, s));
     }
     if (weights) { // two products with x; rows of both operands are k
-        a.b[0] = f.x_dev; a.b_stride[0] = f.x_stride * size;
-        if (p.pad_x && f.rows > 0) {
-            MC_HIP(launch_pad_rows(f.x_dev, f.x_stride, f.rows, f.dim, ws + p.x, padded, size, s));
-            a.b[0] = ws + p.x; a.b_stride[0] = (int64_t)padded * size;
-        }
+        a.b[0] = x; a.b_stride[0] = (p.pad_x ? padded : f.x_stride) * size;
         if (!dgate_dev) a.a[0] = a.a[1];
         a.m = f.hidden; a.k = (int)f.rows; a.sum = 1; a.batch = dgate_dev && dup_dev ? 2 : 1;
         a.c[0] = dgate_dev ? dgate_dev : dup_dev; a.c_stride[0] = dgate_dev ? dgate_stride : dup_stride; a.c[1] = dup_dev; a.c_stride[1] = dup_stride;
