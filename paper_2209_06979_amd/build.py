@@ -25,11 +25,15 @@ FLAGS = [
     "-Wno-inline-asm",
 ]
 
+# Accumulators of 256 registers stay where they are only if the matrix instructions are chosen in their vector-register form first (in the
+# other form the compiler moves them between both register files, and spills).
+SOURCE_FLAGS = {"gated_ffn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def source_id() -> str:
     """Twelve hex digits that change with any source file or compiler flag of the library; mc_version() carries
     them, so that a stored profile can say which build it was taken from."""
-    h = hashlib.sha256(" ".join(FLAGS).encode())
+    h = hashlib.sha256(" ".join([*FLAGS, str(sorted(SOURCE_FLAGS.items()))]).encode())
     for name in sorted(os.listdir(CSRC)):
         if name.endswith((".hip", ".cpp", ".h")):
             with open(os.path.join(CSRC, name), "rb") as f:
@@ -48,7 +52,7 @@ def build_library(verbose: bool = False, jobs: int = 4) -> str:
     sid = source_id()
     for src in SOURCES:
         obj = os.path.join(objdir, os.path.splitext(src)[0] + ".o")
-        cmd = [hipcc, *FLAGS, *([f'-DMC_SOURCE_ID="{sid}"'] if src == "api.hip" else []),
+        cmd = [hipcc, *FLAGS, *SOURCE_FLAGS.get(src, []), *([f'-DMC_SOURCE_ID="{sid}"'] if src == "api.hip" else []),
                "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)

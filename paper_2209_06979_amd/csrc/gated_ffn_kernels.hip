@@ -67,6 +67,11 @@ template <class F> __device__ __forceinline__ void with_activation(int kind, F &
 // ---- matrix instructions ----------------------------------------------------------------------------------------------------
 // 16 rows of either operand, 16 bytes of each along k: a lane holds piece lane / 16 of row lane % 16.  (fp32: element e of the four pieces are
 // the four k of instruction e.)  The result has 4 rows of the first, 4 (lane / 16) + i, for row lane % 16 of the second.
+template <int TYPE> __device__ __forceinline__ v4f multiply_one(const v4i &a, const v4i &b, const v4f &c) // (16-bit types)
+{
+    if constexpr (TYPE == MC_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
 template <int TYPE, int N, int M> __device__ __forceinline__ void multiply(const v4i (&a)[N], const v4i (&b)[M], v4f (&c)[N][M])
 {
     if constexpr (TYPE == MC_F32) {
@@ -80,10 +85,7 @@ template <int TYPE, int N, int M> __device__ __forceinline__ void multiply(const
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int m = 0; m < M; ++m) {
-                if constexpr (TYPE == MC_F16) c[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a[n]), __builtin_bit_cast(v8h, b[m]), c[n][m], 0, 0, 0);
-                else c[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a[n]), __builtin_bit_cast(v8bf, b[m]), c[n][m], 0, 0, 0);
-            }
+            for (int m = 0; m < M; ++m) c[n][m] = multiply_one<TYPE>(a[n], b[m], c[n][m]);
     }
 }
 
@@ -102,28 +104,37 @@ template <class T, int RUN> __device__ __forceinline__ void store_run(T *to, con
 // ---- the tiled product ------------------------------------------------------------------------------------------------------
 __device__ const v4i zeros[1] = {};
 
-constexpr int STEP = 128;           // bytes of k that a step takes
+constexpr int COMPUTE_UNITS = 256;
 constexpr int TOGETHER = 8;         // tiles of rows that follow one another for the same columns
 enum { PLAIN, GATED, PARTIAL };     // what becomes of a tile: C, act(g) u, or fp32 sums of a piece of k
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 
-// One operand's share of the kernel: X of its rows (m or n) to a tile, of which a wave multiplies X / SHARES in FRAGMENTS of 16.
-// ROWS false: k along rows.  LDS holds a row's eight pieces of 16 bytes at places (piece ^ row % 8), so that what a read addresses at once has different banks.
+// One operand's share of the kernel: X of its rows (m or n) to a tile, of which a wave multiplies X / SHARES in FRAGMENTS of 16, STEP bytes of k at a time (64 or 128).
+// ROWS false: k along rows.  LDS holds lines of 128 bytes, a row's eight pieces of 16 or two rows' four, at places (piece ^ line % 8): what a read
+// addresses at once has different banks.
 // ROWS true: a row for each k.  LDS holds the rows, in units of 16 elements at places (unit ^ turned(row)), for the same reason.
-template <int TYPE, int X, int SHARES, int WAVES, bool ROWS> struct Operand {
+template <int TYPE, int X, int SHARES, int WAVES, int STEP, bool ROWS> struct Operand {
     typedef typename RealOf<TYPE>::type T;
-    static constexpr int SIZE = sizeof(T), PER = 16 / SIZE, KS = STEP / SIZE, COPIES = X / 8 / WAVES, FRAGMENTS = X / SHARES / 16;
+    static constexpr int SIZE = sizeof(T), PER = 16 / SIZE, KS = STEP / SIZE, BYTES = X * STEP, COPIES = BYTES / 1024 / WAVES, FRAGMENTS = X / SHARES / 16;
     static constexpr int LINE = X * SIZE, LANES = LINE / 16, UNITS = X / 16; // of a row of the second form
-    static_assert(COPIES * 8 * WAVES == X && FRAGMENTS * 16 * SHARES == X, "whole copies and fragments");
+    static constexpr int TO_LINE = 128 / STEP;                              // rows of a line of the first
+    static_assert(COPIES * 1024 * WAVES == BYTES && FRAGMENTS * 16 * SHARES == X, "whole copies and fragments");
     unsigned from[COPIES];  // of the lane's pieces, behind the step's address
     unsigned at[FRAGMENTS]; // of the lane's fragments, behind the stage's address
 
     static __device__ __forceinline__ int turned(int row) { return (SIZE == 4 ? row >> 2 & 3 : (row & 3) | (row >> 3 & 1) << 2) & (UNITS - 1); }
-    static __device__ __forceinline__ int row_of(int copy, int lane) { return ROWS ? copy * (64 / LANES) + lane / LANES : copy * 8 + (lane >> 3); }
-    // the tile's rows from `first` on of `count`; the wave's share
-    __device__ __forceinline__ void set(int first, int count, int64_t stride, int w, int share, int lane)
+    // of the lane's piece of a copy: its place within the line, its row, and its number along k
+    static __device__ __forceinline__ int place(int lane) { return (lane & 7) ^ (lane >> 3); }
+    static __device__ __forceinline__ int row_of(int copy, int lane)
+    {
+        if constexpr (ROWS) return copy * (64 / LANES) + lane / LANES;
+        else return (copy * 8 + (lane >> 3)) * TO_LINE + (TO_LINE == 2 ? place(lane) >> 2 : 0);
+    }
+    static __device__ __forceinline__ int piece(int lane) { return TO_LINE == 2 ? place(lane) & 3 : place(lane); }
+    // the tile's rows from `first` on of `count`
+    __device__ __forceinline__ void set(int first, int count, int64_t stride, int w, int lane)
     {
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
@@ -135,27 +146,27 @@ template <int TYPE, int X, int SHARES, int WAVES, bool ROWS> struct Operand {
                 from[i] = (unsigned)((min(first + row, count - 1) - first) * stride) + piece(lane) * 16;
             }
         }
-        fragments(share, lane);
     }
-    static __device__ __forceinline__ int piece(int lane) { return (lane & 7) ^ (lane >> 3); }
+    // the wave's share
     __device__ __forceinline__ void fragments(int share, int lane)
     {
         const int i = lane & 15, q = lane >> 4;
 #pragma unroll
         for (int f = 0; f < FRAGMENTS; ++f) {
             const int unit = share * FRAGMENTS + f;
-            if constexpr (!ROWS) at[f] = (unit * 16 + i) * STEP;
+            if constexpr (!ROWS && TO_LINE == 2) at[f] = unit * 16 * STEP + (i >> 1) * 128 + ((((i & 1) * 4 + q) ^ (i >> 1)) * 16);
+            else if constexpr (!ROWS) at[f] = (unit * 16 + i) * STEP;
             else if constexpr (SIZE == 4) at[f] = 4 * q * LINE + (unit ^ (q & (UNITS - 1))) * 64 + i * 4;
             else at[f] = (8 * q + (i >> 2)) * LINE + (unit ^ turned(8 * q + (i >> 2))) * 32 + (i & 3) * 8;
         }
     }
     // what the lane's piece of copy i begins with along k, of the step's
     static __device__ __forceinline__ int begins(int copy, int lane) { return ROWS ? row_of(copy, lane) : piece(lane) * PER; }
-    // Half `h` of a step.
+    // Fragment f, 64 bytes of k from 64 h on.
     __device__ __forceinline__ v4i read(const char *stage, int f, int h, int lane) const
     {
         if constexpr (!ROWS) {
-            return *reinterpret_cast<const v4i *>(stage + at[f] + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
+            return *reinterpret_cast<const v4i *>(stage + at[f] + (TO_LINE == 2 ? 0 : ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
         } else if constexpr (SIZE == 4) {
             v4i v;
 #pragma unroll
@@ -169,145 +180,294 @@ template <int TYPE, int X, int SHARES, int WAVES, bool ROWS> struct Operand {
     }
 };
 
-// BM x BN tiles, WM x WN waves, NS stages.  GATED: the rows of B are half gate's, half up's, such that each wave has both of its columns; where it has 32 of
+// The value, made wide here and not ahead of a loop (the pairs would be spilled).
+__device__ __forceinline__ uint64_t here(unsigned x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// What a workgroup multiplies at a time: a tile of one of the products, over all of k or a piece.
+struct Work { int m0, n0, z, split, first, steps; };
+
+// BM x BN tiles, WM x WN waves, NS stages of STEP bytes of k.  GATED: the rows of B are half gate's, half up's, such that each wave has both of its columns; where it has 32 of
 // them, a lane's eight neighbouring ones.
-template <int TYPE, int BM, int BN, int WM, int WN, int NS, bool AR, bool BR, int MODE> __global__ __launch_bounds__(64 * WM *WN) void product_kernel(ProductArgs a)
+template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, bool BR, int MODE> __global__ __launch_bounds__(64 * WM *WN) void product_kernel(ProductArgs a)
 {
     typedef typename RealOf<TYPE>::type T;
     constexpr int W = WM * WN, RM = BM / WM, RN = BN / WN, MF = RM / 16, NF = RN / 16, STAGE = (BM + BN) * STEP;
     constexpr int KS = STEP / sizeof(T), COLUMNS = MODE == GATED ? BN / 2 : BN;
     constexpr bool EIGHT = MODE == GATED && RN % 64 == 0;
-    typedef Operand<TYPE, BM, WM, W, AR> A;
-    typedef Operand<TYPE, BN, WN, W, BR> B;
+    typedef Operand<TYPE, BM, WM, W, STEP, AR> A;
+    typedef Operand<TYPE, BN, WN, W, STEP, BR> B;
     constexpr int COPIES = A::COPIES + B::COPIES;
     static_assert(MODE != GATED || (!AR && !BR), "weights lie with k along their rows");
     __shared__ __attribute__((aligned(1024))) char lds[NS][STAGE];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
 
-    // Workgroups go to the eight XCDs round-robin: each gets a run of tiles, in blocks of TOGETHER tiles of rows.
-    const int tiles = a.tiles_m * a.tiles_n, per = (tiles + 7) / 8, t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || t >= tiles) return;
-    const int block = t / (TOGETHER * a.tiles_n), high = min(TOGETHER, a.tiles_m - block * TOGETHER), in = t - block * TOGETHER * a.tiles_n;
-    const int m0 = (block * TOGETHER + in % high) * BM, n0 = in / high * COLUMNS, z = blockIdx.y;
+    // Workgroups go to the eight XCDs round-robin: each XCD has a run of the work, in blocks of TOGETHER tiles of rows, and its workgroups take turns.
+    const int tiles = a.tiles_m * a.tiles_n, all = tiles * (MODE == GATED ? 1 : a.batch) * (MODE == PARTIAL ? a.splits : 1);
+    const int per = (all + 7) / 8, xcd = blockIdx.x & 7, turns = gridDim.x >> 3, end = min(xcd * per + per, all);
+    const int each = (a.k + KS - 1) / KS; // steps of one of the products of a sum
+    auto work = [&](int u) {
+        const int o = u / tiles, t = u - o * tiles, block = t / (TOGETHER * a.tiles_n), high = min(TOGETHER, a.tiles_m - block * TOGETHER), in = t - block * TOGETHER * a.tiles_n;
+        const int batch = MODE == GATED ? 1 : a.batch, steps = MODE == GATED ? each : each * a.sum;
+        Work v = {(block * TOGETHER + in % high) * BM, in / high * COLUMNS, o % batch, o / batch, 0, steps};
+        if constexpr (MODE == PARTIAL) {
+            v.first = (int)((int64_t)steps * v.split / a.splits);
+            v.steps = (int)((int64_t)steps * (v.split + 1) / a.splits) - v.first;
+        }
+        return v;
+    };
 
+    // What is being asked for
     A oa;
     B ob;
-    oa.set(m0, a.m, a.a_stride, w, wm, lane);
-    const char *pa[2], *pb[2]; // of the products of a sum
+    oa.fragments(wm, lane);
+    ob.fragments(wn, lane);
+    const char *pa[2], *pb[2], *gated[B::COPIES]; // (pa, pb: of the products of a sum)
     const int64_t a_ahead = AR ? KS * a.a_stride : STEP, b_ahead = BR ? KS * a.b_stride[0] : STEP;
-    pa[0] = static_cast<const char *>(z ? a.a[1] : a.a[0]) + (AR ? m0 * (int64_t)sizeof(T) : m0 * a.a_stride);
-    pa[1] = static_cast<const char *>(a.a[1]) + (AR ? m0 * (int64_t)sizeof(T) : m0 * a.a_stride);
-    const char *gated[B::COPIES];
-    if constexpr (MODE == GATED) {
-#pragma unroll
-        for (int i = 0; i < B::COPIES; ++i) {
-            const int first = (w * B::COPIES + i) * 8, which = first % RN >= RN / 2, in = first % (RN / 2) + (lane >> 3);
-            // (row 16 f + 4 q + e of 32 holds column 8 q + 4 f + e)
-            const int column = first / RN * (RN / 2) + (EIGHT ? (in & ~31) + (in >> 2 & 3) * 8 + (in >> 4 & 1) * 4 + (in & 3) : in);
-            const int64_t stride = which ? a.b_stride[1] : a.b_stride[0];
-            gated[i] = static_cast<const char *>(which ? a.b[1] : a.b[0]) + n0 * stride;
-            ob.from[i] = (unsigned)((min(n0 + column, a.n - 1) - n0) * stride) + B::piece(lane) * 16;
-        }
-        ob.fragments(wn, lane);
-    } else {
-        ob.set(n0, a.n, a.b_stride[0], w, wn, lane);
-        pb[0] = static_cast<const char *>(a.b[0]) + (BR ? n0 * (int64_t)sizeof(T) : n0 * a.b_stride[0]);
-        pb[1] = static_cast<const char *>(a.b[1]) + (BR ? n0 * (int64_t)sizeof(T) : n0 * a.b_stride[0]);
-    }
     const unsigned base = mcu::lds_addr_uniform(lds);
-    const int each = (a.k + KS - 1) / KS, all = MODE == GATED ? each : each * a.sum;
-    int first = 0, steps = all;
-    if constexpr (MODE == PARTIAL) {
-        first = (int)((int64_t)all * blockIdx.z / a.splits);
-        steps = (int)((int64_t)all * (blockIdx.z + 1) / a.splits) - first;
-    }
-    auto request = [&](int s) { // step s of this workgroup's
-        const int step = first + s, second = MODE != GATED && step >= each, own = second ? step - each : step;
-        const unsigned to = base + s % NS * STAGE;
-        const char *const ca = (second ? pa[1] : pa[0]) + own * a_ahead;
-        if ((own + 1) * KS <= a.k) {
+    Work asked;
+    auto ask_of = [&](int u) {
+        asked = work(u);
+        oa.set(asked.m0, a.m, a.a_stride, w, lane);
+        pa[0] = static_cast<const char *>(asked.z ? a.a[1] : a.a[0]) + (AR ? asked.m0 * (int64_t)sizeof(T) : asked.m0 * a.a_stride);
+        pa[1] = static_cast<const char *>(a.a[1]) + (AR ? asked.m0 * (int64_t)sizeof(T) : asked.m0 * a.a_stride);
+        if constexpr (MODE == GATED) {
 #pragma unroll
-            for (int i = 0; i < A::COPIES; ++i) mcu::copy16_to_lds(ca, oa.from[i], to + (w * A::COPIES + i) * 1024);
-#pragma unroll
-            for (int i = 0; i < B::COPIES; ++i)
-                mcu::copy16_to_lds((MODE == GATED ? gated[i] : second ? pb[1] : pb[0]) + own * b_ahead, ob.from[i], to + BM * STEP + (w * B::COPIES + i) * 1024);
-        } else { // what lies beyond k is zeros of both operands
-            const int left = a.k - own * KS;
-#pragma unroll
-            for (int i = 0; i < A::COPIES; ++i)
-                mcu::copy16_to_lds(A::begins(w * A::COPIES + i, lane) < left ? (const void *)(ca + oa.from[i]) : zeros, to + (w * A::COPIES + i) * 1024);
-#pragma unroll
-            for (int i = 0; i < B::COPIES; ++i)
-                mcu::copy16_to_lds(B::begins(w * B::COPIES + i, lane) < left ? (const void *)((MODE == GATED ? gated[i] : second ? pb[1] : pb[0]) + own * b_ahead + ob.from[i]) : zeros,
-                                   to + BM * STEP + (w * B::COPIES + i) * 1024);
+            for (int i = 0; i < B::COPIES; ++i) {
+                const int first = (w * B::COPIES + i) * 8 * B::TO_LINE, which = first % RN >= RN / 2, in = (first + B::row_of(0, lane)) % (RN / 2);
+                // (row 16 f + 4 q + e of 32 holds column 8 q + 4 f + e)
+                const int column = first / RN * (RN / 2) + (EIGHT ? (in & ~31) + (in >> 2 & 3) * 8 + (in >> 4 & 1) * 4 + (in & 3) : in);
+                const int64_t stride = which ? a.b_stride[1] : a.b_stride[0];
+                gated[i] = static_cast<const char *>(which ? a.b[1] : a.b[0]) + asked.n0 * stride;
+                ob.from[i] = (unsigned)((min(asked.n0 + column, a.n - 1) - asked.n0) * stride) + B::piece(lane) * 16;
+            }
+        } else {
+            ob.set(asked.n0, a.n, a.b_stride[0], w, lane);
+            pb[0] = static_cast<const char *>(a.b[0]) + (BR ? asked.n0 * (int64_t)sizeof(T) : asked.n0 * a.b_stride[0]);
+            pb[1] = static_cast<const char *>(a.b[1]) + (BR ? asked.n0 * (int64_t)sizeof(T) : asked.n0 * a.b_stride[0]);
         }
+    };
+    // A step's copies: their bases, and whether all of the step is there
+    struct Step { const char *a, *b; int second; int64_t b_at; int left; };
+    auto step_of = [&](int s) {
+        const int step = asked.first + s, second = MODE != GATED && step >= each, own = second ? step - each : step;
+        return Step{(second ? pa[1] : pa[0]) + own * a_ahead, MODE == GATED ? nullptr : (second ? pb[1] : pb[0]) + own * b_ahead, second, own * b_ahead,
+                    s < asked.steps ? a.k - own * KS : 0};
+    };
+    auto copy = [&](const Step &v, auto i_, int stage) {
+        constexpr int i = decltype(i_)::value, j = i - A::COPIES;
+        if constexpr (i < A::COPIES) mcu::copy16_to_lds(v.a, oa.from[i], base + stage * STAGE + (w * A::COPIES + i) * 1024);
+        else mcu::copy16_to_lds(MODE == GATED ? gated[j] + v.b_at : v.b, ob.from[j], base + stage * STAGE + BM * STEP + (w * B::COPIES + j) * 1024);
+    };
+    auto request = [&](const Step &v, int stage) {
+        if (v.left >= KS) return mcu::static_for<COPIES>([&](auto i) { copy(v, i, stage); });
+        // what lies beyond k is zeros of both operands
+        const unsigned to = base + stage * STAGE;
+#pragma unroll
+        for (int i = 0; i < A::COPIES; ++i)
+            mcu::copy16_to_lds(A::begins(w * A::COPIES + i, lane) < v.left ? (const void *)(v.a + here(oa.from[i])) : zeros, to + (w * A::COPIES + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < B::COPIES; ++i)
+            mcu::copy16_to_lds(B::begins(w * B::COPIES + i, lane) < v.left ? (const void *)((MODE == GATED ? gated[i] + v.b_at : v.b) + here(ob.from[i])) : zeros,
+                               to + BM * STEP + (w * B::COPIES + i) * 1024);
     };
 
     v4f acc[NF][MF];
+    auto clear = [&] {
 #pragma unroll
-    for (int n = 0; n < NF; ++n)
+        for (int n = 0; n < NF; ++n)
 #pragma unroll
-        for (int m = 0; m < MF; ++m) acc[n][m] = (v4f){0, 0, 0, 0};
+            for (int m = 0; m < MF; ++m) acc[n][m] = (v4f){0, 0, 0, 0};
+    };
+    // What becomes of a tile
+    auto finish = [&](const Work &v) {
+        if constexpr (MODE == GATED) {
+            constexpr int RUN = EIGHT ? 8 : 4, FS = RUN / 4;
+            with_activation(a.activation, [&](auto kind) {
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-        if (s < steps) request(s);
-    for (int s = 0; s < steps; ++s) {
-        if (s + NS - 1 <= steps) mcu::vm_wait<(NS - 2) * COPIES>(); // (step s has come: that many copies were asked for behind it)
-        else mcu::vm_wait<0>();
-        asm volatile("s_barrier" ::: "memory"); // for all waves, whose reads of the stage that is written next have returned, too
-        if (s + NS - 1 < steps) request(s + NS - 1);
-        const char *const la = lds[s % NS], *const lb = lds[s % NS] + BM * STEP;
+                for (int m = 0; m < MF; ++m) {
+                    const int row = v.m0 + wm * RM + m * 16 + (lane & 15);
+                    if (row >= a.m) continue;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v4i fa[MF], fb[NF];
+                    for (int n = 0; n < NF / 2; n += FS) {
+                        const int column = v.n0 + wn * (RN / 2) + n * 16 + RUN * (lane >> 4), count = a.n - column;
+                        if (count <= 0) continue;
+                        float h[RUN], g[RUN], u[RUN];
 #pragma unroll
-            for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
-#pragma unroll
-            for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
-            multiply<TYPE>(fb, fa, acc);
-        }
-        mcu::lgkm_wait();
-    }
-
-    if constexpr (MODE == GATED) {
-        constexpr int RUN = EIGHT ? 8 : 4, FS = RUN / 4;
-        with_activation(a.activation, [&](auto kind) {
-#pragma unroll
-            for (int m = 0; m < MF; ++m) {
-                const int row = m0 + wm * RM + m * 16 + (lane & 15);
-                if (row >= a.m) continue;
-#pragma unroll
-                for (int n = 0; n < NF / 2; n += FS) {
-                    const int column = n0 + wn * (RN / 2) + n * 16 + RUN * (lane >> 4), count = a.n - column;
-                    if (count <= 0) continue;
-                    float h[RUN], g[RUN], u[RUN];
-#pragma unroll
-                    for (int e = 0; e < RUN; ++e) {
-                        g[e] = acc[n + e / 4][m][e % 4];
-                        u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
-                        h[e] = activated<decltype(kind)::value>(g[e]) * u[e];
-                    }
-                    store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
-                    if (a.g) {
-                        store_run(a.g + row * a.saved_stride + column, g, count);
-                        store_run(a.u + row * a.saved_stride + column, u, count);
+                        for (int e = 0; e < RUN; ++e) {
+                            g[e] = acc[n + e / 4][m][e % 4];
+                            u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
+                            h[e] = activated<decltype(kind)::value>(g[e]) * u[e];
+                        }
+                        store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
+                        if (a.g) {
+                            store_run(a.g + row * a.saved_stride + column, g, count);
+                            store_run(a.u + row * a.saved_stride + column, u, count);
+                        }
                     }
                 }
+            });
+        } else {
+#pragma unroll
+            for (int m = 0; m < MF; ++m) {
+                const int row = v.m0 + wm * RM + m * 16 + (lane & 15);
+                if (row >= a.m) continue;
+#pragma unroll
+                for (int n = 0; n < NF; ++n) {
+                    const int column = v.n0 + wn * RN + n * 16 + 4 * (lane >> 4), count = a.n - column;
+                    if (count <= 0) continue;
+                    const float c[4] = {acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3]};
+                    if constexpr (MODE == PARTIAL) store_run(a.partial + ((int64_t)(v.split * a.batch + v.z) * a.m + row) * a.n + column, c, count);
+                    else store_run(static_cast<T *>(v.z ? a.c[1] : a.c[0]) + row * (v.z ? a.c_stride[1] : a.c_stride[0]) + column, c, count);
+                }
             }
-        });
+        }
+    };
+
+    int u = xcd * per + (int)(blockIdx.x >> 3);
+    if (u >= end) return;
+    if constexpr (STEP == 64) {
+        // The steps of all of a workgroup's tiles are one sequence; copies are asked for NS - 1 steps ahead, those of the next tile before this one's results
+        // are written.
+        int ask = u, s_asked = 0;      // what is asked for next
+        ask_of(ask);
+        unsigned came = 0, requested = 0, now = 0; // steps whose own copies have come for certain, that were asked for, and that were multiplied
+        constexpr int WHOLE = AR ? 2 : 1;          // a tile's steps are a multiple of this (filled up with zeros)
+        auto advance = [&] {
+            ++requested;
+            if (++s_asked < (asked.steps + WHOLE - 1) / WHOLE * WHOLE) return;
+            s_asked = 0;
+            ask += turns;
+            if (ask < end) ask_of(ask);
+        };
+        const bool any = asked.steps > 0;
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i)
+            if (any && ask < end) {
+                request(step_of(s_asked), i);
+                advance();
+            }
+        if (requested == NS - 1) mcu::vm_wait<(NS - 2) * COPIES>();
+        else mcu::vm_wait<0>();
+        asm volatile("s_barrier" ::: "memory");
+        if constexpr (AR) {
+            // Fragments that are put together from two reads each take too long for a turn of reading: a step's are read while the step before it
+            // is multiplied, each of B's as soon as the last product with the one before it is under way, and copies take turns with both.  At a step's
+            // barrier the next step has come, and all waves have used the step before.
+            constexpr int ALL = NF * MF, APART = ALL / COPIES, AT_ONCE = (MF + NF - 1) / NF; // fragments of A to a row of products
+            static_assert(APART * COPIES <= ALL && APART > 1 && MF > 2 * AT_ONCE, "a place for each");
+            v4i fa[2][MF], fb[NF];
+#pragma unroll
+            for (int n = 0; n < NF; ++n) fb[n] = ob.read(lds[0] + BM * STEP, n, 0, lane);
+#pragma unroll
+            for (int m = 0; m < MF; ++m) fa[0][m] = oa.read(lds[0], m, 0, lane);
+            auto turn = [&](auto odd_) {
+                constexpr int odd = decltype(odd_)::value;
+                if (now + 1 >= came) { // (the step after this one has come: that many copies were asked for behind it)
+                    if (requested >= now + NS - 1) mcu::vm_wait<(NS - 3) * COPIES>();
+                    else mcu::vm_wait<0>();
+                }
+                asm volatile("s_barrier" ::: "memory");
+                const bool more = any && ask < end;
+                const Step v = step_of(s_asked);
+                const bool full = more && v.left >= KS;
+                const int to = (now + NS - 1) % NS;
+                if (more && !full) request(v, to);
+                const char *const la = lds[(now + 1) % NS], *const lb = lds[(now + 1) % NS] + BM * STEP; // (behind the last step: read, and not used)
+                mcu::static_for<ALL>([&](auto j_) {
+                    constexpr int j = decltype(j_)::value, n = j / MF, m = j % MF;
+                    acc[n][m] = multiply_one<TYPE>(fb[n], fa[odd][m], acc[n][m]);
+                    if constexpr (m % 2 == 1 && m / 2 < AT_ONCE && n * AT_ONCE + m / 2 < MF) fa[odd ^ 1][n * AT_ONCE + m / 2] = oa.read(la, n * AT_ONCE + m / 2, 0, lane);
+                    if constexpr (m == MF - 1) fb[n] = ob.read(lb, n, 0, lane);
+                    if constexpr (j % APART == APART / 2 && j / APART < COPIES) {
+                        if (full) copy(v, std::integral_constant<int, j / APART>{}, to);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if (more) advance();
+                ++now;
+            };
+            for (; u < end; u += turns) {
+                const Work mine = work(u);
+                clear();
+                for (int s = 0; s < mine.steps; s += 2) {
+                    turn(std::integral_constant<int, 0>{});
+                    turn(std::integral_constant<int, 1>{});
+                }
+                mcu::vm_wait<0>(); // (so that no step of the next tile waits for the stores)
+                came = requested;
+                finish(mine);
+            }
+        } else {
+            // The waves are two groups, one wave of each to a SIMD, half a step apart: while one group multiplies, the other reads its next fragments and
+            // asks for copies.  Two barriers to a step hand the matrix units over.  Before a group leaves its turn of reading, its copies of the step
+            // behind have come; a stage is written again when both groups have read it.
+            static_assert(W == 8, "two waves to a SIMD");
+            const bool late = w >= 4;
+            if (late) asm volatile("s_barrier" ::: "memory");
+            for (; u < end; u += turns) {
+                const Work mine = work(u);
+                clear();
+                for (int s = 0; s < mine.steps; ++s, ++now) {
+                    v4i fa[MF], fb[NF];
+                    const char *const la = lds[now % NS], *const lb = lds[now % NS] + BM * STEP;
+#pragma unroll
+                    for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, 0, lane);
+#pragma unroll
+                    for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, 0, lane);
+                    if (any && ask < end) {
+                        request(step_of(s_asked), (now + NS - 1) % NS);
+                        advance();
+                    }
+                    if (now + 1 >= came) { // (that many copies were asked for behind the next step's)
+                        if (requested >= now + NS) mcu::vm_wait<(NS - 2) * COPIES>();
+                        else mcu::vm_wait<0>();
+                    }
+                    mcu::lgkm_wait();
+                    __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("s_barrier" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply<TYPE>(fb, fa, acc);
+                    __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("s_barrier" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                mcu::vm_wait<0>(); // (so that no step of the next tile waits for the stores)
+                came = requested;
+                finish(mine);
+            }
+            if (!late) asm volatile("s_barrier" ::: "memory");
+        }
     } else {
+        for (; u < end; u += turns) {
+            ask_of(u);
+            clear();
+            const int steps = asked.steps;
 #pragma unroll
-        for (int m = 0; m < MF; ++m) {
-            const int row = m0 + wm * RM + m * 16 + (lane & 15);
-            if (row >= a.m) continue;
+            for (int s = 0; s < NS - 1; ++s)
+                if (s < steps) request(step_of(s), s);
+            for (int s = 0; s < steps; ++s) {
+                if (s + NS - 1 <= steps) mcu::vm_wait<(NS - 2) * COPIES>(); // (step s has come: that many copies were asked for behind it)
+                else mcu::vm_wait<0>();
+                asm volatile("s_barrier" ::: "memory"); // for all waves, whose reads of the stage that is written next have returned, too
+                if (s + NS - 1 < steps) request(step_of(s + NS - 1), (s + NS - 1) % NS);
+                const char *const la = lds[s % NS], *const lb = lds[s % NS] + BM * STEP;
 #pragma unroll
-            for (int n = 0; n < NF; ++n) {
-                const int column = n0 + wn * RN + n * 16 + 4 * (lane >> 4), count = a.n - column;
-                if (count <= 0) continue;
-                const float v[4] = {acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3]};
-                if constexpr (MODE == PARTIAL) store_run(a.partial + ((int64_t)(blockIdx.z * a.batch + z) * a.m + row) * a.n + column, v, count);
-                else store_run(static_cast<T *>(z ? a.c[1] : a.c[0]) + row * (z ? a.c_stride[1] : a.c_stride[0]) + column, v, count);
+                for (int h = 0; h < 2; ++h) {
+                    v4i fa[MF], fb[NF];
+#pragma unroll
+                    for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
+#pragma unroll
+                    for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
+                    multiply<TYPE>(fb, fa, acc);
+                }
+                mcu::lgkm_wait();
             }
+            finish(asked);
+            asm volatile("s_barrier" ::: "memory"); // (all reads of this tile's stages have returned)
         }
     }
 }
@@ -469,20 +629,21 @@ template <class T> __global__ __launch_bounds__(256) void pad_rows_kernel(PadRow
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------------------
-template <int TYPE, int BM, int BN, int WM, int WN, int NS, bool AR, bool BR, int MODE> hipError_t product(ProductArgs a, hipStream_t s)
+template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, bool BR, int MODE> hipError_t product(ProductArgs a, hipStream_t s)
 {
     constexpr int COLUMNS = MODE == GATED ? BN / 2 : BN;
     a.tiles_m = (a.m + BM - 1) / BM;
     a.tiles_n = (a.n + COLUMNS - 1) / COLUMNS;
-    const dim3 grid((unsigned)((a.tiles_m * a.tiles_n + 7) / 8 * 8), MODE == GATED ? 1 : a.batch, MODE == PARTIAL ? a.splits : 1);
-    return launch_kernel((product_kernel<TYPE, BM, BN, WM, WN, NS, AR, BR, MODE>), grid, dim3(64 * WM * WN), 0, s, a);
+    const int64_t all = ((int64_t)a.tiles_m * a.tiles_n * (MODE == GATED ? 1 : a.batch) * (MODE == PARTIAL ? a.splits : 1) + 7) / 8 * 8;
+    const dim3 grid((unsigned)(STEP == 64 && all > COMPUTE_UNITS ? COMPUTE_UNITS : all)); // (the large tiles: a workgroup to a compute unit)
+    return launch_kernel((product_kernel<TYPE, BM, BN, WM, WN, STEP, NS, AR, BR, MODE>), grid, dim3(64 * WM * WN), 0, s, a);
 }
 
 template <int TYPE, bool AR, bool BR, int MODE> hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t s)
 {
-    if (tile == 256) return product<TYPE, 256, 256, 2, 4, 2, AR, BR, MODE>(a, s);
-    if (tile == 128) return product<TYPE, 128, 128, 2, 2, 2, AR, BR, MODE>(a, s);
-    return product<TYPE, 64, 64, 2, 2, 3, AR, BR, MODE>(a, s);
+    if (tile == 256) return product<TYPE, 256, 256, 2, 4, TYPE == MC_F32 ? 128 : 64, TYPE == MC_F32 ? 2 : 4, AR, BR, MODE>(a, s);
+    if (tile == 128) return product<TYPE, 128, 128, 2, 2, 128, 2, AR, BR, MODE>(a, s);
+    return product<TYPE, 64, 64, 2, 2, 128, 3, AR, BR, MODE>(a, s);
 }
 
 template <int TYPE, bool AR> hipError_t product_plain(ProductArgs a, ProductPlan p, hipStream_t s)
@@ -513,7 +674,7 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type typ
     // What a compute unit takes for a step of 128 bytes of each tile, and workgroups that it runs at once
     struct Shape { int tile; double cost; };
     const Shape shapes[3] = {{256, type == MC_F32 ? 16.0 : 16.0}, {128, type == MC_F32 ? 4.0 : 4.8}, {64, type == MC_F32 ? 1.05 : 1.8}};
-    const int64_t size = type == MC_F32 ? 4 : 2, steps = (k * size + STEP - 1) / STEP;
+    const int64_t size = type == MC_F32 ? 4 : 2, steps = (k * size + 127) / 128;
     ProductPlan best = {256, 1};
     double least = 1e30;
     for (const Shape &s : shapes) {
