@@ -6,8 +6,9 @@
 //   dyt = dy + r2 (W(dn) - mean W(dn) - yhat mean(W(dn) yhat)),   dr = residual_scale dyt,   da = branch_scale gate dyt,
 //   dx = r1 (W(da) - mean W(da) - xhat mean(W(da) xhat))          (without the first mean where the norm has none)
 // and the parameters' gradients are sums over rows of dn yhat, dn, da xhat, da and branch_scale a dyt.  Nothing is kept from the forward call: y is
-// worked out again from x and r, unrounded, for the bytes that reading it would cost.  A workgroup takes consecutive rows and
-// keeps these sums in registers; a second kernel adds the workgroups' in their order, so that results are the same from call to call.
+// worked out again from x and r, unrounded, for the bytes that reading it would cost.  A workgroup takes consecutive rows, asks for a
+// row while it works on the one before, and keeps these sums in registers; a second kernel adds the workgroups' in their order, so that results are the
+// same from call to call.
 #include "layer.h"
 
 #include "lds_async.h"
@@ -16,371 +17,463 @@ namespace {
 
 using mcu::v4i;
 
-// Eight elements as they lie in memory, of either width
-struct Raw { v4i lo, hi; };
+// Eight elements as they lie in memory
+template <int TYPE> struct Raw { v4i v[TYPE == MC_F32 ? 2 : 1]; };
 
-__device__ __forceinline__ Raw load_raw(const void *p, int type, int64_t at)
+// `n` of them from element `at` on (any alignment), zeros behind them
+template <int TYPE> __device__ __forceinline__ Raw<TYPE> load(const void *p, int64_t at, int n)
 {
-    Raw r;
-    if (type == MC_F32) {
-        __builtin_memcpy(&r.lo, static_cast<const float *>(p) + at, 16);
-        __builtin_memcpy(&r.hi, static_cast<const float *>(p) + at + 4, 16);
-    } else {
-        __builtin_memcpy(&r.lo, static_cast<const uint16_t *>(p) + at, 16);
-        r.hi = r.lo;
+    typedef typename RealOf<TYPE>::type T;
+    const T *from = static_cast<const T *>(p) + at;
+    Raw<TYPE> r = {};
+    if (n >= 8) {
+        __builtin_memcpy(&r, from, sizeof r);
+    } else if (n > 0) {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? from[i] : (T)0;
+        __builtin_memcpy(&r, e, sizeof r);
     }
     return r;
 }
-__device__ __forceinline__ float as_float(uint16_t bits, int type)
+template <int TYPE> __device__ __forceinline__ void decode(const Raw<TYPE> &r, float (&v)[8])
 {
-    if (type == MC_BF16) return __int_as_float((int)bits << 16);
-    _Float16 h;
-    __builtin_memcpy(&h, &bits, 2);
-    return (float)h;
+    typename RealOf<TYPE>::type e[8];
+    __builtin_memcpy(e, &r, sizeof r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)e[i];
 }
-// `n` elements (fewer than eight), zeros behind them
-__device__ __forceinline__ Raw load_part(const void *p, int type, int64_t at, int n)
+template <int TYPE> __device__ __forceinline__ void store(void *p, int64_t at, int n, const float (&v)[8])
 {
-    uint32_t w[8];
+    typedef typename RealOf<TYPE>::type T;
+    T *to = static_cast<T *>(p) + at, e[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = 0;
-    if (type == MC_F32) {
+    for (int i = 0; i < 8; ++i) e[i] = (T)v[i];
+    if (n >= 8) {
+        __builtin_memcpy(to, e, sizeof e);
+    } else if (n > 0) {
+        asm volatile("" ::: "memory"); // (the compiler would else make some elements' stores those of both cases, and write whole chunks in parts)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) w[e] = static_cast<const uint32_t *>(p)[at + e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) w[e / 2] |= (uint32_t)static_cast<const uint16_t *>(p)[at + e] << (16 * (e % 2));
-    }
-    return {(v4i){(int)w[0], (int)w[1], (int)w[2], (int)w[3]}, (v4i){(int)w[4], (int)w[5], (int)w[6], (int)w[7]}};
-}
-__device__ __forceinline__ void decode(const Raw &r, int type, float (&v)[8])
-{
-    if (type == MC_F32) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __int_as_float(r.lo[e]), v[4 + e] = __int_as_float(r.hi[e]);
-    } else if (type == MC_BF16) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[2 * e] = __int_as_float(r.lo[e] << 16), v[2 * e + 1] = __int_as_float(r.lo[e] & 0xffff0000);
-    } else {
-        _Float16 h[8];
-        __builtin_memcpy(h, &r.lo, 16);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+        for (int i = 0; i < 8; ++i)
+            if (i < n) to[i] = e[i];
+        asm volatile("" ::: "memory");
     }
 }
-__device__ __forceinline__ void store(void *p, int type, int64_t at, int n, const float (&v)[8])
+
+// A wave's sum, in all of its lanes: exchanges within 16 lanes, then of the 16s and of the halves.
+template <int CONTROL> __device__ __forceinline__ float exchanged(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float wave_sum(float x)
 {
-    if (type == MC_F32) {
-        float *to = static_cast<float *>(p) + at;
-        if (n >= 8) return (void)__builtin_memcpy(to, v, 32);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) to[e] = v[e];
-    } else if (type == MC_BF16) {
-        __bf16 h[8], *to = static_cast<__bf16 *>(p) + at;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = (__bf16)v[e];
-        if (n >= 8) return (void)__builtin_memcpy(to, h, 16);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) to[e] = h[e];
-    } else {
-        _Float16 h[8], *to = static_cast<_Float16 *>(p) + at;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = (_Float16)v[e];
-        if (n >= 8) return (void)__builtin_memcpy(to, h, 16);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) to[e] = h[e];
-    }
+    x += exchanged<0xb1>(x);  // lanes 1 apart
+    x += exchanged<0x4e>(x);  // 2 apart
+    x += exchanged<0x141>(x); // mirrored in eights
+    x += exchanged<0x140>(x); // and in 16s
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // A row over THREADS threads, E chunks of eight elements each: chunk k of thread t begins at element 8 (t + k THREADS).
-// WHOLE: the row is whole chunks.
-template <int THREADS, int E, bool WHOLE> struct Row {
+template <int THREADS, int E> struct Row {
     static constexpr int WAVES = THREADS / 64;
     int t, dim;
-    float *shared;    // 2 x 2 x WAVES floats
+    float inverse;    // 1 / dim
+    float *shared;    // 2 x WAVES x 2 floats
     int turn;         // which half of them the next sum uses (one barrier to a sum)
 
     __device__ __forceinline__ int at(int k) const { return 8 * (t + k * THREADS); }
-    __device__ __forceinline__ int count(int k) const { return WHOLE ? (at(k) < dim ? 8 : 0) : min(max(dim - at(k), 0), 8); }
-    // (chunks beyond the row: the first elements, which are not used)
-    __device__ __forceinline__ void load(Raw (&r)[E], const void *p, int type, int64_t row_at) const
-    {
-        if (WHOLE) {
-            if (type == MC_F32) {
-#pragma unroll
-                for (int k = 0; k < E; ++k) r[k] = load_raw(p, MC_F32, row_at + (at(k) < dim ? at(k) : 0));
-            } else {
-#pragma unroll
-                for (int k = 0; k < E; ++k) r[k] = load_raw(p, MC_F16, row_at + (at(k) < dim ? at(k) : 0));
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < E; ++k) r[k] = count(k) == 8 ? load_raw(p, type, row_at + at(k)) : load_part(p, type, row_at + at(k), count(k));
-        }
-    }
+    __device__ __forceinline__ int count(int k) const { return min(max(dim - at(k), 0), 8); }
     __device__ __forceinline__ void sums(float &a, float &b)
     {
-#pragma unroll
-        for (int j = 32; j > 0; j >>= 1) {
-            a += __shfl_xor(a, j);
-            b += __shfl_xor(b, j);
-        }
+        a = wave_sum(a);
+        b = wave_sum(b);
         if constexpr (WAVES > 1) {
             float *s = shared + turn * 2 * WAVES;
             turn ^= 1;
-            if ((t & 63) == 0) s[t >> 6] = a, s[WAVES + (t >> 6)] = b;
+            if ((t & 63) == 0) s[2 * (t >> 6)] = a, s[2 * (t >> 6) + 1] = b;
             __syncthreads();
-            a = b = 0;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) a += s[w], b += s[WAVES + w];
+            a = s[2 * (t & (WAVES - 1))], b = s[2 * (t & (WAVES - 1)) + 1]; // (a wave's to each lane)
+            a += exchanged<0xb1>(a), b += exchanged<0xb1>(b);
+            if constexpr (WAVES > 2) a += exchanged<0x4e>(a), b += exchanged<0x4e>(b);
+            if constexpr (WAVES > 4) a += exchanged<0x141>(a), b += exchanged<0x141>(b);
+            if constexpr (WAVES > 8) a += exchanged<0x140>(a), b += exchanged<0x140>(b);
         }
     }
-    // v becomes its normed values; returns 1 / deviation.
+    // v (zeros beyond the row) becomes its normed values, zeros beyond the row; returns 1 / deviation.
     __device__ __forceinline__ float norm(float (&v)[E][8], int kind, float eps)
     {
+        float m;
+        return norm(v, kind, eps, m);
+    }
+    __device__ __forceinline__ float norm(float (&v)[E][8], int kind, float eps, float &m)
+    {
         float q = 0, none = 0;
+        m = 0;
         if (kind == MC_NORM_LAYER) {
-            float m = 0;
 #pragma unroll
             for (int k = 0; k < E; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) m += e < count(k) ? v[k][e] : 0;
+                for (int e = 0; e < 8; ++e) m += v[k][e];
             sums(m, none);
             m /= dim;
 #pragma unroll
-            for (int k = 0; k < E; ++k)
+            for (int k = 0; k < E; ++k) {
+                const int n = count(k);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] -= m;
+                for (int e = 0; e < 8; ++e) v[k][e] = e < n ? v[k][e] - m : 0;
+            }
         }
 #pragma unroll
         for (int k = 0; k < E; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q += e < count(k) ? v[k][e] * v[k][e] : 0;
+            for (int e = 0; e < 8; ++e) q += v[k][e] * v[k][e];
         sums(q, none);
-        const float r = 1.0f / sqrtf(q / dim + eps);
+        const float r = 1.0f / sqrtf(q * inverse + eps);
 #pragma unroll
         for (int k = 0; k < E; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[k][e] *= r;
         return r;
     }
-    // d becomes the gradient through a norm, from that of the normed values `hat`.
-    __device__ __forceinline__ void norm_backward(float (&d)[E][8], const float (&hat)[E][8], float r, int kind)
+    // Parameters in fp32 (`otherwise` where there are none), zeros beyond the row
+    __device__ __forceinline__ void parameters(float (&v)[E][8], const void *p, int type, int64_t from, float otherwise) const
     {
-        float mean = 0, dot = 0;
 #pragma unroll
-        for (int k = 0; k < E; ++k)
+        for (int k = 0; k < E; ++k) {
+            const int n = count(k);
+            if (!p) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mean += e < count(k) ? d[k][e] : 0;
-                dot += e < count(k) ? d[k][e] * hat[k][e] : 0;
-            }
-        sums(mean, dot);
-        mean = kind == MC_NORM_LAYER ? mean / dim : 0;
-        dot /= dim;
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[k][e] = r * (d[k][e] - mean - hat[k][e] * dot);
-    }
-    // v = v w + b, either null
-    __device__ __forceinline__ void scale(float (&v)[E][8], const Raw (&w)[E], bool has_w, const void *b, int type) const
-    {
-        float f[8];
-        if (has_w)
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                decode(w[k], type, f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] *= f[e];
-            }
-        if (b) {
-            Raw r[E];
-            load(r, b, type, 0);
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                decode(r[k], type, f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] += f[e];
+                for (int e = 0; e < 8; ++e) v[k][e] = e < n ? otherwise : 0;
+            } else if (type == MC_F32) {
+                decode(load<MC_F32>(p, from + at(k), n), v[k]);
+            } else if (type == MC_F16) {
+                decode(load<MC_F16>(p, from + at(k), n), v[k]);
+            } else {
+                decode(load<MC_BF16>(p, from + at(k), n), v[k]);
             }
         }
     }
-    __device__ __forceinline__ void write(void *p, int type, int64_t row_at, const float (&v)[E][8]) const
+    template <int TYPE> __device__ __forceinline__ void write(void *p, int64_t from, const float (&v)[E][8]) const
     {
 #pragma unroll
-        for (int k = 0; k < E; ++k)
-            if (count(k) > 0) store(p, type, row_at + at(k), count(k), v[k]);
+        for (int k = 0; k < E; ++k) store<TYPE>(p, from + at(k), count(k), v[k]);
+    }
+    __device__ __forceinline__ void write_parameters(void *p, int type, int64_t from, const float (&v)[E][8]) const
+    {
+        if (type == MC_F32) write<MC_F32>(p, from, v);
+        else if (type == MC_F16) write<MC_F16>(p, from, v);
+        else write<MC_BF16>(p, from, v);
     }
 };
 
-// PACKED: rows of a workgroup, a wave each
-template <int TYPE, int THREADS, int E, bool WHOLE, int PACKED> __global__ __launch_bounds__(THREADS *PACKED) void block_norm_kernel(NormArgs a)
+#define EACH(k, e)                 \
+    _Pragma("unroll")              \
+    for (int k = 0; k < E; ++k)    \
+        _Pragma("unroll") for (int e = 0; e < 8; ++e)
+
+// Parameters as they lie in memory, of a type that is known when the kernel runs
+struct RawParameters { v4i lo, hi; };
+__device__ __forceinline__ RawParameters load_parameters(const void *p, int type, int64_t at, int n)
+{
+    if (type == MC_F32) {
+        const Raw<MC_F32> r = load<MC_F32>(p, at, n);
+        return {r.v[0], r.v[1]};
+    }
+    const Raw<MC_F16> r = load<MC_F16>(p, at, n); // (or bf16: bits, and zeros)
+    return {r.v[0], r.v[0]};
+}
+__device__ __forceinline__ void decode_parameters(const RawParameters &r, int type, float (&v)[8])
+{
+    if (type == MC_F32) decode(Raw<MC_F32>{{r.lo, r.hi}}, v);
+    else if (type == MC_F16) decode(Raw<MC_F16>{{r.lo}}, v);
+    else decode(Raw<MC_BF16>{{r.lo}}, v);
+}
+
+// PACKED: rows of a workgroup, a wave each.  WHOLE: rows are whole chunks.  All operands are asked for before the first is used.  (Without these two, 16384 rows of
+// 4096 bf16 took 141 us instead of 101.)
+template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __global__ __launch_bounds__(THREADS *PACKED) void block_norm_kernel(NormArgs a)
 {
     __shared__ float shared[4 * THREADS / 64];
     const int64_t row = (int64_t)blockIdx.x * PACKED + (PACKED > 1 ? threadIdx.x / THREADS : 0);
     if (row >= a.rows) return;
-    Row<THREADS, E, WHOLE> of = {(int)(PACKED > 1 ? threadIdx.x % THREADS : threadIdx.x), a.dim, shared, 0};
-    Raw x[E], r[E], w[E], pw[E], g[E];
-    of.load(x, a.x, TYPE, row * a.x_stride);
-    if (a.r) of.load(r, a.r, a.r_type, row * a.r_stride);
-    if (a.post_weight) of.load(pw, a.post_weight, a.p_type, 0);
-    if (a.gate) of.load(g, a.gate, a.p_type, row / a.gate_rows * a.gate_stride);
-    if (a.weight) of.load(w, a.weight, a.p_type, 0);
-    float v[E][8], f[8];
+    Row<THREADS, E> of = {(int)(PACKED > 1 ? threadIdx.x % THREADS : threadIdx.x), a.dim, 1.0f / a.dim, shared, 0};
+    // (chunks beyond a whole row: the first elements, and zeros from where they are decoded on)
+    auto at = [&](int k) { return WHOLE && of.at(k) >= a.dim ? 0 : of.at(k); };
+    auto count = [&](int k) { return WHOLE ? 8 : of.count(k); };
+    Raw<TYPE> x[E];
+    Raw<RTYPE> r[E];
+    RawParameters pw[E], g[E], w[E];
 #pragma unroll
-    for (int k = 0; k < E; ++k) decode(x[k], TYPE, v[k]);
+    for (int k = 0; k < E; ++k) x[k] = load<TYPE>(a.x, row * a.x_stride + at(k), count(k));
+    if (a.r)
+#pragma unroll
+        for (int k = 0; k < E; ++k) r[k] = load<RTYPE>(a.r, row * a.r_stride + at(k), count(k));
+    auto ask = [&](RawParameters (&to)[E], const void *p, int64_t from) {
+        if (!p) return;
+        if (a.p_type == MC_F32) {
+#pragma unroll
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F32, from + at(k), count(k));
+        } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F16, from + at(k), count(k));
+        }
+    };
+    ask(pw, a.post_weight, 0);
+    ask(g, a.gate, row / a.gate_rows * a.gate_stride);
+    ask(w, a.weight, 0);
+    float v[E][8], f[8];
+    auto times = [&](const RawParameters (&p)[E], const void *there, const void *bias) {
+        if (there)
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                decode_parameters(p[k], a.p_type, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] *= f[e];
+            }
+        if (bias) {
+            RawParameters b[E];
+            ask(b, bias, 0);
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                decode_parameters(b[k], a.p_type, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] += f[e];
+            }
+        }
+    };
+    auto trim = [&] { // zeros beyond the row
+        if (WHOLE && E * THREADS * 8 == a.dim) return;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int n = of.count(k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = e < n ? v[k][e] : 0;
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < E; ++k) decode(x[k], v[k]);
+    trim();
     if (a.post) {
         of.norm(v, a.post, a.eps);
-        of.scale(v, pw, a.post_weight != nullptr, a.post_bias, a.p_type);
+        times(pw, a.post_weight, a.post_bias);
     }
-    if (a.gate) of.scale(v, g, true, nullptr, a.p_type);
+    times(g, a.gate, nullptr);
 #pragma unroll
     for (int k = 0; k < E; ++k) {
-        if (a.r) decode(r[k], a.r_type, f);
+        if (a.r) decode(r[k], f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[k][e] = a.branch_scale * v[k][e] + (a.r ? a.residual_scale * f[e] : 0);
     }
-    if (a.y) of.write(a.y, a.r_type, row * a.y_stride, v);
+    trim();
+    if (a.y) of.template write<RTYPE>(a.y, row * a.y_stride, v);
     if (!a.pre) return;
     of.norm(v, a.pre, a.eps);
-    of.scale(v, w, a.weight != nullptr, a.bias, a.p_type);
-    of.write(a.n, TYPE, row * a.n_stride, v);
+    times(w, a.weight, a.bias);
+    of.template write<TYPE>(a.n, row * a.n_stride, v);
 }
 
-// LAYER: gradients of biases are asked for, or one of the norms takes means
-template <int TYPE, int THREADS, int E, bool WHOLE, bool LAYER> __global__ __launch_bounds__(THREADS) void block_norm_backward_kernel(NormArgs a)
+// LAYER: one of the norms takes means, or there are biases.  Parameters stay in registers with one chunk to a thread, and are read again for each row (from
+// the caches) with more; the next row is asked for ahead with up to two.  SUMS false: the sums over rows, which would not fit into the registers of so wide a row, are left to
+// the kernel below, for which a row's means and deviations are written out.
+template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __global__ __launch_bounds__(THREADS, THREADS == 512 || (LAYER && RTYPE == MC_F32) ? 2 : 3) void block_norm_backward_kernel(NormArgs a)
 {
     __shared__ float shared[4 * THREADS / 64];
-    Row<THREADS, E, WHOLE> of = {(int)threadIdx.x, a.dim, shared, 0};
+    Row<THREADS, E> of = {(int)threadIdx.x, a.dim, 1.0f / a.dim, shared, 0};
     const int64_t first = blockIdx.x * a.per, end = min(first + a.per, a.rows);
-    Raw w[E], pw[E];
-    if (a.weight) of.load(w, a.weight, a.p_type, 0);
-    if (a.post_weight) of.load(pw, a.post_weight, a.p_type, 0);
-    float sum_g[E][8], sum_w[E][8], sum_pw[E][8], sum_b[LAYER ? E : 1][8], sum_pb[LAYER ? E : 1][8];
-#pragma unroll
-    for (int k = 0; k < E; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            sum_g[k][e] = sum_w[k][e] = sum_pw[k][e] = 0;
-            if constexpr (LAYER) sum_b[k][e] = sum_pb[k][e] = 0;
-        }
+    float w[E][8], pw[E][8], pb[LAYER ? E : 1][8], g[E][8]; // (g: times the branch's scale)
+    constexpr bool HELD = E == 1, AHEAD = E <= 2;
+    auto post_parameters = [&] {
+        of.parameters(pw, a.post_weight, a.p_type, 0, 1);
+        if constexpr (LAYER) of.parameters(pb, a.post_bias, a.p_type, 0, 0);
+    };
+    if constexpr (HELD) {
+        of.parameters(w, a.weight, a.p_type, 0, 1);
+        post_parameters();
+    }
+    if (!a.gate) EACH(k, e) g[k][e] = a.branch_scale;
+    float sum_g[E][8] = {}, sum_w[E][8] = {}, sum_pw[E][8] = {}, sum_b[LAYER ? E : 1][8] = {}, sum_pb[LAYER ? E : 1][8] = {};
     float *const mine = a.partial + (int64_t)blockIdx.x * 6 * a.dim;
-    for (int64_t row = first; row < end; ++row) {
-        Raw x[E], r[E], dn[E], dy[E], g[E];
-        of.load(x, a.x, TYPE, row * a.x_stride);
-        if (a.r) of.load(r, a.r, a.r_type, row * a.r_stride);
-        if (a.dn) of.load(dn, a.dn, TYPE, row * a.dn_stride);
-        if (a.dy) of.load(dy, a.dy, a.r_type, row * a.dy_stride);
-        if (a.gate) of.load(g, a.gate, a.p_type, row / a.gate_rows * a.gate_stride);
-        float hat1[E][8], hat2[E][8], d[E][8], f[8], h[8];
-#pragma unroll
-        for (int k = 0; k < E; ++k) decode(x[k], TYPE, hat1[k]);
-        const float r1 = a.post ? of.norm(hat1, a.post, a.eps) : 1;
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!WHOLE || E > 1) hat1[k][e] = e < of.count(k) ? hat1[k][e] : 0; // (what lies beyond the row stays out of all sums)
-                d[k][e] = hat1[k][e];
-            }
-        auto branch = [&](float (&v)[E][8]) { // a from xhat
-            if (a.post) of.scale(v, pw, a.post_weight != nullptr, LAYER ? a.post_bias : nullptr, a.p_type);
-        };
-        branch(d);
+    Raw<TYPE> rx[E], rdn[E];
+    Raw<RTYPE> rr[E], rdy[E];
+    auto ask = [&](int64_t row) {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            if (a.r) decode(r[k], a.r_type, f);
-            if (a.gate) decode(g[k], a.p_type, h);
+            const int n = row < end ? of.count(k) : 0;
+            rx[k] = load<TYPE>(a.x, row * a.x_stride + of.at(k), n);
+            rr[k] = load<RTYPE>(a.r, row * a.r_stride + of.at(k), a.r ? n : 0);
+            rdn[k] = load<TYPE>(a.dn, row * a.dn_stride + of.at(k), a.dn ? n : 0);
+            rdy[k] = load<RTYPE>(a.dy, row * a.dy_stride + of.at(k), a.dy ? n : 0);
+        }
+    };
+    if constexpr (AHEAD) ask(first);
+    int64_t group = first / a.gate_rows, group_end = (group + 1) * a.gate_rows; // the row's gate, and where its rows end
+    bool fresh = true;
+    for (int64_t row = first; row < end; ++row) {
+        float hat1[E][8], hat2[E][8], d[E][8], dy[E][8];
+        if constexpr (!AHEAD) ask(row);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) hat2[k][e] = a.branch_scale * (a.gate ? h[e] * d[k][e] : d[k][e]) + (a.r ? a.residual_scale * f[e] : 0);
+        for (int k = 0; k < E; ++k) {
+            decode(rx[k], hat1[k]);
+            decode(rr[k], hat2[k]);
+            decode(rdn[k], d[k]);
+            decode(rdy[k], dy[k]);
+        }
+        if constexpr (AHEAD) ask(row + 1);
+        if (a.gate && (fresh || !HELD)) {
+            of.parameters(g, a.gate, a.p_type, group * a.gate_stride, 1);
+            EACH(k, e) g[k][e] *= a.branch_scale;
+        }
+        float m1 = 0, m2 = 0, r2 = 0, mean2 = 0, dot2 = 0;
+        const float r1 = a.post ? of.norm(hat1, a.post, a.eps, m1) : 1;
+        if constexpr (!HELD) post_parameters();
+        EACH(k, e) {
+            float b = hat1[k][e] * pw[k][e];
+            if constexpr (LAYER) b += pb[k][e];
+            hat2[k][e] = g[k][e] * b + (a.r ? a.residual_scale * hat2[k][e] : 0); // y
         }
         if (a.pre && a.dn) {
-            const float r2 = of.norm(hat2, a.pre, a.eps);
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                decode(dn[k], TYPE, d[k]);
-                if (a.weight) decode(w[k], a.p_type, h);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    d[k][e] = e < of.count(k) ? d[k][e] : 0;
-                    sum_w[k][e] += d[k][e] * hat2[k][e];
-                    if constexpr (LAYER) sum_b[k][e] += d[k][e];
-                    if (a.weight) d[k][e] *= h[e];
+            float mean = 0, dot = 0;
+            if constexpr (!HELD) of.parameters(w, a.weight, a.p_type, 0, 1);
+            if (LAYER) {
+                r2 = of.norm(hat2, a.pre, a.eps, m2);
+                EACH(k, e) {
+                    mean += d[k][e] * w[k][e];
+                    dot += d[k][e] * w[k][e] * hat2[k][e];
                 }
+                of.sums(mean, dot);
+                mean = a.pre == MC_NORM_LAYER ? mean / a.dim : 0;
+                dot /= a.dim;
+            } else { // (both sums at once, of y that is not normed yet)
+                float q = 0;
+                EACH(k, e) {
+                    q += hat2[k][e] * hat2[k][e];
+                    dot += d[k][e] * w[k][e] * hat2[k][e];
+                }
+                of.sums(q, dot);
+                r2 = 1.0f / sqrtf(q * of.inverse + a.eps);
+                dot *= r2 * of.inverse;
+                EACH(k, e) hat2[k][e] *= r2;
             }
-            of.norm_backward(d, hat2, r2, a.pre);
-        } else {
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[k][e] = 0;
+            mean2 = mean, dot2 = dot;
+            EACH(k, e) {
+                if constexpr (SUMS) sum_w[k][e] += d[k][e] * hat2[k][e];
+                if constexpr (SUMS && LAYER) sum_b[k][e] += d[k][e];
+                dy[k][e] += r2 * (d[k][e] * w[k][e] - mean - hat2[k][e] * dot);
+            }
         }
-        if (a.dy)
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                decode(dy[k], a.r_type, f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[k][e] += e < of.count(k) ? f[e] : 0;
-            }
         if (a.dr) {
-            float v[E][8];
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] = a.residual_scale * d[k][e];
-            of.write(a.dr, a.r_type, row * a.dr_stride, v);
+            EACH(k, e) d[k][e] = a.residual_scale * dy[k][e];
+            of.template write<RTYPE>(a.dr, row * a.dr_stride, d);
         }
-        // the branch's share: d becomes da, the gate's gradient takes a
-        if (a.grads[0]) {
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) hat2[k][e] = hat1[k][e];
-            branch(hat2);
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum_g[k][e] += a.branch_scale * hat2[k][e] * d[k][e];
-            // a row of the gate ends here, or the workgroup does: written out whole, or left for the second kernel in the place of a gate's row that began before (0) or in (1) these rows
-            const int64_t group = row / a.gate_rows, begin = group * a.gate_rows;
-            const bool last = row + 1 == begin + a.gate_rows;
-            if (last || row + 1 == end) {
-                if (last && begin >= first) of.write(a.grads[0], a.p_type, group * a.dgate_stride, sum_g);
-                else of.write(mine, MC_F32, begin < first ? 0 : a.dim, sum_g);
-#pragma unroll
-                for (int k = 0; k < E; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum_g[k][e] = 0;
+        if (!SUMS && threadIdx.x == 0) {
+            float *to = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
+            to[0] = m1, to[1] = r1, to[2] = m2, to[3] = r2, to[4] = mean2, to[5] = dot2;
+        }
+        float mean = 0, dot = 0;
+        if constexpr (!HELD) {
+            post_parameters();
+            if (a.gate) {
+                of.parameters(g, a.gate, a.p_type, group * a.gate_stride, 1);
+                EACH(k, e) g[k][e] *= a.branch_scale;
             }
         }
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            if (a.gate) decode(g[k], a.p_type, h);
-            if (a.post_weight) decode(pw[k], a.p_type, f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                d[k][e] *= a.branch_scale;
-                if (a.gate) d[k][e] *= h[e];
-                sum_pw[k][e] += d[k][e] * hat1[k][e];
-                if constexpr (LAYER) sum_pb[k][e] += d[k][e];
-                if (a.post_weight) d[k][e] *= f[e];
+        EACH(k, e) {
+            const float da = g[k][e] * dy[k][e];
+            if constexpr (SUMS) {
+                float b = hat1[k][e] * pw[k][e];
+                if constexpr (LAYER) b += pb[k][e];
+                sum_g[k][e] += a.branch_scale * b * dy[k][e];
+                sum_pw[k][e] += da * hat1[k][e];
+                if constexpr (LAYER) sum_pb[k][e] += da;
             }
+            d[k][e] = da * pw[k][e];
+            mean += e < of.count(k) ? d[k][e] : 0;
+            dot += e < of.count(k) ? d[k][e] * hat1[k][e] : 0;
         }
+        // a row of the gate ends here, or the workgroup does: written out whole, or left for the second kernel in the place of a gate's row that began before (0) or in (1) these rows
+        fresh = row + 1 == group_end;
+        if (SUMS && a.grads[0] && (fresh || row + 1 == end)) {
+            const int64_t begin = group_end - a.gate_rows;
+            if (fresh && begin >= first) of.write_parameters(a.grads[0], a.p_type, group * a.dgate_stride, sum_g);
+            else of.template write<MC_F32>(mine, begin < first ? 0 : a.dim, sum_g);
+            EACH(k, e) sum_g[k][e] = 0;
+        }
+        if (fresh) ++group, group_end += a.gate_rows;
         if (!a.dx) continue;
-        if (a.post) of.norm_backward(d, hat1, r1, a.post);
-        of.write(a.dx, TYPE, row * a.dx_stride, d);
+        if (a.post) {
+            of.sums(mean, dot);
+            mean = LAYER && a.post == MC_NORM_LAYER ? mean / a.dim : 0;
+            dot /= a.dim;
+            EACH(k, e) d[k][e] = r1 * (d[k][e] - mean - hat1[k][e] * dot);
+        }
+        of.template write<TYPE>(a.dx, row * a.dx_stride, d);
     }
-    if (a.grads[1]) of.write(mine, MC_F32, 2 * a.dim, sum_w);
-    if (a.grads[3]) of.write(mine, MC_F32, 4 * a.dim, sum_pw);
+    if constexpr (!SUMS) return;
+    if (a.grads[1]) of.template write<MC_F32>(mine, 2 * a.dim, sum_w);
+    if (a.grads[3]) of.template write<MC_F32>(mine, 4 * a.dim, sum_pw);
     if constexpr (LAYER) {
-        if (a.grads[2]) of.write(mine, MC_F32, 3 * a.dim, sum_b);
-        if (a.grads[4]) of.write(mine, MC_F32, 5 * a.dim, sum_pb);
+        if (a.grads[2]) of.template write<MC_F32>(mine, 3 * a.dim, sum_b);
+        if (a.grads[4]) of.template write<MC_F32>(mine, 5 * a.dim, sum_pb);
     }
+}
+
+// The sums over rows, of COLUMNS_EACH columns (eight to a thread) and one workgroup's rows, where the kernel above does not keep them: the same terms again, from the row's
+// means and deviations.
+constexpr int COLUMN_THREADS = 256, COLUMNS_EACH = 8 * COLUMN_THREADS;
+template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void block_norm_columns_kernel(NormArgs a)
+{
+    constexpr int E = 1;
+    const int64_t first = blockIdx.y * a.per, end = min(first + a.per, a.rows);
+    const int left = a.dim - (int)blockIdx.x * COLUMNS_EACH, shift = blockIdx.x * COLUMNS_EACH; // columns from here on
+    Row<COLUMN_THREADS, 1> of = {(int)threadIdx.x, left, 0, nullptr, 0};
+    const int n = of.count(0), at = shift + of.at(0);
+    auto from = [&](const void *p) { return p ? static_cast<const char *>(p) + (int64_t)shift * (a.p_type == MC_F32 ? 4 : 2) : nullptr; };
+    float w[1][8], pw[1][8], pb[1][8], g[1][8];
+    of.parameters(w, from(a.weight), a.p_type, 0, 1);
+    of.parameters(pw, from(a.post_weight), a.p_type, 0, 1);
+    of.parameters(pb, from(a.post_bias), a.p_type, 0, 0);
+    if (!a.gate) EACH(k, e) g[k][e] = a.branch_scale;
+    float sum_g[1][8] = {}, sum_w[1][8] = {}, sum_pw[1][8] = {}, sum_b[1][8] = {}, sum_pb[1][8] = {};
+    float *const mine = a.partial + (int64_t)blockIdx.y * 6 * a.dim + shift;
+    int64_t group = first / a.gate_rows, group_end = (group + 1) * a.gate_rows;
+    bool fresh = true;
+    for (int64_t row = first; row < end; ++row) {
+        const float *of_row = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
+        const float m1 = of_row[0], r1 = of_row[1], m2 = of_row[2], r2 = of_row[3], mean = of_row[4], dot = of_row[5];
+        float x[8], r[8], dn[8], dy[8];
+        const Raw<TYPE> rx = load<TYPE>(a.x, row * a.x_stride + at, n), rdn = load<TYPE>(a.dn, row * a.dn_stride + at, a.dn ? n : 0);
+        const Raw<RTYPE> rr = load<RTYPE>(a.r, row * a.r_stride + at, a.r ? n : 0), rdy = load<RTYPE>(a.dy, row * a.dy_stride + at, a.dy ? n : 0);
+        if (a.gate && fresh) {
+            of.parameters(g, from(a.gate), a.p_type, group * a.gate_stride, 1);
+            EACH(k, e) g[k][e] *= a.branch_scale;
+        }
+        decode(rx, x);
+        decode(rr, r);
+        decode(rdn, dn);
+        decode(rdy, dy);
+        EACH(k, e) {
+            const float hat1 = (x[e] - m1) * r1, b = hat1 * pw[k][e] + pb[k][e], y = g[k][e] * b + (a.r ? a.residual_scale * r[e] : 0), hat2 = (y - m2) * r2;
+            const float dyt = dy[e] + r2 * (dn[e] * w[k][e] - mean - hat2 * dot), da = g[k][e] * dyt;
+            sum_w[k][e] += dn[e] * hat2;
+            sum_b[k][e] += dn[e];
+            sum_g[k][e] += a.branch_scale * b * dyt;
+            sum_pw[k][e] += da * hat1;
+            sum_pb[k][e] += da;
+        }
+        fresh = row + 1 == group_end; // (see the kernel above)
+        if (a.grads[0] && (fresh || row + 1 == end)) {
+            const int64_t begin = group_end - a.gate_rows;
+            if (fresh && begin >= first) of.write_parameters(a.grads[0], a.p_type, group * a.dgate_stride + shift, sum_g);
+            else of.template write<MC_F32>(mine, begin < first ? 0 : a.dim, sum_g);
+            EACH(k, e) sum_g[k][e] = 0;
+        }
+        if (fresh) ++group, group_end += a.gate_rows;
+    }
+    if (a.grads[1]) of.template write<MC_F32>(mine, 2 * a.dim, sum_w);
+    if (a.grads[2]) of.template write<MC_F32>(mine, 3 * a.dim, sum_b);
+    if (a.grads[3]) of.template write<MC_F32>(mine, 4 * a.dim, sum_pw);
+    if (a.grads[4]) of.template write<MC_F32>(mine, 5 * a.dim, sum_pb);
 }
 
 __device__ __forceinline__ void store_one(void *p, int type, int64_t at, float v)
@@ -390,13 +483,13 @@ __device__ __forceinline__ void store_one(void *p, int type, int64_t at, float v
     else static_cast<__bf16 *>(p)[at] = (__bf16)v;
 }
 
-constexpr int SUM_COLUMNS = 64, SUM_LINES = 16;
-// The workgroups' sums of 64 columns, 16 threads to a column.  blockIdx.y: 0 .. 3 the parameters, from 4 on rows of the gate that several
+constexpr int SUM_COLUMNS = 64, SUM_LINES = 64;
+// The workgroups' sums of 64 columns, four to a thread and 64 threads to a column.  blockIdx.y: 0 .. 3 the parameters, from 4 on rows of the gate that several
 // workgroups share: by the row's number, or (`by_border`) by the first border between workgroups that lies in it.
-__global__ __launch_bounds__(SUM_COLUMNS *SUM_LINES) void block_norm_sum_kernel(NormArgs a, int by_border)
+__global__ __launch_bounds__(SUM_COLUMNS / 4 * SUM_LINES) void block_norm_sum_kernel(NormArgs a, int by_border)
 {
-    __shared__ float part[SUM_LINES][SUM_COLUMNS];
-    const int column = blockIdx.x * SUM_COLUMNS + threadIdx.x % SUM_COLUMNS, line = threadIdx.x / SUM_COLUMNS;
+    __shared__ float part[SUM_LINES][SUM_COLUMNS + 4];
+    const int quad = threadIdx.x % (SUM_COLUMNS / 4), line = threadIdx.x / (SUM_COLUMNS / 4), column = blockIdx.x * SUM_COLUMNS + 4 * quad;
     int from = 0, to = a.workgroups - 1, slot = 1 + (int)blockIdx.y + 1;
     int64_t group = 0;
     void *out;
@@ -409,92 +502,104 @@ __global__ __launch_bounds__(SUM_COLUMNS *SUM_LINES) void block_norm_sum_kernel(
         const int64_t begin = group * a.gate_rows, last = begin + a.gate_rows - 1;
         from = (int)(begin / a.per);
         to = (int)(last / a.per);
-        if (from == to || (by_border && from != i)) return;
+        if (a.rows > 0 && (from == to || (by_border && from != i))) return;
         out = a.grads[0];
         slot = -1;
     }
-    float s = 0;
-    if (column < a.dim)
+    float s[4] = {0, 0, 0, 0};
+    const int n = a.dim - column;
+    if (n > 0 && a.rows > 0) {
+#pragma unroll 4
         for (int w = from + line; w <= to; w += SUM_LINES) {
             const int place = slot >= 0 ? slot : group * a.gate_rows < w * a.per ? 0 : 1;
-            s += a.partial[((int64_t)w * 6 + place) * a.dim + column];
-        }
-    part[line][threadIdx.x % SUM_COLUMNS] = s;
-    __syncthreads();
-    if (line != 0 || column >= a.dim) return;
+            const float *p = a.partial + ((int64_t)w * 6 + place) * a.dim + column;
+            float v[4];
+            if (n >= 4) {
+                __builtin_memcpy(v, p, 16);
+            } else {
 #pragma unroll
-    for (int l = 1; l < SUM_LINES; ++l) s += part[l][threadIdx.x];
-    store_one(out, a.p_type, (slot >= 0 ? 0 : group * a.dgate_stride) + column, s);
+                for (int e = 0; e < 4; ++e) v[e] = e < n ? p[e] : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
+    }
+    __builtin_memcpy(&part[line][4 * quad], s, 16);
+    __syncthreads();
+    if (threadIdx.x >= SUM_COLUMNS || (int)(blockIdx.x * SUM_COLUMNS + threadIdx.x) >= a.dim) return;
+    float sum = 0;
+#pragma unroll 8
+    for (int l = 0; l < SUM_LINES; ++l) sum += part[l][threadIdx.x];
+    store_one(out, a.p_type, (slot >= 0 ? 0 : group * a.dgate_stride) + blockIdx.x * SUM_COLUMNS + threadIdx.x, sum);
 }
 
-template <int TYPE, int THREADS, int E, bool WHOLE> hipError_t forward(const NormArgs &a, hipStream_t s)
+template <int TYPE, int RTYPE, int THREADS, int E> hipError_t forward(const NormArgs &a, hipStream_t s)
 {
     constexpr int PACKED = THREADS == 64 ? 4 : 1;
-    return launch_kernel((block_norm_kernel<TYPE, THREADS, E, WHOLE, PACKED>), dim3((unsigned)((a.rows + PACKED - 1) / PACKED)), dim3(THREADS * PACKED), 0, s, a);
+    const dim3 grid((unsigned)((a.rows + PACKED - 1) / PACKED)), block(THREADS * PACKED);
+    return a.dim % 8 == 0 ? launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, true>), grid, block, 0, s, a)
+                          : launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, false>), grid, block, 0, s, a);
+}
+template <int TYPE, int RTYPE> hipError_t forward_of(const NormArgs &a, hipStream_t s)
+{
+    if (a.dim <= 512) return forward<TYPE, RTYPE, 64, 1>(a, s);
+    if (a.dim <= 1024) return forward<TYPE, RTYPE, 64, 2>(a, s);
+    if (a.dim <= 2048) return forward<TYPE, RTYPE, 256, 1>(a, s);
+    if (a.dim <= 4096) return forward<TYPE, RTYPE, 256, 2>(a, s);
+    if (a.dim <= 8192) return forward<TYPE, RTYPE, 512, 2>(a, s);
+    return forward<TYPE, RTYPE, 1024, 2>(a, s);
 }
 
-template <int TYPE> hipError_t forward_type(const NormArgs &a, hipStream_t s)
+template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> hipError_t backward(const NormArgs &a, hipStream_t s)
 {
-    if (a.dim % 8 != 0) {
-        if (a.dim <= 1024) return forward<TYPE, 64, 2, false>(a, s);
-        if (a.dim <= 4096) return forward<TYPE, 256, 2, false>(a, s);
-        return forward<TYPE, 1024, 2, false>(a, s);
-    }
-    if (a.dim <= 512) return forward<TYPE, 64, 1, true>(a, s);
-    if (a.dim <= 1024) return forward<TYPE, 64, 2, true>(a, s);
-    if (a.dim <= 2048) return forward<TYPE, 256, 1, true>(a, s);
-    if (a.dim <= 4096) return forward<TYPE, 256, 2, true>(a, s);
-    if (a.dim <= 8192) return forward<TYPE, 512, 2, true>(a, s);
-    return forward<TYPE, 1024, 2, true>(a, s);
+    const hipError_t e = launch_kernel((block_norm_backward_kernel<TYPE, RTYPE, THREADS, E, LAYER, SUMS>), dim3(a.workgroups), dim3(THREADS), 0, s, a);
+    if (SUMS || e != hipSuccess || !(a.grads[0] || a.grads[1] || a.grads[2] || a.grads[3] || a.grads[4])) return e;
+    return launch_kernel((block_norm_columns_kernel<TYPE, RTYPE>), dim3((a.dim + COLUMNS_EACH - 1) / COLUMNS_EACH, a.workgroups), dim3(COLUMN_THREADS), 0, s, a);
 }
-
-template <int TYPE, int THREADS, int E, bool WHOLE> hipError_t backward(const NormArgs &a, hipStream_t s)
+template <int TYPE, int RTYPE, bool LAYER> hipError_t backward_kind(const NormArgs &a, hipStream_t s)
 {
-    const bool layer = a.pre == MC_NORM_LAYER || a.post == MC_NORM_LAYER || a.bias || a.post_bias || a.grads[2] || a.grads[4];
-    const dim3 grid(a.workgroups), block(THREADS);
-    return layer ? launch_kernel((block_norm_backward_kernel<TYPE, THREADS, E, WHOLE, true>), grid, block, 0, s, a)
-                 : launch_kernel((block_norm_backward_kernel<TYPE, THREADS, E, WHOLE, false>), grid, block, 0, s, a);
+    if (a.dim <= 512) return backward<TYPE, RTYPE, 64, 1, LAYER, true>(a, s);
+    if (a.dim <= 1024) return backward<TYPE, RTYPE, 128, 1, LAYER, true>(a, s);
+    if (a.dim <= 2048) return backward<TYPE, RTYPE, 256, 1, LAYER, true>(a, s);
+    if (a.dim <= 4096) return backward<TYPE, RTYPE, 512, 1, LAYER, true>(a, s);
+    if (a.dim <= 8192) return backward<TYPE, RTYPE, 512, 2, LAYER, !LAYER && TYPE != MC_F32>(a, s);
+    return backward<TYPE, RTYPE, 512, 4, LAYER, false>(a, s);
 }
-
-template <int TYPE> hipError_t backward_type(const NormArgs &a, hipStream_t s)
+template <int TYPE, int RTYPE> hipError_t backward_of(const NormArgs &a, hipStream_t s)
 {
-    if (a.dim % 8 != 0) {
-        if (a.dim <= 1024) return backward<TYPE, 64, 2, false>(a, s);
-        if (a.dim <= 4096) return backward<TYPE, 256, 2, false>(a, s);
-        return backward<TYPE, 512, 4, false>(a, s);
-    }
-    if (a.dim <= 512) return backward<TYPE, 64, 1, true>(a, s);
-    if (a.dim <= 1024) return backward<TYPE, 64, 2, true>(a, s);
-    if (a.dim <= 2048) return backward<TYPE, 256, 1, true>(a, s);
-    if (a.dim <= 4096) return backward<TYPE, 256, 2, true>(a, s);
-    if (a.dim <= 8192) return backward<TYPE, 512, 2, true>(a, s);
-    return backward<TYPE, 512, 4, true>(a, s);
+    const bool layer = a.pre == MC_NORM_LAYER || a.post == MC_NORM_LAYER || a.bias || a.post_bias;
+    return layer ? backward_kind<TYPE, RTYPE, true>(a, s) : backward_kind<TYPE, RTYPE, false>(a, s);
 }
 
 } // namespace
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t s)
 {
-    return a.type == MC_F32 ? forward_type<MC_F32>(a, s) : a.type == MC_F16 ? forward_type<MC_F16>(a, s) : forward_type<MC_BF16>(a, s);
+    if (a.type == MC_F32) return forward_of<MC_F32, MC_F32>(a, s);
+    if (a.type == MC_F16) return a.r_type == MC_F16 ? forward_of<MC_F16, MC_F16>(a, s) : forward_of<MC_F16, MC_F32>(a, s);
+    return a.r_type == MC_BF16 ? forward_of<MC_BF16, MC_BF16>(a, s) : forward_of<MC_BF16, MC_F32>(a, s);
 }
 
 hipError_t launch_block_norm_backward(NormArgs a, hipStream_t s)
 {
+    const bool params = a.grads[1] || a.grads[2] || a.grads[3] || a.grads[4];
+    const dim3 block(SUM_COLUMNS / 4 * SUM_LINES);
+    const unsigned columns = (a.dim + SUM_COLUMNS - 1) / SUM_COLUMNS;
     if (a.rows == 0) { // sums over no rows
         a.per = 1;
         a.workgroups = 0;
-        return launch_kernel(block_norm_sum_kernel, dim3((a.dim + SUM_COLUMNS - 1) / SUM_COLUMNS, (unsigned)(4 + (a.grads[0] ? a.gate_groups : 0))), dim3(SUM_COLUMNS * SUM_LINES), 0, s, a, 0);
+        return launch_kernel(block_norm_sum_kernel, dim3(columns, (unsigned)(4 + (a.grads[0] ? a.gate_groups : 0))), block, 0, s, a, 0);
     }
     a.workgroups = norm_workgroups(a.rows, a.dim);
     a.per = (a.rows + a.workgroups - 1) / a.workgroups;
     a.workgroups = (int)((a.rows + a.per - 1) / a.per);
-    const hipError_t e = a.type == MC_F32 ? backward_type<MC_F32>(a, s) : a.type == MC_F16 ? backward_type<MC_F16>(a, s) : backward_type<MC_BF16>(a, s);
-    const bool params = a.grads[1] || a.grads[2] || a.grads[3] || a.grads[4];
+    const hipError_t e = a.type == MC_F32 ? backward_of<MC_F32, MC_F32>(a, s)
+                       : a.type == MC_F16 ? (a.r_type == MC_F16 ? backward_of<MC_F16, MC_F16>(a, s) : backward_of<MC_F16, MC_F32>(a, s))
+                                          : (a.r_type == MC_BF16 ? backward_of<MC_BF16, MC_BF16>(a, s) : backward_of<MC_BF16, MC_F32>(a, s));
     // rows of the gate that no border between workgroups can cut: written by the first kernel
     const bool cut = a.grads[0] && a.workgroups > 1 && a.gate_rows > 1;
     if (e != hipSuccess || (!params && !cut)) return e;
-    const int64_t groups = a.gate_groups;
-    const int by_border = groups > a.workgroups - 1;
-    const unsigned gates = cut ? (unsigned)(by_border ? a.workgroups - 1 : groups) : 0;
-    return launch_kernel(block_norm_sum_kernel, dim3((a.dim + SUM_COLUMNS - 1) / SUM_COLUMNS, 4 + gates), dim3(SUM_COLUMNS * SUM_LINES), 0, s, a, by_border);
+    const int by_border = a.gate_groups > a.workgroups - 1;
+    const unsigned gates = cut ? (unsigned)(by_border ? a.workgroups - 1 : a.gate_groups) : 0;
+    return launch_kernel(block_norm_sum_kernel, dim3(columns, 4 + gates), block, 0, s, a, by_border);
 }

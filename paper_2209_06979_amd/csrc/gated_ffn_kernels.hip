@@ -96,9 +96,11 @@ template <class T, int RUN> __device__ __forceinline__ void store_run(T *to, con
 #pragma unroll
     for (int e = 0; e < RUN; ++e) h[e] = (T)v[e];
     if (n >= RUN) return (void)__builtin_memcpy(to, h, RUN * sizeof(T));
+    asm volatile("" ::: "memory"); // (the compiler would else make some of the stores those of both cases, and write whole runs in parts)
 #pragma unroll
     for (int e = 0; e < RUN; ++e)
         if (e < n) to[e] = h[e];
+    asm volatile("" ::: "memory");
 }
 
 // ---- the tiled product ------------------------------------------------------------------------------------------------------

@@ -26,13 +26,13 @@ struct NormArgs {
     int64_t dgate_stride;
     int64_t per;                   // rows of a workgroup (filled by the launcher)
     int workgroups;
-    float *partial;                // workgroups x (2 for the gate, 4) x dim
+    float *partial;                // workgroups x (2 for the gate, 4) x dim; rows of more than NORM_SUMS elements: eight floats for each row
 };
-constexpr int NORM_MOST_DIM = 16384;
-// Workgroups that a backward pass is cut into, at most (rows of up to 1024 elements: workgroups of one wave)
+constexpr int NORM_MOST_DIM = 16384, NORM_SUMS = 4096;
+// Workgroups that a backward pass is cut into, at most: as many as run at once
 inline int norm_workgroups(int64_t rows, int dim)
 {
-    const int most = dim <= 1024 ? 2048 : 512;
+    const int most = dim <= 512 ? 2048 : dim <= 1024 ? 1536 : dim <= 2048 ? 768 : 256;
     return (int)(rows < most ? rows : most);
 }
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t s);

@@ -159,7 +159,7 @@ extern "C" int mc_block_norm(const mc_block_norm_args *args, void *y_dev, int64_
 extern "C" size_t mc_block_norm_backward_workspace(int64_t rows, int dim)
 {
     if (rows < 1 || rows > 0x7fffffff || dim < 1 || dim > NORM_MOST_DIM) return 0;
-    return (size_t)norm_workgroups(rows, dim) * 6 * dim * sizeof(float);
+    return ((size_t)norm_workgroups(rows, dim) * 6 * dim + (dim > NORM_SUMS ? 8 * (size_t)rows : 0)) * sizeof(float);
 }
 
 extern "C" int mc_block_norm_backward(const mc_block_norm_args *args, const void *dy_dev, int64_t dy_stride, const void *dn_dev, int64_t dn_stride,

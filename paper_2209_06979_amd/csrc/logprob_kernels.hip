@@ -298,9 +298,11 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void logprob_backward_
         if (all) {
             __builtin_memcpy(dx + from, &d, 16);
         } else if (i + u * THREADS < end) {
+            asm volatile("" ::: "memory"); // (whole vectors are written as such)
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 if (from + e < a.vocab) dx[from + e] = d.e[e];
+            asm volatile("" ::: "memory");
         }
     }
     if (!a.dtop || none) return;
