@@ -3,8 +3,9 @@
 //   s = sum e^z,  t = sum e^z d,   log p = z - log s,   entropy = log s - scale t / s,
 // kept per thread for the largest x so far and rescaled when a larger one comes (four vectors of 16 bytes at a time).
 // The largest `top` logits are kept by each wave as keys in one register pair, sorted over its lanes: a vector whose largest element is below
-// the last of them is passed over by one comparison, and an element above it is moved into its place.  After the first vectors the
-// largest of each lane, sorted, give a bound that `top` elements reach, so that only about as many are put in place at the start.
+// the last of them is passed over by one comparison, and an element above it is moved into its place.  The four waves of a workgroup share a
+// bound: where each has a quarter of `top` keys that reach it, what is below it is not among the row's `top`.  It comes first from the largest element of
+// each lane after the first vectors, sorted, so that only about `top` elements are put in place at the start, and rises with the waves' keys.
 // A row is read by one workgroup, or cut into pieces where there are few rows; a second kernel joins these.
 #include "layer.h"
 
@@ -60,6 +61,13 @@ __device__ __forceinline__ Key smaller(Key a, Key b) { return a > b ? b : a; }
 __device__ __forceinline__ Key key_of_lane(Key k, int lane)
 {
     return (Key)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// The key of the lane before (lane 0: its own)
+__device__ __forceinline__ Key key_before(Key k)
+{
+    const int hi = (int)(k >> 32), lo = (int)k;
+    return (Key)(unsigned)__builtin_amdgcn_update_dpp(hi, hi, 0x138, 0xf, 0xf, false) << 32 | (unsigned)__builtin_amdgcn_update_dpp(lo, lo, 0x138, 0xf, 0xf, false);
 }
 
 // The 64 largest of two lists that fall from lane 0 on (`other` read backwards): larger elements of both make a bitonic list, which six exchanges sort.
@@ -141,6 +149,14 @@ template <int TYPE, bool TOP> __global__ __launch_bounds__(THREADS) void logprob
     Key held = 0;                    // of this lane's place
     Key last = 0;                    // the key at place top - 1, of all lanes
     unsigned bound = 0;              // what a key's logit has to reach
+    const int quarter = TOP ? (a.top + WAVES - 1) / WAVES - 1 : 0; // place of a wave's key that the bound goes by
+    __shared__ unsigned reached[WAVES]; // those keys' logits: they only rise, so that a wave that reads old ones has a lower bound
+    auto common = [&] {
+        unsigned b = __hip_atomic_load(&reached[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) b = min(b, __hip_atomic_load(&reached[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+        bound = max(bound, (unsigned)__builtin_amdgcn_readfirstlane((int)b));
+    };
     for (int at = first; at < end; at += THREADS * UNROLL) {
         Vector<TYPE> v[UNROLL];
         const int i = at + (int)threadIdx.x;
@@ -177,14 +193,20 @@ template <int TYPE, bool TOP> __global__ __launch_bounds__(THREADS) void logprob
                 unsigned o = ordered(most[0]);
 #pragma unroll
                 for (int u = 1; u < UNROLL; ++u) o = max(o, ordered(most[u]));
-                bound = (unsigned)__builtin_amdgcn_readlane((int)sorted(o, lane), a.top - 1);
+                o = sorted(o, lane);
+                bound = (unsigned)__builtin_amdgcn_readlane((int)o, a.top - 1); // (at least `top` of this wave's elements reach it)
+                if (lane == quarter) reached[wave] = o;
+                __syncthreads(); // (every wave comes here once: a piece is no shorter than one batch's first vectors, or its elements are -infinity)
             }
+            common();
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
-                if (__ballot(ordered(most[u]) >= bound) == 0) continue;
+                float least = logit_of((Key)bound << 32); // (a NaN is not below it)
+                if (__ballot(!(most[u] < least)) == 0) continue;
                 const int from = (i + u * THREADS) * N;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
+                    if (__ballot(!((float)v[u].e[e] < least)) == 0) continue;
                     const Key k = (Key)ordered((float)v[u].e[e]) << 32 | (unsigned)~(unsigned)(from + e);
                     unsigned long long more = __ballot((unsigned)(k >> 32) >= bound && k > last && from + e < a.vocab);
                     while (more) {
@@ -193,13 +215,18 @@ template <int TYPE, bool TOP> __global__ __launch_bounds__(THREADS) void logprob
                         const Key fresh = key_of_lane(k, l);
                         if (fresh <= last) continue;
                         const int place = __builtin_popcountll(__ballot(held > fresh));
-                        const Key before = __shfl_up(held, 1);
+                        const Key before = key_before(held);
                         held = lane < place ? held : lane == place ? fresh : before;
                         last = key_of_lane(held, a.top - 1);
                         bound = max(bound, (unsigned)(last >> 32));
                     }
+                    least = logit_of((Key)bound << 32);
                 }
             }
+            // (a key of 0 stands for none)
+            const unsigned mine = (unsigned)(key_of_lane(held, quarter) >> 32);
+            if (lane == 0 && mine > __hip_atomic_load(&reached[wave], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP))
+                __hip_atomic_store(&reached[wave], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
     }
 
