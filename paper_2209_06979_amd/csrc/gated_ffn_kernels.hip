@@ -486,9 +486,19 @@ template <int TYPE> __global__ __launch_bounds__(256) void product_join_kernel(P
     const int column = (int)(id - z * all - row * quads) * 4, count = a.n - column;
     const float *from = a.partial + ((int64_t)z * a.m + row) * a.n + column;
     float v[4] = {0, 0, 0, 0};
-    for (int s = 0; s < a.splits; ++s, from += (int64_t)a.batch * a.m * a.n)
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const float *p = from + (int64_t)s * a.batch * a.m * a.n;
+        float w[4];
+        if (count >= 4) {
+            __builtin_memcpy(w, p, 16);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += e < count ? from[e] : 0;
+            for (int e = 0; e < 4; ++e) w[e] = e < count ? p[e] : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[e];
+    }
     store_run(static_cast<T *>(z ? a.c[1] : a.c[0]) + row * (z ? a.c_stride[1] : a.c_stride[0]) + column, v, count);
 }
 
@@ -643,9 +653,13 @@ template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, b
 
 template <int TYPE, bool AR, bool BR, int MODE> hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t s)
 {
-    if (tile == 256) return product<TYPE, 256, 256, 2, 4, TYPE == MC_F32 ? 128 : 64, TYPE == MC_F32 ? 2 : 4, AR, BR, MODE>(a, s);
-    if (tile == 128) return product<TYPE, 128, 128, 2, 2, 128, 2, AR, BR, MODE>(a, s);
-    return product<TYPE, 64, 64, 2, 2, 128, 3, AR, BR, MODE>(a, s);
+    switch (tile) {
+    case 256: return product<TYPE, 256, 256, 2, 4, TYPE == MC_F32 ? 128 : 64, TYPE == MC_F32 ? 2 : 4, AR, BR, MODE>(a, s);
+    case 128: return product<TYPE, 128, 128, 2, 2, 128, 2, AR, BR, MODE>(a, s);
+    case 96: return product<TYPE, 128, 64, 2, 2, 128, 3, AR, BR, MODE>(a, s);
+    case 64: return product<TYPE, 64, 64, 2, 2, 128, 3, AR, BR, MODE>(a, s);
+    default: return product<TYPE, 32, 64, 2, 2, 128, 3, AR, BR, MODE>(a, s);
+    }
 }
 
 template <int TYPE, bool AR> hipError_t product_plain(ProductArgs a, ProductPlan p, hipStream_t s)
@@ -671,22 +685,29 @@ template <int TYPE> hipError_t few_rows_of(const FewRowsArgs &a, hipStream_t s)
 
 } // namespace
 
+// The shape of tiles and number of pieces along k with the smallest expected time.  A step of 128 bytes of k takes a workgroup `alone` (us) by itself on a compute
+// unit, which runs `together` of them at once and spends `busy` on a step of each when it is full; the pieces' sums cost a launch and their bytes.
+// Measured, us, tiles of 256 x 256, 128 x 128, 128 x 64, 64 x 64 and 32 x 64 (with the best number of pieces), dx of rows x dim from hidden:
+//   bf16  4096 x 4096 from 11008   566, 760, 1148, 1325, 1732        fp32  2048 x 2048 from 5632   698, 669, 682, 730, 808
+//         1024 x 4096 from 4096    87, 82, 86, 117, 176                    777 x 1001 from 2731    145, 107, 103, 105, 110
+//         128 x 4096 from 14336    80, 62, 65, 79, 98                      100 x 512 from 1400     70, 27, 19, 15, 12
 ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type type, bool gated)
 {
-    // What a compute unit takes for a step of 128 bytes of each tile, and workgroups that it runs at once
-    struct Shape { int tile; double cost; };
-    const Shape shapes[3] = {{256, type == MC_F32 ? 16.0 : 16.0}, {128, type == MC_F32 ? 4.0 : 4.8}, {64, type == MC_F32 ? 1.05 : 1.8}};
+    struct Shape { int tile, m, n, together; double alone, busy; };
+    static constexpr Shape shapes[2][5] = {{{256, 256, 256, 1, 7.3, 7.3}, {128, 128, 128, 2, 2.05, 1.9}, {96, 128, 64, 2, 1.2, 0.97}, {64, 64, 64, 3, 0.8, 0.53}, {32, 32, 64, 4, 0.5, 0.31}},
+                                           {{256, 256, 256, 1, 1.45, 1.45}, {128, 128, 128, 2, 0.65, 0.55}, {96, 128, 64, 2, 0.5, 0.4}, {64, 64, 64, 3, 0.375, 0.24}, {32, 32, 64, 4, 0.34, 0.16}}};
     const int64_t size = type == MC_F32 ? 4 : 2, steps = (k * size + 127) / 128;
     ProductPlan best = {256, 1};
     double least = 1e30;
-    for (const Shape &s : shapes) {
-        const int64_t tiles = (m + s.tile - 1) / s.tile * ((n * (gated ? 2 : 1) + s.tile - 1) / s.tile) * batch;
+    for (const Shape &s : shapes[type != MC_F32]) {
+        const int64_t tiles = (m + s.m - 1) / s.m * ((n * (gated ? 2 : 1) + s.n - 1) / s.n) * batch;
         for (int splits = 1; splits <= (gated ? 1 : 16); ++splits) {
-            if (splits > 1 && (steps / splits < 8 || tiles * splits > 4096)) break;
-            const double rounds = (double)((tiles * splits + 255) / 256);
-            double cost = rounds * s.cost * ((double)(steps + splits - 1) / splits + 3);
-            if (splits > 1) cost += 12 + (splits + 1) * (double)(m * n * batch) * 4 / 4e5; // (the join: a launch, and its bytes)
-            if (cost < least) least = cost, best = {s.tile, splits};
+            if (splits > 1 && (steps / splits < 4 || tiles * splits > 4096)) break;
+            const int64_t each = (tiles * splits + COMPUTE_UNITS - 1) / COMPUTE_UNITS, rounds = (each + s.together - 1) / s.together;
+            const double alone = rounds * s.alone, busy = each * s.busy;
+            double us = (alone > busy ? alone : busy) * ((double)(steps + splits - 1) / splits) + 3;
+            if (splits > 1) us += 6 + (splits + 1) * (double)(m * n * batch) * 4 / 3.5e6;
+            if (us < least) least = us, best = {s.tile, splits};
         }
     }
     return best;

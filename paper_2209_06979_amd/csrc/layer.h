@@ -121,6 +121,13 @@ struct PadRowsArgs { // rows of `width` elements into rows of `padded`, zeros be
     int count, width, padded;
 };
 constexpr int FEW_ROWS = 64;
+// Up to 64 rows go to the kernel that cuts k among waves and copies nothing where the tiles of 64 x 64 would be fewer than compute units, or weights would have to be copied
+// for them.  That kernel and the tiles, bf16, us: 16 rows of 4096 to 4096 18.3, 27.8, 64 rows 30.8, 28.6; 16 rows of 1024 to 2816 5.9, 9.2; fp16 1 row of 4096 to 14336 49.5, 47.8,
+// 16 rows 57.8, 47.6, 48 rows 85.3, 52.5; bf16 1 row of 4096 to 11008 35.4, 37.2.
+inline bool few_rows_best(int64_t rows, int hidden, bool copies)
+{
+    return rows <= FEW_ROWS && (copies || (rows <= 32 && hidden <= 32 * 256) || (rows <= 4 && hidden <= 32 * 384));
+}
 hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s);
 // Shapes of a product's tiles, and pieces along k
 struct ProductPlan { int tile, splits; };

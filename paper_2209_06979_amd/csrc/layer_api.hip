@@ -101,12 +101,12 @@ struct FfnPlan { bool few, pad_x, pad_gate, pad_up; size_t x, gate, up, bytes; }
 FfnPlan ffn_plan(const mc_gated_ffn_args *f)
 {
     FfnPlan p = {};
-    p.few = f->rows <= FEW_ROWS;
-    if (p.few) return p;
     const size_t line = (size_t)pieces_up(f->dim, f->type) * size_of(f->type);
     p.pad_x = !in_pieces(f->x_dev, f->x_stride, f->rows, f->dim, f->type);
     p.pad_gate = !in_pieces(f->gate_dev, f->gate_stride, f->hidden, f->dim, f->type);
     p.pad_up = !in_pieces(f->up_dev, f->up_stride, f->hidden, f->dim, f->type);
+    p.few = few_rows_best(f->rows, f->hidden, p.pad_gate || p.pad_up);
+    if (p.few) return p;
     p.gate = p.pad_x ? rounded(f->rows * line) : 0;
     p.up = p.gate + (p.pad_gate ? rounded(f->hidden * line) : 0);
     p.bytes = p.up + (p.pad_up ? rounded(f->hidden * line) : 0);
