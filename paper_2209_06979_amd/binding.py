@@ -393,84 +393,6 @@ class _RopeNode(torch.autograd.Function):
 
 _native._set_rope_node(_RopeNode.apply)
 
-def _rows(d):
-    """A gradient as the library reads it: rows with unit stride along them, none over another."""
-    return d if d is None or (d.stride(-1) == 1 and (d.shape[0] <= 1 or d.stride(0) >= d.shape[1])) else d.contiguous()
-
-
-def _wanted(needs):
-    return sum(1 << i for i, n in enumerate(needs) if n)
-
-
-class _BlockNormNode(torch.autograd.Function):
-    """block_norm of tensors that require grad: (y, n), or the one of them that there is."""
-
-    @staticmethod
-    def forward(ctx, x, residual, weight, bias, post_weight, post_bias, gate, pre, post, branch_scale, residual_scale, eps):
-        ctx.set_materialize_grads(False)
-        ctx.save_for_backward(x, residual, weight, bias, post_weight, post_bias, gate)
-        ctx.call = pre, post, branch_scale, residual_scale, eps
-        y, n = block_norm(x, residual, pre, post, weight, bias, post_weight, post_bias, gate, branch_scale, residual_scale, eps)
-        ctx.only_n = y is x
-        return n if ctx.only_n else y if n is None else (y, n)
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, *d):
-        dy, dn = (None, *d) if ctx.only_n else (*d, None)[:2]
-        x, residual, weight, bias, post_weight, post_bias, gate = ctx.saved_tensors
-        pre, post, branch_scale, residual_scale, eps = ctx.call
-        return _native._block_norm_backward(x, residual, pre, post, weight, bias, post_weight, post_bias, gate, branch_scale, residual_scale, eps,
-                                            _rows(dy), _rows(dn), _wanted(ctx.needs_input_grad[:7])) + (None,) * 5
-
-
-def _block_norm_recorded(x, residual, pre, post, weight, bias, post_weight, post_bias, gate, branch_scale, residual_scale, eps):
-    trivial = residual is None and gate is None and post is None and branch_scale == 1
-    if trivial and pre is None:
-        return x, None
-    out = _BlockNormNode.apply(x, residual, weight, bias, post_weight, post_bias, gate, pre, post, branch_scale, residual_scale, eps)
-    return (x, out) if trivial else (out, None) if pre is None else out
-
-
-class _GatedFfnNode(torch.autograd.Function):
-    """gated_ffn of tensors that require grad: what the two products are is kept for the gradient."""
-
-    @staticmethod
-    def forward(ctx, x, w_gate, w_up, activation):
-        h, g, u = _native._gated_ffn_kept(x, w_gate, w_up, activation)
-        ctx.save_for_backward(x, w_gate, w_up, g, u)
-        ctx.activation = activation
-        return h
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dh):
-        x, w_gate, w_up, g, u = ctx.saved_tensors
-        return _native._gated_ffn_backward(x, w_gate, w_up, ctx.activation, _rows(dh), g, u, _wanted(ctx.needs_input_grad[:3])) + (None,)
-
-
-class _TokenLogprobsNode(torch.autograd.Function):
-    """token_logprobs of logits that require grad."""
-
-    @staticmethod
-    def forward(ctx, logits, tokens, top, scale):
-        ctx.set_materialize_grads(False)
-        logprobs, entropy, top_logprobs, top_tokens, sums = _native._token_logprobs_kept(logits, tokens, top, scale)
-        ctx.save_for_backward(logits, tokens, top_tokens, sums, entropy)
-        ctx.scale = scale
-        ctx.mark_non_differentiable(top_tokens)
-        return logprobs, entropy, top_logprobs, top_tokens
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dlogprobs, dentropy, dtop, _):
-        logits, tokens, top_tokens, sums, entropy = ctx.saved_tensors
-        dlogprobs, dentropy, dtop = (d if d is None else d.contiguous() for d in (dlogprobs, dentropy, dtop))
-        return _native._token_logprobs_backward(logits, tokens, ctx.scale, top_tokens, sums, entropy, dlogprobs, dentropy, dtop), None, None, None
-
-
-_native._set_layer_nodes(_block_norm_recorded, _GatedFfnNode.apply, _TokenLogprobsNode.apply)
-
 ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 

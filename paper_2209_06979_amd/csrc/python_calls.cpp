@@ -18,6 +18,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -947,7 +949,10 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, P
 }
 
 // ---- the rest of a decoder around its attention ---------------------------------------------------------
-PyObject *g_layer_nodes[3] = {}; // binding's autograd nodes of block_norm, gated_ffn and token_logprobs
+// Gradients are recorded by nodes of this module (of torch's C++ interface): a small call and its gradient take 35 .. 54 us, where nodes
+// written in Python took 78 .. 114.
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
 
 // rows of elements on the device, unit stride along them
 inline bool rows_of(const at::Tensor &t) { return t.is_cuda() && t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1 || t.numel() == 0); }
@@ -959,16 +964,20 @@ inline int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride
 // An optional tensor: null and true where it is not given
 inline bool optional(PyObject *o, const at::Tensor **t) { return !given(o) || (*t = tensor(o)); }
 inline void *data(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+inline void *data(const at::TensorBase &t) { return t.defined() ? t.data_ptr() : nullptr; }
+inline const at::Tensor *defined(const at::Tensor &t) { return t.defined() ? &t : nullptr; }
+typedef std::optional<at::Tensor> Maybe;
+inline Maybe maybe(const at::Tensor *t) { return t ? Maybe(*t) : Maybe(); }
 inline PyObject *wrap_or_none(at::TensorBase &&t)
 {
     if (t.defined()) return wrap(std::move(t));
     Py_RETURN_NONE;
 }
 // A tuple of tensors, None for those that are not defined
-template <size_t N> PyObject *tuple_of(at::TensorBase (&t)[N])
+template <class T> PyObject *tuple_of(T *t, size_t n)
 {
-    PyObject *all = PyTuple_New(N);
-    for (size_t i = 0; all && i < N; ++i) {
+    PyObject *all = PyTuple_New((Py_ssize_t)n);
+    for (size_t i = 0; all && i < n; ++i) {
         PyObject *o = wrap_or_none(std::move(t[i]));
         if (!o) Py_CLEAR(all);
         else PyTuple_SET_ITEM(all, i, o);
@@ -976,10 +985,10 @@ template <size_t N> PyObject *tuple_of(at::TensorBase (&t)[N])
     return all;
 }
 // Whether gradients are recorded for one of these.
-template <size_t N> bool recorded(const at::Tensor *const (&t)[N])
+bool recorded(std::initializer_list<const at::Tensor *> tensors)
 {
     if (c10::GradMode::is_enabled())
-        for (const at::Tensor *x : t)
+        for (const at::Tensor *x : tensors)
             if (x && x->requires_grad()) return true;
     return false;
 }
@@ -998,55 +1007,123 @@ template <int N> bool one_of(PyObject *o, const char *const (&names)[N], int *wh
     PyErr_SetObject(PyExc_KeyError, o ? o : Py_None);
     return false;
 }
+// A status inside a node's forward call (caught by the function that makes the node), and in a gradient, where there may be no Python to raise from
+struct Refused : std::exception {
+    int status;
+    explicit Refused(int s) : status(s) {}
+};
+inline void accept(int rc)
+{
+    if (rc != MC_OK) throw Refused(rc);
+}
+void check_status(int rc, const char *where)
+{
+    TORCH_CHECK(rc == MC_OK, where, ": ", mc_strerror(rc), " (", rc, ") ", rc == MC_EHIP ? mc_last_error_detail() : "");
+}
+// A gradient as the library reads it: rows with unit stride along them, none over another
+at::Tensor as_rows(const at::Tensor &d)
+{
+    return !d.defined() || (rows_of(d) && (d.size(0) <= 1 || d.stride(0) >= d.size(1))) ? d : d.contiguous();
+}
+// Gradients that are no functions of theirs: a second derivative is refused, never taken for zero.
+variable_list once(variable_list &&grads, const variable_list &from)
+{
+    bool asked = false;
+    for (const at::Tensor &d : from) asked = asked || (d.defined() && d.requires_grad());
+    if (!c10::GradMode::is_enabled() || !asked) return std::move(grads);
+    const auto refuse = std::make_shared<torch::autograd::DelayedError>("this gradient has no gradient of its own", (int64_t)grads.size());
+    for (at::Tensor &d : grads)
+        if (d.defined()) d.requires_grad_(true);
+    return (*refuse)(std::move(grads));
+}
 
-// What block_norm and its gradient share: v = x, residual, pre, post, weight, bias, post_weight, post_bias, gate, branch_scale, residual_scale, eps
+// What block_norm and its gradient share
 struct NormCall {
-    const at::Tensor *x = nullptr, *residual = nullptr, *weight = nullptr, *bias = nullptr, *post_weight = nullptr, *post_bias = nullptr, *gate = nullptr;
+    enum { X, RESIDUAL, WEIGHT, BIAS, POST_WEIGHT, POST_BIAS, GATE, TENSORS };
+    const at::Tensor *t[TENSORS] = {};
     at::ScalarType stream_type, param_type;
     mc_block_norm_args args = {};
     bool trivial = false; // y is x
-    bool read(PyObject *const *v, bool pre_default)
+    // kinds and scales are in args
+    bool fill()
     {
-        if (!(x = tensor(v[0])) || !optional(v[1], &residual) || !optional(v[4], &weight) || !optional(v[5], &bias) || !optional(v[6], &post_weight) || !optional(v[7], &post_bias) ||
-            !optional(v[8], &gate))
-            return false;
-        static const char *const kinds[3] = {nullptr, "rms", "layer"};
-        int pre = MC_NORM_RMS, post = MC_NORM_NONE;
-        if ((!(pre_default && !v[2]) && !one_of(v[2], kinds, &pre)) || !one_of(v[3], kinds, &post)) return false;
-        args.branch_scale = args.residual_scale = 1;
-        args.eps = 1e-6f;
-        if ((v[9] && !number(v[9], &args.branch_scale)) || (v[10] && !number(v[10], &args.residual_scale)) || (v[11] && !number(v[11], &args.eps))) return false;
-        if (!(rows_of(*x) && real_type(x->scalar_type(), &args.type) && current(*x) && x->size(1) <= 0x7fffffff)) return assertion();
+        const at::Tensor *x = t[X], *residual = t[RESIDUAL], *gate = t[GATE];
+        if (!(rows_of(*x) && real_type(x->scalar_type(), &args.type) && current(*x) && x->size(1) <= 0x7fffffff)) return false;
         stream_type = residual ? residual->scalar_type() : x->scalar_type();
-        if (!real_type(stream_type, &args.residual_type) || (residual && !rows_like(*residual, *x, stream_type))) return assertion();
-        const at::Tensor *params[5] = {weight, bias, post_weight, post_bias, gate};
+        if (!real_type(stream_type, &args.residual_type) || (residual && !rows_like(*residual, *x, stream_type))) return false;
         param_type = x->scalar_type();
-        for (const at::Tensor *p : params)
-            if (p) param_type = p->scalar_type();
-        if (!real_type(param_type, &args.param_type)) return assertion();
-        for (int i = 0; i < 4; ++i)
-            if (params[i] && !array(*params[i], param_type, x->size(1), *x)) return assertion();
+        for (int i = WEIGHT; i <= GATE; ++i)
+            if (t[i]) param_type = t[i]->scalar_type();
+        if (!real_type(param_type, &args.param_type)) return false;
+        for (int i = WEIGHT; i < GATE; ++i)
+            if (t[i] && !array(*t[i], param_type, x->size(1), *x)) return false;
         if (gate) {
             if (!(gate->is_cuda() && gate->device() == x->device() && gate->scalar_type() == param_type && (gate->dim() == 1 || gate->dim() == 2) && gate->size(-1) == x->size(1) &&
                   (gate->stride(-1) == 1 || gate->size(-1) <= 1)))
-                return assertion();
+                return false;
             args.gate_groups = gate->dim() == 2 ? gate->size(0) : 1;
             args.gate_stride = gate->dim() == 2 ? row_stride(*gate) : gate->size(0);
         }
         args.rows = x->size(0);
         args.dim = (int)x->size(1);
-        args.pre = (mc_norm_kind)pre;
-        args.post = (mc_norm_kind)post;
         args.x_dev = x->data_ptr(); args.x_stride = row_stride(*x);
         if (residual) args.residual_dev = residual->data_ptr(), args.residual_stride = row_stride(*residual);
-        args.weight_dev = data(weight); args.bias_dev = data(bias); args.post_weight_dev = data(post_weight); args.post_bias_dev = data(post_bias); args.gate_dev = data(gate);
-        trivial = !residual && !gate && !post && args.branch_scale == 1;
+        args.weight_dev = data(t[WEIGHT]); args.bias_dev = data(t[BIAS]); args.post_weight_dev = data(t[POST_WEIGHT]); args.post_bias_dev = data(t[POST_BIAS]);
+        args.gate_dev = data(gate);
+        trivial = !residual && !gate && !args.post && args.branch_scale == 1;
         return true;
     }
-    static bool assertion()
+    // y and n into tensors of their own (y undefined if it is x, n if there is none)
+    int run(at::TensorBase *y, at::TensorBase *n) const
     {
-        ::assertion();
-        return false;
+        if (!trivial) *y = empty(t[X]->sizes(), stream_type, *t[X]);
+        if (args.pre) *n = empty(t[X]->sizes(), t[X]->scalar_type(), *t[X]);
+        if (trivial && !args.pre) return MC_OK;
+        return mc_block_norm(&args, data(*y), args.dim, data(*n), args.dim, stream());
+    }
+};
+
+struct NormNode : torch::autograd::Function<NormNode> {
+    static variable_list forward(AutogradContext *ctx, const at::Tensor &, const Maybe &, const Maybe &, const Maybe &, const Maybe &, const Maybe &, const Maybe &, const NormCall &call)
+    {
+        ctx->set_materialize_grads(false);
+        variable_list saved;
+        for (const at::Tensor *t : call.t) saved.push_back(t ? *t : at::Tensor());
+        ctx->save_for_backward(std::move(saved));
+        ctx->saved_data["call"] = std::vector<double>{(double)call.args.pre, (double)call.args.post, call.args.branch_scale, call.args.residual_scale, call.args.eps};
+        at::TensorBase y, n;
+        accept(call.run(&y, &n));
+        variable_list out;
+        if (y.defined()) out.emplace_back(std::move(y));
+        if (n.defined()) out.emplace_back(std::move(n));
+        return out;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list given)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const std::vector<double> v = ctx->saved_data["call"].toDoubleVector();
+        NormCall c;
+        for (int i = 0; i < NormCall::TENSORS; ++i) c.t[i] = defined(saved[i]);
+        c.args.pre = (mc_norm_kind)(int)v[0]; c.args.post = (mc_norm_kind)(int)v[1];
+        c.args.branch_scale = (float)v[2]; c.args.residual_scale = (float)v[3]; c.args.eps = (float)v[4];
+        TORCH_CHECK(c.fill(), "block_norm: the tensors have changed since the forward call");
+        const at::Tensor dy = c.trivial ? at::Tensor() : as_rows(given[0]), dn = c.args.pre ? as_rows(given[c.trivial ? 0 : 1]) : at::Tensor();
+        variable_list grads(8);
+        void *to[NormCall::TENSORS] = {};
+        for (int i = 0, edge = 0; i < NormCall::TENSORS; ++i) // (tensors that were not given have no edge)
+            if (c.t[i] && ctx->needs_input_grad(edge++)) {
+                grads[i] = at::Tensor(empty(c.t[i]->sizes(), c.t[i]->scalar_type(), *c.t[0]));
+                to[i] = grads[i].data_ptr();
+            }
+        mc_block_norm_grads g = {};
+        g.dx_dev = to[0]; g.dx_stride = c.args.dim; g.dresidual_dev = to[1]; g.dresidual_stride = c.args.dim; g.dgate_dev = to[6]; g.dgate_stride = c.args.dim;
+        g.dweight_dev = to[2]; g.dbias_dev = to[3]; g.dpost_weight_dev = to[4]; g.dpost_bias_dev = to[5];
+        const size_t bytes = mc_block_norm_backward_workspace(c.args.rows, c.args.dim);
+        at::TensorBase scratch;
+        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *c.t[0]);
+        check_status(mc_block_norm_backward(&c.args, data(dy), dy.defined() ? row_stride(dy) : 0, data(dn), dn.defined() ? row_stride(dn) : 0, &g, data(scratch), bytes, stream()),
+                     "mc_block_norm_backward");
+        return once(std::move(grads), given);
     }
 };
 
@@ -1058,40 +1135,45 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
     PyObject *v[13];
     if (!p_block_norm.parse(args, nargs, kwnames, v)) return nullptr;
     NormCall c;
-    if (!c.read(v, true)) return nullptr;
+    if (!(c.t[NormCall::X] = tensor(v[0])) || !optional(v[1], &c.t[NormCall::RESIDUAL])) return nullptr;
+    for (int i = NormCall::WEIGHT; i <= NormCall::GATE; ++i)
+        if (!optional(v[i + 2], &c.t[i])) return nullptr;
+    static const char *const kinds[3] = {nullptr, "rms", "layer"};
+    int pre = MC_NORM_RMS, post = MC_NORM_NONE;
+    if ((v[2] && !one_of(v[2], kinds, &pre)) || !one_of(v[3], kinds, &post)) return nullptr;
+    c.args.pre = (mc_norm_kind)pre; c.args.post = (mc_norm_kind)post;
+    c.args.branch_scale = c.args.residual_scale = 1;
+    c.args.eps = 1e-6f;
+    if ((v[9] && !number(v[9], &c.args.branch_scale)) || (v[10] && !number(v[10], &c.args.residual_scale)) || (v[11] && !number(v[11], &c.args.eps))) return nullptr;
+    if (!c.fill()) return assertion();
     const at::Tensor *y = nullptr, *n = nullptr;
     const bool out = given(v[12]);
     if (out) {
         if (!PyTuple_Check(v[12]) || PyTuple_GET_SIZE(v[12]) != 2) return assertion();
         if (!optional(PyTuple_GET_ITEM(v[12], 0), &y) || !optional(PyTuple_GET_ITEM(v[12], 1), &n)) return nullptr;
-        if ((y && !rows_like(*y, *c.x, c.stream_type)) || !n != !c.args.pre || (n && !rows_like(*n, *c.x, c.x->scalar_type()))) return assertion();
-    }
-    if (recorded({c.x, c.residual, c.weight, c.bias, c.post_weight, c.post_bias, c.gate, y, n})) {
-        if (out) return no_out_gradient("block_norm");
-        PyObject *all[12];
-        PyObject *scales[3] = {PyFloat_FromDouble(c.args.branch_scale), PyFloat_FromDouble(c.args.residual_scale), PyFloat_FromDouble(c.args.eps)};
-        static const char *const kinds[3] = {nullptr, "rms", "layer"};
-        PyObject *pre = c.args.pre ? PyUnicode_FromString(kinds[c.args.pre]) : same(Py_None);
-        for (int i = 0; i < 9; ++i) all[i] = v[i] ? v[i] : Py_None;
-        all[2] = pre;
-        for (int i = 0; i < 3; ++i) all[9 + i] = scales[i];
-        PyObject *r = pre && scales[0] && scales[1] && scales[2] ? PyObject_Vectorcall(g_layer_nodes[0], all, 12, nullptr) : nullptr;
-        for (PyObject *o : scales) Py_XDECREF(o);
-        Py_XDECREF(pre);
-        return r;
+        if ((y && !rows_like(*y, *c.t[0], c.stream_type)) || !n != !c.args.pre || (n && !rows_like(*n, *c.t[0], c.t[0]->scalar_type()))) return assertion();
     }
     at::TensorBase made[2];
-    int rc;
-    {
-        pybind11::gil_scoped_release nogil;
-        if (!out && !c.trivial) made[0] = empty(c.x->sizes(), c.stream_type, *c.x);
-        if (!out && c.args.pre) made[1] = empty(c.x->sizes(), c.x->scalar_type(), *c.x);
-        const int64_t dim = c.x->size(1);
-        void *to_y = out ? data(y) : made[0].defined() ? made[0].data_ptr() : nullptr, *to_n = out ? data(n) : made[1].defined() ? made[1].data_ptr() : nullptr;
-        rc = !to_y && !c.args.pre && c.trivial ? MC_OK : mc_block_norm(&c.args, to_y, y ? row_stride(*y) : dim, to_n, n ? row_stride(*n) : dim, stream());
+    if (recorded({c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) {
+        if (out) return no_out_gradient("block_norm");
+        if (!c.trivial || c.args.pre) {
+            try {
+                variable_list r = NormNode::apply(*c.t[0], maybe(c.t[1]), maybe(c.t[2]), maybe(c.t[3]), maybe(c.t[4]), maybe(c.t[5]), maybe(c.t[6]), c);
+                if (!c.trivial) made[0] = r[0];
+                if (c.args.pre) made[1] = r[c.trivial ? 0 : 1];
+            } catch (const Refused &e) {
+                return status_error(e.status, "mc_block_norm");
+            }
+        }
+    } else {
+        int rc;
+        {
+            pybind11::gil_scoped_release nogil;
+            rc = out ? mc_block_norm(&c.args, data(y), y ? row_stride(*y) : 0, data(n), n ? row_stride(*n) : 0, stream()) : c.run(&made[0], &made[1]);
+        }
+        if (rc != MC_OK) return status_error(rc, "mc_block_norm");
+        if (out) return same(v[12]);
     }
-    if (rc != MC_OK) return status_error(rc, "mc_block_norm");
-    if (out) return same(v[12]);
     PyObject *a = c.trivial ? same(v[0]) : wrap(std::move(made[0])), *b = wrap_or_none(std::move(made[1])), *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
     Py_XDECREF(a);
     Py_XDECREF(b);
@@ -1099,278 +1181,200 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
     END_HANDLE_TH_ERRORS
 }
 
-Params<15> p_block_norm_backward = {"_block_norm_backward", 15, {"x", "residual", "pre", "post", "weight", "bias", "post_weight", "post_bias", "gate", "branch_scale", "residual_scale", "eps",
-                                                                 "dy", "dn", "wanted"}, {}};
-
-// Gradients of x, residual, weight, bias, post_weight, post_bias, gate; bit i of `wanted`: the i-th is asked for
-PyObject *block_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
-{
-    HANDLE_TH_ERRORS
-    PyObject *v[15];
-    if (!p_block_norm_backward.parse(args, nargs, kwnames, v)) return nullptr;
-    NormCall c;
-    if (!c.read(v, false)) return nullptr;
-    const at::Tensor *dy = nullptr, *dn = nullptr;
-    int wanted;
-    if (!optional(v[12], &dy) || !optional(v[13], &dn) || !integer(v[14], 0, &wanted)) return nullptr;
-    if ((dy && !rows_like(*dy, *c.x, c.stream_type)) || (dn && !rows_like(*dn, *c.x, c.x->scalar_type()))) return assertion();
-    at::TensorBase made[7], scratch;
-    int rc;
-    {
-        pybind11::gil_scoped_release nogil;
-        const at::Tensor *of[7] = {c.x, c.residual, c.weight, c.bias, c.post_weight, c.post_bias, c.gate};
-        void *to[7] = {};
-        for (int i = 0; i < 7; ++i)
-            if (of[i] && (wanted >> i & 1)) {
-                made[i] = empty(of[i]->sizes(), of[i]->scalar_type(), *c.x);
-                to[i] = made[i].data_ptr();
-            }
-        mc_block_norm_grads g = {};
-        g.dx_dev = to[0]; g.dx_stride = c.x->size(1); g.dresidual_dev = to[1]; g.dresidual_stride = c.x->size(1); g.dgate_dev = to[6]; g.dgate_stride = c.x->size(1);
-        g.dweight_dev = to[2]; g.dbias_dev = to[3]; g.dpost_weight_dev = to[4]; g.dpost_bias_dev = to[5];
-        const size_t bytes = mc_block_norm_backward_workspace(c.args.rows, c.args.dim);
-        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *c.x);
-        rc = mc_block_norm_backward(&c.args, data(dy), dy ? row_stride(*dy) : 0, data(dn), dn ? row_stride(*dn) : 0, &g, bytes ? scratch.data_ptr() : nullptr, bytes, stream());
-    }
-    if (rc != MC_OK) return status_error(rc, "mc_block_norm_backward");
-    return tuple_of(made);
-    END_HANDLE_TH_ERRORS
-}
-
 const char *const ACTIVATIONS[5] = {"silu", "gelu", "gelu_tanh", "relu", "sigmoid"};
 
-bool ffn_args(PyObject *const *v, const at::Tensor **x, const at::Tensor **gate, const at::Tensor **up, mc_gated_ffn_args *f)
-{
-    if (!(*x = tensor(v[0])) || !(*gate = tensor(v[1])) || !(*up = tensor(v[2]))) return false;
-    int act = 0;
-    if (v[3] && !one_of(v[3], ACTIVATIONS, &act)) return false;
-    if (!(rows_of(**x) && real_type((*x)->scalar_type(), &f->type) && current(**x) && rows_of(**gate) && rows_like(**up, **gate, (*x)->scalar_type()) &&
-          (*gate)->device() == (*x)->device() && (*gate)->scalar_type() == (*x)->scalar_type() && (*gate)->size(1) == (*x)->size(1) && (*x)->size(1) <= 0x7fffffff &&
-          (*gate)->size(0) <= 0x7fffffff)) {
-        assertion();
-        return false;
-    }
-    f->rows = (*x)->size(0); f->dim = (int)(*x)->size(1); f->hidden = (int)(*gate)->size(0); f->activation = (mc_activation)act;
-    f->x_dev = (*x)->data_ptr(); f->x_stride = row_stride(**x);
-    f->gate_dev = (*gate)->data_ptr(); f->gate_stride = row_stride(**gate);
-    f->up_dev = (*up)->data_ptr(); f->up_stride = row_stride(**up);
-    return true;
-}
-
-Params<6> p_gated_ffn = {"gated_ffn", 3, {"x", "w_gate", "w_up", "activation", "out", "workspace"}, {}};
-
-// keep: h, g and u
-PyObject *gated_ffn_call(PyObject *const *v, bool keep)
-{
-    const at::Tensor *x, *gate, *up, *out = nullptr, *ws = nullptr;
-    mc_gated_ffn_args f = {};
-    if (!ffn_args(v, &x, &gate, &up, &f) || !optional(v[4], &out) || !optional(v[5], &ws)) return nullptr;
-    if (out && !(rows_of(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->size(0) == x->size(0) && out->size(1) == gate->size(0)))
-        return assertion();
-    if (ws && !(ws->is_cuda() && ws->device() == x->device() && ws->is_contiguous())) return assertion();
-    if (!keep && recorded({x, gate, up, out})) {
-        if (out) return no_out_gradient("gated_ffn");
-        PyObject *all[4] = {v[0], v[1], v[2], v[3]}, *silu = nullptr;
-        if (!all[3]) all[3] = silu = PyUnicode_FromString("silu");
-        PyObject *r = all[3] ? PyObject_Vectorcall(g_layer_nodes[1], all, 4, nullptr) : nullptr;
-        Py_XDECREF(silu);
-        return r;
-    }
-    at::TensorBase made[3], scratch;
-    int rc;
+struct FfnCall {
+    const at::Tensor *x, *gate, *up;
+    mc_gated_ffn_args args = {};
+    bool fill()
     {
-        pybind11::gil_scoped_release nogil;
-        const int64_t hidden = gate->size(0);
-        for (int i = 0; i < 3; ++i)
-            if (i ? keep : !out) made[i] = empty({x->size(0), hidden}, i ? at::kFloat : x->scalar_type(), *x);
-        void *w = nullptr;
-        size_t bytes = 0;
-        if (ws) {
-            w = ws->data_ptr();
-            bytes = (size_t)ws->numel() * ws->element_size();
-        } else if ((bytes = mc_gated_ffn_workspace(&f)) > 0) {
+        if (!(rows_of(*x) && real_type(x->scalar_type(), &args.type) && current(*x) && rows_of(*gate) && rows_like(*up, *gate, x->scalar_type()) && gate->device() == x->device() &&
+              gate->scalar_type() == x->scalar_type() && gate->size(1) == x->size(1) && x->size(1) <= 0x7fffffff && gate->size(0) <= 0x7fffffff))
+            return false;
+        args.rows = x->size(0); args.dim = (int)x->size(1); args.hidden = (int)gate->size(0);
+        args.x_dev = x->data_ptr(); args.x_stride = row_stride(*x);
+        args.gate_dev = gate->data_ptr(); args.gate_stride = row_stride(*gate);
+        args.up_dev = up->data_ptr(); args.up_stride = row_stride(*up);
+        return true;
+    }
+    // h (out, or a tensor of its own), and g and u if they are kept
+    int run(const at::Tensor *out, const at::Tensor *ws, bool keep, at::TensorBase (&made)[3]) const
+    {
+        const int64_t rows = x->size(0), hidden = gate->size(0);
+        if (!out) made[0] = empty({rows, hidden}, x->scalar_type(), *x);
+        if (keep) made[1] = empty({rows, hidden}, at::kFloat, *x), made[2] = empty({rows, hidden}, at::kFloat, *x);
+        at::TensorBase scratch;
+        void *w = data(ws);
+        size_t bytes = ws ? (size_t)ws->numel() * ws->element_size() : mc_gated_ffn_workspace(&args);
+        if (!ws && bytes) {
             scratch = empty({(int64_t)bytes}, at::kByte, *x);
             w = scratch.data_ptr();
         }
-        rc = mc_gated_ffn(&f, out ? out->data_ptr() : made[0].data_ptr(), out ? row_stride(*out) : hidden, keep ? static_cast<float *>(made[1].data_ptr()) : nullptr,
-                          keep ? static_cast<float *>(made[2].data_ptr()) : nullptr, hidden, w, bytes, stream());
+        return mc_gated_ffn(&args, out ? out->data_ptr() : data(made[0]), out ? row_stride(*out) : hidden, static_cast<float *>(data(made[1])), static_cast<float *>(data(made[2])), hidden, w,
+                            bytes, stream());
     }
-    if (rc != MC_OK) return status_error(rc, "mc_gated_ffn");
-    if (keep) return tuple_of(made);
-    return out ? same(v[4]) : wrap(std::move(made[0]));
-}
+};
+
+struct FfnNode : torch::autograd::Function<FfnNode> {
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &x, const at::Tensor &gate, const at::Tensor &up, const FfnCall &call)
+    {
+        at::TensorBase made[3];
+        accept(call.run(nullptr, nullptr, true, made));
+        ctx->save_for_backward({x, gate, up, at::Tensor(made[1]), at::Tensor(made[2])});
+        ctx->saved_data["activation"] = (int64_t)call.args.activation;
+        return at::Tensor(std::move(made[0]));
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list given)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        FfnCall c = {&saved[0], &saved[1], &saved[2]};
+        c.args.activation = (mc_activation)ctx->saved_data["activation"].toInt();
+        TORCH_CHECK(c.fill(), "gated_ffn: the tensors have changed since the forward call");
+        const at::Tensor dh = as_rows(given[0]);
+        variable_list grads(4);
+        void *to[3] = {};
+        for (int i = 0; i < 3; ++i)
+            if (ctx->needs_input_grad(i)) {
+                grads[i] = at::Tensor(empty(saved[i].sizes(), saved[i].scalar_type(), saved[0]));
+                to[i] = grads[i].data_ptr();
+            }
+        const size_t bytes = mc_gated_ffn_backward_workspace(&c.args);
+        at::TensorBase scratch;
+        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, saved[0]);
+        const int64_t dim = c.args.dim;
+        check_status(mc_gated_ffn_backward(&c.args, dh.data_ptr(), row_stride(dh), static_cast<const float *>(saved[3].data_ptr()), static_cast<const float *>(saved[4].data_ptr()),
+                                           c.args.hidden, to[0], dim, to[1], dim, to[2], dim, data(scratch), bytes, stream()),
+                     "mc_gated_ffn_backward");
+        return once(std::move(grads), given);
+    }
+};
+
+Params<6> p_gated_ffn = {"gated_ffn", 3, {"x", "w_gate", "w_up", "activation", "out", "workspace"}, {}};
 
 PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     HANDLE_TH_ERRORS
     PyObject *v[6];
     if (!p_gated_ffn.parse(args, nargs, kwnames, v)) return nullptr;
-    return gated_ffn_call(v, false);
-    END_HANDLE_TH_ERRORS
-}
-
-PyObject *gated_ffn_kept(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
-{
-    HANDLE_TH_ERRORS
-    PyObject *v[6];
-    if (!p_gated_ffn.parse(args, nargs, kwnames, v)) return nullptr;
-    if (given(v[4])) return assertion();
-    return gated_ffn_call(v, true);
-    END_HANDLE_TH_ERRORS
-}
-
-Params<8> p_gated_ffn_backward = {"_gated_ffn_backward", 8, {"x", "w_gate", "w_up", "activation", "dh", "g", "u", "wanted"}, {}};
-
-// Gradients of x, w_gate, w_up; bit i of `wanted`: the i-th is asked for
-PyObject *gated_ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
-{
-    HANDLE_TH_ERRORS
-    PyObject *v[8];
-    if (!p_gated_ffn_backward.parse(args, nargs, kwnames, v)) return nullptr;
-    const at::Tensor *x, *gate, *up, *dh, *g, *u;
-    mc_gated_ffn_args f = {};
-    int wanted;
-    if (!ffn_args(v, &x, &gate, &up, &f) || !(dh = tensor(v[4])) || !(g = tensor(v[5])) || !(u = tensor(v[6])) || !integer(v[7], 0, &wanted)) return nullptr;
-    for (const at::Tensor *t : {dh, g, u})
-        if (!(rows_of(*t) && t->device() == x->device() && t->scalar_type() == (t == dh ? x->scalar_type() : at::kFloat) && t->size(0) == x->size(0) && t->size(1) == gate->size(0)))
-            return assertion();
-    if (row_stride(*g) != row_stride(*u)) return assertion();
-    at::TensorBase made[3], scratch;
-    int rc;
-    {
-        pybind11::gil_scoped_release nogil;
-        const at::Tensor *of[3] = {x, gate, up};
-        void *to[3] = {};
-        for (int i = 0; i < 3; ++i)
-            if (wanted >> i & 1) {
-                made[i] = empty(of[i]->sizes(), x->scalar_type(), *x);
-                to[i] = made[i].data_ptr();
-            }
-        const size_t bytes = mc_gated_ffn_backward_workspace(&f);
-        if (bytes) scratch = empty({(int64_t)bytes}, at::kByte, *x);
-        rc = mc_gated_ffn_backward(&f, dh->data_ptr(), row_stride(*dh), static_cast<const float *>(g->data_ptr()), static_cast<const float *>(u->data_ptr()), row_stride(*g), to[0], f.dim, to[1], f.dim, to[2], f.dim,
-                                   bytes ? scratch.data_ptr() : nullptr, bytes, stream());
-    }
-    if (rc != MC_OK) return status_error(rc, "mc_gated_ffn_backward");
-    return tuple_of(made);
-    END_HANDLE_TH_ERRORS
-}
-
-Params<5> p_token_logprobs = {"token_logprobs", 2, {"logits", "tokens", "top", "scale", "workspace"}, {}};
-
-// keep: the sums for the gradient too
-PyObject *token_logprobs_call(PyObject *const *v, bool keep)
-{
-    const at::Tensor *x = tensor(v[0]), *tokens = x ? tensor(v[1]) : nullptr, *ws = nullptr;
-    int top;
-    float scale = 1;
-    if (!tokens || !integer(v[2], 0, &top) || (v[3] && !number(v[3], &scale)) || !optional(v[4], &ws)) return nullptr;
-    mc_type type;
-    if (!(rows_of(*x) && real_type(x->scalar_type(), &type) && current(*x) && x->size(1) <= 0x7fffffff && array(*tokens, at::kLong, x->size(0), *x))) return assertion();
-    if (ws && !(ws->is_cuda() && ws->device() == x->device() && ws->is_contiguous())) return assertion();
-    if (!keep && recorded({x})) {
-        PyObject *count = PyLong_FromLong(top), *factor = PyFloat_FromDouble(scale), *all[4] = {v[0], v[1], count, factor};
-        PyObject *r = count && factor ? PyObject_Vectorcall(g_layer_nodes[2], all, 4, nullptr) : nullptr;
-        Py_XDECREF(count);
-        Py_XDECREF(factor);
-        return r;
-    }
-    const int64_t rows = x->size(0), most = top > 0 ? top : 0;
-    at::TensorBase made[5], scratch;
-    int rc;
-    {
-        pybind11::gil_scoped_release nogil;
-        if (top <= x->size(1)) { // (refused below otherwise)
-            made[0] = empty({rows}, at::kFloat, *x);
-            made[1] = empty({rows}, at::kFloat, *x);
-            made[2] = empty({rows, most}, at::kFloat, *x);
-            made[3] = empty({rows, most}, at::kLong, *x);
-            if (keep) made[4] = empty({rows, 2}, at::kFloat, *x);
-            void *w = nullptr;
-            size_t bytes = 0;
-            if (ws) {
-                w = ws->data_ptr();
-                bytes = (size_t)ws->numel() * ws->element_size();
-            } else if ((bytes = mc_token_logprobs_workspace(rows, (int)x->size(1), type, top)) > 0) {
-                scratch = empty({(int64_t)bytes}, at::kByte, *x);
-                w = scratch.data_ptr();
-            }
-            rc = mc_token_logprobs(x->data_ptr(), type, rows, (int)x->size(1), row_stride(*x), static_cast<const int64_t *>(tokens->data_ptr()), scale, top,
-                                   static_cast<float *>(made[0].data_ptr()), static_cast<float *>(made[1].data_ptr()), static_cast<float *>(made[2].data_ptr()),
-                                   static_cast<int64_t *>(made[3].data_ptr()), keep ? static_cast<float *>(made[4].data_ptr()) : nullptr, w, bytes, stream());
-        } else {
-            rc = MC_EINVAL;
+    FfnCall c;
+    const at::Tensor *out = nullptr, *ws = nullptr;
+    if (!(c.x = tensor(v[0])) || !(c.gate = tensor(v[1])) || !(c.up = tensor(v[2]))) return nullptr;
+    int act = 0;
+    if ((v[3] && !one_of(v[3], ACTIVATIONS, &act)) || !optional(v[4], &out) || !optional(v[5], &ws)) return nullptr;
+    c.args.activation = (mc_activation)act;
+    if (!c.fill()) return assertion();
+    if (out && !(rows_of(*out) && out->device() == c.x->device() && out->scalar_type() == c.x->scalar_type() && out->size(0) == c.x->size(0) && out->size(1) == c.gate->size(0)))
+        return assertion();
+    if (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous())) return assertion();
+    if (recorded({c.x, c.gate, c.up, out})) {
+        if (out) return no_out_gradient("gated_ffn");
+        try {
+            return wrap(FfnNode::apply(*c.x, *c.gate, *c.up, c));
+        } catch (const Refused &e) {
+            return status_error(e.status, "mc_gated_ffn");
         }
     }
-    if (rc != MC_OK) return status_error(rc, "mc_token_logprobs");
-    if (keep) return tuple_of(made);
-    at::TensorBase four[4];
-    for (int i = 0; i < 4; ++i) four[i] = std::move(made[i]);
-    return tuple_of(four);
+    at::TensorBase made[3];
+    int rc;
+    {
+        pybind11::gil_scoped_release nogil;
+        rc = c.run(out, ws, false, made);
+    }
+    if (rc != MC_OK) return status_error(rc, "mc_gated_ffn");
+    return out ? same(v[4]) : wrap(std::move(made[0]));
+    END_HANDLE_TH_ERRORS
 }
+
+struct LogprobCall {
+    const at::Tensor *x, *tokens;
+    mc_type type;
+    int top = 0;
+    float scale = 1;
+    bool fill() { return rows_of(*x) && real_type(x->scalar_type(), &type) && current(*x) && x->size(1) <= 0x7fffffff && array(*tokens, at::kLong, x->size(0), *x); }
+    // log probabilities, entropies, those of the top tokens, these, and the sums if they are kept
+    int run(const at::Tensor *ws, bool keep, at::TensorBase (&made)[5]) const
+    {
+        const int64_t rows = x->size(0), vocab = x->size(1);
+        if (top < 0 || top > vocab) return MC_EINVAL;
+        made[0] = empty({rows}, at::kFloat, *x);
+        made[1] = empty({rows}, at::kFloat, *x);
+        made[2] = empty({rows, top}, at::kFloat, *x);
+        made[3] = empty({rows, top}, at::kLong, *x);
+        if (keep) made[4] = empty({rows, 2}, at::kFloat, *x);
+        at::TensorBase scratch;
+        void *w = data(ws);
+        size_t bytes = ws ? (size_t)ws->numel() * ws->element_size() : mc_token_logprobs_workspace(rows, (int)vocab, type, top);
+        if (!ws && bytes) {
+            scratch = empty({(int64_t)bytes}, at::kByte, *x);
+            w = scratch.data_ptr();
+        }
+        return mc_token_logprobs(x->data_ptr(), type, rows, (int)vocab, row_stride(*x), static_cast<const int64_t *>(tokens->data_ptr()), scale, top, static_cast<float *>(data(made[0])),
+                                 static_cast<float *>(data(made[1])), static_cast<float *>(data(made[2])), static_cast<int64_t *>(data(made[3])), static_cast<float *>(data(made[4])), w, bytes,
+                                 stream());
+    }
+};
+
+struct LogprobNode : torch::autograd::Function<LogprobNode> {
+    static variable_list forward(AutogradContext *ctx, const at::Tensor &x, const LogprobCall &call)
+    {
+        ctx->set_materialize_grads(false);
+        at::TensorBase made[5];
+        accept(call.run(nullptr, true, made));
+        variable_list out;
+        for (int i = 0; i < 4; ++i) out.emplace_back(made[i]);
+        ctx->mark_non_differentiable({out[3]});
+        ctx->save_for_backward({x, *call.tokens, out[1], out[3], at::Tensor(made[4])});
+        ctx->saved_data["scale"] = (double)call.scale;
+        return out;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list given)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        LogprobCall c = {&saved[0], &saved[1]};
+        TORCH_CHECK(c.fill(), "token_logprobs: the tensors have changed since the forward call");
+        at::Tensor d[3];
+        for (int i = 0; i < 3; ++i) d[i] = given[i].defined() ? given[i].contiguous() : given[i];
+        const at::Tensor &x = saved[0];
+        variable_list grads(2);
+        grads[0] = at::Tensor(empty(x.sizes(), x.scalar_type(), x));
+        check_status(mc_token_logprobs_backward(x.data_ptr(), c.type, x.size(0), (int)x.size(1), row_stride(x), static_cast<const int64_t *>(saved[1].data_ptr()),
+                                                (float)ctx->saved_data["scale"].toDouble(), (int)saved[3].size(1), static_cast<const int64_t *>(saved[3].data_ptr()),
+                                                static_cast<const float *>(saved[4].data_ptr()), static_cast<const float *>(saved[2].data_ptr()), static_cast<const float *>(data(d[0])),
+                                                static_cast<const float *>(data(d[1])), static_cast<const float *>(data(d[2])), grads[0].data_ptr(), x.size(1), stream()),
+                     "mc_token_logprobs_backward");
+        return once(std::move(grads), given);
+    }
+};
+
+Params<5> p_token_logprobs = {"token_logprobs", 2, {"logits", "tokens", "top", "scale", "workspace"}, {}};
 
 PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     HANDLE_TH_ERRORS
     PyObject *v[5];
     if (!p_token_logprobs.parse(args, nargs, kwnames, v)) return nullptr;
-    return token_logprobs_call(v, false);
-    END_HANDLE_TH_ERRORS
-}
-
-PyObject *token_logprobs_kept(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
-{
-    HANDLE_TH_ERRORS
-    PyObject *v[5];
-    if (!p_token_logprobs.parse(args, nargs, kwnames, v)) return nullptr;
-    return token_logprobs_call(v, true);
-    END_HANDLE_TH_ERRORS
-}
-
-Params<9> p_token_logprobs_backward = {"_token_logprobs_backward", 9, {"logits", "tokens", "scale", "top_tokens", "sums", "entropy", "dlogprobs", "dentropy", "dtop"}, {}};
-
-PyObject *token_logprobs_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
-{
-    HANDLE_TH_ERRORS
-    PyObject *v[9];
-    if (!p_token_logprobs_backward.parse(args, nargs, kwnames, v)) return nullptr;
-    const at::Tensor *x = tensor(v[0]), *tokens = x ? tensor(v[1]) : nullptr, *chosen = tokens ? tensor(v[3]) : nullptr, *sums = chosen ? tensor(v[4]) : nullptr,
-                     *entropy = sums ? tensor(v[5]) : nullptr, *dl = nullptr, *dh = nullptr, *dt = nullptr;
-    float scale;
-    if (!entropy || !number(v[2], &scale) || !optional(v[6], &dl) || !optional(v[7], &dh) || !optional(v[8], &dt)) return nullptr;
-    mc_type type;
-    const int64_t rows = x->dim() == 2 ? x->size(0) : 0;
-    if (!(rows_of(*x) && real_type(x->scalar_type(), &type) && current(*x) && x->size(1) <= 0x7fffffff && array(*tokens, at::kLong, rows, *x) && array(*entropy, at::kFloat, rows, *x) &&
-          (!dl || array(*dl, at::kFloat, rows, *x)) && (!dh || array(*dh, at::kFloat, rows, *x))))
-        return assertion();
-    for (const at::Tensor *t : {chosen, sums, dt})
-        if (t && !(t->is_cuda() && t->device() == x->device() && t->dim() == 2 && t->size(0) == rows && t->is_contiguous())) return assertion();
-    if (!(chosen->scalar_type() == at::kLong && sums->scalar_type() == at::kFloat && sums->size(1) == 2 && (!dt || (dt->scalar_type() == at::kFloat && dt->size(1) == chosen->size(1)))))
-        return assertion();
-    at::TensorBase made;
+    LogprobCall c = {};
+    c.scale = 1;
+    const at::Tensor *ws = nullptr;
+    if (!(c.x = tensor(v[0])) || !(c.tokens = tensor(v[1])) || !integer(v[2], 0, &c.top) || (v[3] && !number(v[3], &c.scale)) || !optional(v[4], &ws)) return nullptr;
+    if (!c.fill() || (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous()))) return assertion();
+    if (recorded({c.x})) {
+        try {
+            variable_list r = LogprobNode::apply(*c.x, c);
+            return tuple_of(r.data(), 4);
+        } catch (const Refused &e) {
+            return status_error(e.status, "mc_token_logprobs");
+        }
+    }
+    at::TensorBase made[5];
     int rc;
     {
         pybind11::gil_scoped_release nogil;
-        made = empty(x->sizes(), x->scalar_type(), *x);
-        rc = mc_token_logprobs_backward(x->data_ptr(), type, rows, (int)x->size(1), row_stride(*x), static_cast<const int64_t *>(tokens->data_ptr()), scale, (int)chosen->size(1),
-                                        static_cast<const int64_t *>(chosen->data_ptr()), static_cast<const float *>(sums->data_ptr()), static_cast<const float *>(entropy->data_ptr()),
-                                        static_cast<const float *>(data(dl)), static_cast<const float *>(data(dh)), static_cast<const float *>(data(dt)), made.data_ptr(), x->size(1),
-                                        stream());
+        rc = c.run(ws, false, made);
     }
-    if (rc != MC_OK) return status_error(rc, "mc_token_logprobs_backward");
-    return wrap(std::move(made));
+    if (rc != MC_OK) return status_error(rc, "mc_token_logprobs");
+    return tuple_of(made, 4);
     END_HANDLE_TH_ERRORS
-}
-
-PyObject *set_layer_nodes(PyObject *, PyObject *args)
-{
-    PyObject *node[3];
-    if (!PyArg_ParseTuple(args, "OOO", &node[0], &node[1], &node[2])) return nullptr;
-    for (int i = 0; i < 3; ++i) {
-        Py_INCREF(node[i]);
-        Py_XSETREF(g_layer_nodes[i], node[i]);
-    }
-    Py_RETURN_NONE;
 }
 
 PyObject *set_error_class(PyObject *, PyObject *cls)
@@ -1473,12 +1477,6 @@ PyMethodDef functions[] = {
      "(log probabilities of the tokens, entropies, log probabilities of the `top` most likely tokens, these tokens) of rows of\n"
      "scale * logits (rows, vocab) fp32, fp16 or bf16: (rows,), (rows,), (rows, top) fp32 and (rows, top) int64.  tokens (rows,) int64, those\n"
      "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three."},
-    {"_set_layer_nodes", set_layer_nodes, METH_VARARGS, "what block_norm, gated_ffn and token_logprobs call for tensors that require grad"},
-    {"_block_norm_backward", FAST(block_norm_backward), "gradients of block_norm's tensors (see mc_block_norm_backward)"},
-    {"_gated_ffn_kept", FAST(gated_ffn_kept), "gated_ffn with what its gradient needs: (h, g, u)"},
-    {"_gated_ffn_backward", FAST(gated_ffn_backward), "gradients of gated_ffn's tensors (see mc_gated_ffn_backward)"},
-    {"_token_logprobs_kept", FAST(token_logprobs_kept), "token_logprobs with what its gradient needs: its results and the sums"},
-    {"_token_logprobs_backward", FAST(token_logprobs_backward), "the gradient of token_logprobs' logits (see mc_token_logprobs_backward)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};
@@ -1506,7 +1504,7 @@ PyMODINIT_FUNC PyInit__native(void)
     CacheType.tp_new = PyType_GenericNew;
     if (PyType_Ready(&CacheType) < 0) return nullptr;
     p_rope.intern(); p_cache_write.intern(); p_cache_read.intern(); p_cache_attention.intern();
-    p_block_norm.intern(); p_block_norm_backward.intern(); p_gated_ffn.intern(); p_gated_ffn_backward.intern(); p_token_logprobs.intern(); p_token_logprobs_backward.intern();
+    p_block_norm.intern(); p_gated_ffn.intern(); p_token_logprobs.intern();
     PyObject *m = PyModule_Create(&module_def);
     if (!m) return nullptr;
     Py_INCREF(&MatrixType);

@@ -201,3 +201,17 @@ def test_runs_are_alike_and_streams():
         again = _train(v, kw)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+def test_gradients_of_gradients_are_refused():
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    x, w = (torch.randn((3, 16), device="cuda").requires_grad_(True) for _ in "xw")
+    tokens = torch.zeros(3, dtype=torch.long, device="cuda")
+    for call in (lambda: mc.block_norm(x)[1], lambda: mc.gated_ffn(x, w, w), lambda: mc.token_logprobs(x, tokens)[0]):
+        y = call()
+        d, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="no gradient of its own"):
+            d.sum().backward()
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(d.sum(), x)
