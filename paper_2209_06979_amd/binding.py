@@ -67,6 +67,26 @@ class RopeKeys(ctypes.Structure):
     _fields_ = [("positions_dev", c_void_p), ("inv_freq_dev", c_void_p), ("rot", c_int), ("interleaved", c_int), ("magnitude", c_float)]
 
 
+class BlockNormArgs(ctypes.Structure):
+    """mc_block_norm_args: the tensors, kinds and scales of mc_block_norm and its gradient."""
+    _fields_ = [("rows", c_int64), ("dim", c_int), ("type", c_int), ("residual_type", c_int), ("param_type", c_int), ("pre", c_int), ("post", c_int),
+                ("x_dev", c_void_p), ("x_stride", c_int64), ("residual_dev", c_void_p), ("residual_stride", c_int64),
+                ("weight_dev", c_void_p), ("bias_dev", c_void_p), ("post_weight_dev", c_void_p), ("post_bias_dev", c_void_p),
+                ("gate_dev", c_void_p), ("gate_groups", c_int64), ("gate_stride", c_int64), ("branch_scale", c_float), ("residual_scale", c_float), ("eps", c_float)]
+
+
+class BlockNormGrads(ctypes.Structure):
+    """mc_block_norm_grads: where the gradients go."""
+    _fields_ = [("dx_dev", c_void_p), ("dx_stride", c_int64), ("dresidual_dev", c_void_p), ("dresidual_stride", c_int64), ("dgate_dev", c_void_p), ("dgate_stride", c_int64),
+                ("dweight_dev", c_void_p), ("dbias_dev", c_void_p), ("dpost_weight_dev", c_void_p), ("dpost_bias_dev", c_void_p)]
+
+
+class GatedFfnArgs(ctypes.Structure):
+    """mc_gated_ffn_args: the operands of mc_gated_ffn and its gradient."""
+    _fields_ = [("rows", c_int64), ("dim", c_int), ("hidden", c_int), ("type", c_int), ("activation", c_int), ("x_dev", c_void_p), ("x_stride", c_int64),
+                ("gate_dev", c_void_p), ("gate_stride", c_int64), ("up_dev", c_void_p), ("up_stride", c_int64)]
+
+
 class MagicubeError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -158,6 +178,19 @@ def _load() -> ctypes.CDLL:
                                  POINTER(RopeKeys), c_void_p]
     L.mc_cache_read.argtypes = [POINTER(CacheDescription), c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int64,
                                 c_void_p]
+    L.mc_block_norm.argtypes = [POINTER(BlockNormArgs), c_void_p, c_int64, c_void_p, c_int64, c_void_p]
+    L.mc_block_norm_backward_workspace.argtypes = [c_int64, c_int]; L.mc_block_norm_backward_workspace.restype = c_size_t
+    L.mc_block_norm_backward.argtypes = [POINTER(BlockNormArgs), c_void_p, c_int64, c_void_p, c_int64, POINTER(BlockNormGrads), c_void_p, c_size_t, c_void_p]
+    L.mc_gated_ffn_workspace.argtypes = [POINTER(GatedFfnArgs)]; L.mc_gated_ffn_workspace.restype = c_size_t
+    L.mc_gated_ffn.argtypes = [POINTER(GatedFfnArgs), c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+    L.mc_gated_ffn_backward_workspace.argtypes = [POINTER(GatedFfnArgs)]; L.mc_gated_ffn_backward_workspace.restype = c_size_t
+    L.mc_gated_ffn_backward.argtypes = [POINTER(GatedFfnArgs), c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64,
+                                        c_void_p, c_size_t, c_void_p]
+    L.mc_token_logprobs_workspace.argtypes = [c_int64, c_int, c_int, c_int]; L.mc_token_logprobs_workspace.restype = c_size_t
+    L.mc_token_logprobs.argtypes = [c_void_p, c_int, c_int64, c_int, c_int64, c_void_p, c_float, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_size_t, c_void_p]
+    L.mc_token_logprobs_backward.argtypes = [c_void_p, c_int, c_int64, c_int, c_int64, c_void_p, c_float, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_int64, c_void_p]
     L.mc_cache_attention_workspace.argtypes = [POINTER(CacheDescription), c_int, c_int, c_int, c_int]
     L.mc_cache_attention_workspace.restype = c_size_t
     L.mc_cache_attention.argtypes = [POINTER(CacheDescription), c_void_p, c_int, c_int64, c_int, c_int64, c_int64, c_void_p, c_int, c_int,

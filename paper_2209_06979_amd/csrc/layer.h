@@ -129,9 +129,37 @@ inline bool few_rows_best(int64_t rows, int hidden, bool copies)
     return rows <= FEW_ROWS && (copies || (rows <= 32 && hidden <= 32 * 256) || (rows <= 4 && hidden <= 32 * 384));
 }
 hipError_t launch_gated_product(const ProductArgs &a, mc_type type, hipStream_t s);
-// Shapes of a product's tiles, and pieces along k
+constexpr int COMPUTE_UNITS = 256;
+// Tiles of a product (256, 128, 96 for 128 x 64, 64, or 32 for 32 x 64), and pieces along k
 struct ProductPlan { int tile, splits; };
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type type, bool gated);
+// The shape of tiles and number of pieces along k with the smallest expected time.  A step of 128 bytes of k takes a workgroup `alone` (us) by itself on a compute
+// unit, which runs `together` of them at once and spends `busy` on a step of each when it is full; the pieces' sums cost a launch and their bytes.
+// Measured, us, tiles of 256 x 256, 128 x 128, 128 x 64, 64 x 64 and 32 x 64 (with the best number of pieces), dx of rows x dim from hidden:
+//   bf16  4096 x 4096 from 11008   566, 760, 1148, 1325, 1732        fp32  2048 x 2048 from 5632   698, 669, 682, 730, 808
+//         1024 x 4096 from 4096    87, 82, 86, 117, 176                    777 x 1001 from 2731    145, 107, 103, 105, 110
+//         128 x 4096 from 14336    80, 62, 65, 79, 98                      100 x 512 from 1400     70, 27, 19, 15, 12
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int batch, mc_type type, bool gated)
+{
+    struct Shape { int tile, m, n, together; double alone, busy; };
+    static constexpr Shape shapes[2][5] = {{{256, 256, 256, 1, 7.3, 7.3}, {128, 128, 128, 2, 2.05, 1.9}, {96, 128, 64, 2, 1.2, 0.97}, {64, 64, 64, 3, 0.8, 0.53}, {32, 32, 64, 4, 0.5, 0.31}},
+                                           {{256, 256, 256, 1, 1.45, 1.45}, {128, 128, 128, 2, 0.65, 0.55}, {96, 128, 64, 2, 0.5, 0.4}, {64, 64, 64, 3, 0.375, 0.24}, {32, 32, 64, 4, 0.34, 0.16}}};
+    const int64_t size = type == MC_F32 ? 4 : 2, steps = (k * size + 127) / 128;
+    ProductPlan best = {256, 1};
+    double least = 1e30;
+    for (const Shape &s : shapes[type != MC_F32]) {
+        const int64_t tiles = (m + s.m - 1) / s.m * ((n * (gated ? 2 : 1) + s.n - 1) / s.n) * batch;
+        if (s.tile != 256 && tiles > 1 << 22) continue; // (a grid's threads are counted in 32 bits)
+        for (int splits = 1; splits <= (gated ? 1 : 16); ++splits) {
+            if (splits > 1 && (steps / splits < 4 || tiles * splits > 4096)) break;
+            const int64_t each = (tiles * splits + COMPUTE_UNITS - 1) / COMPUTE_UNITS, rounds = (each + s.together - 1) / s.together;
+            const double alone = rounds * s.alone, busy = each * s.busy;
+            double us = (alone > busy ? alone : busy) * ((double)(steps + splits - 1) / splits) + 3;
+            if (splits > 1) us += 6 + (splits + 1) * (double)(m * n * batch) * 4 / 3.5e6;
+            if (us < least) least = us, best = {s.tile, splits};
+        }
+    }
+    return best;
+}
 // B has a row for each k, and so has A if a_rows
 hipError_t launch_product(const ProductArgs &a, ProductPlan p, bool a_rows, mc_type type, hipStream_t s);
 hipError_t launch_few_rows(const FewRowsArgs &a, mc_type type, hipStream_t s);
