@@ -443,33 +443,31 @@ template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, b
             if (!late) asm volatile("s_barrier" ::: "memory");
         }
     } else {
-        for (; u < end; u += turns) {
-            ask_of(u);
-            clear();
-            const int steps = asked.steps;
+        // (a tile to a workgroup: with a loop over tiles the arguments of all that follows were held in scalar registers, more than there are)
+        ask_of(u);
+        clear();
+        const int steps = asked.steps;
 #pragma unroll
-            for (int s = 0; s < NS - 1; ++s)
-                if (s < steps) request(step_of(s), s);
-            for (int s = 0; s < steps; ++s) {
-                if (s + NS - 1 <= steps) mcu::vm_wait<(NS - 2) * COPIES>(); // (step s has come: that many copies were asked for behind it)
-                else mcu::vm_wait<0>();
-                asm volatile("s_barrier" ::: "memory"); // for all waves, whose reads of the stage that is written next have returned, too
-                if (s + NS - 1 < steps) request(step_of(s + NS - 1), (s + NS - 1) % NS);
-                const char *const la = lds[s % NS], *const lb = lds[s % NS] + BM * STEP;
+        for (int s = 0; s < NS - 1; ++s)
+            if (s < steps) request(step_of(s), s);
+        for (int s = 0; s < steps; ++s) {
+            if (s + NS - 1 <= steps) mcu::vm_wait<(NS - 2) * COPIES>(); // (step s has come: that many copies were asked for behind it)
+            else mcu::vm_wait<0>();
+            asm volatile("s_barrier" ::: "memory"); // for all waves, whose reads of the stage that is written next have returned, too
+            if (s + NS - 1 < steps) request(step_of(s + NS - 1), (s + NS - 1) % NS);
+            const char *const la = lds[s % NS], *const lb = lds[s % NS] + BM * STEP;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    v4i fa[MF], fb[NF];
+            for (int h = 0; h < 2; ++h) {
+                v4i fa[MF], fb[NF];
 #pragma unroll
-                    for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
+                for (int m = 0; m < MF; ++m) fa[m] = oa.read(la, m, h, lane);
 #pragma unroll
-                    for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
-                    multiply<TYPE>(fb, fa, acc);
-                }
-                mcu::lgkm_wait();
+                for (int n = 0; n < NF; ++n) fb[n] = ob.read(lb, n, h, lane);
+                multiply<TYPE>(fb, fa, acc);
             }
-            finish(asked);
-            asm volatile("s_barrier" ::: "memory"); // (all reads of this tile's stages have returned)
+            mcu::lgkm_wait();
         }
+        finish(asked);
     }
 }
 
