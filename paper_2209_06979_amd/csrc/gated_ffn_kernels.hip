@@ -41,7 +41,8 @@ template <int KIND> __device__ __forceinline__ float activated(float g, float &s
         return g * c;
     } else if constexpr (KIND == MC_ACT_GELU_TANH) {
         const float p = sigmoid(2.0f * GELU_A * (g + GELU_B * g * g * g));
-        slope = p + p * (1.0f - p) * 2.0f * GELU_A * (g + 3.0f * GELU_B * g * g * g);
+        const float q = p * (1.0f - p); // (0 far from 0, where the cube may be infinite)
+        slope = q == 0 ? p : p + q * 2.0f * GELU_A * (g + 3.0f * GELU_B * g * g * g);
         return g * p;
     } else if constexpr (KIND == MC_ACT_RELU) {
         slope = g > 0 ? 1 : g != g ? g : 0;

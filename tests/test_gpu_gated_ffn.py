@@ -81,6 +81,24 @@ def test_far_arguments(act):
     _train(x, one, one, act)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("act", ACTIVATIONS)
+def test_arguments_whose_cubes_are_infinite(dtype, act):
+    """Values and slopes of activations at 1e13 .. 1e30: those of their limits, exactly.  (u is 1, and the gate's and up weights name one element of x each.)"""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    t = getattr(torch, dtype)
+    far = torch.tensor([1e13, 1e14, 1e20, 1e30], device="cuda").to(t)
+    x = torch.stack([torch.cat([far, -far]), torch.ones(8, device="cuda", dtype=t)], 1).requires_grad_(True)
+    eye = torch.eye(2, device="cuda", dtype=t)
+    h = mc.gated_ffn(x, eye[:1].contiguous(), eye[1:].contiguous(), activation=act)
+    above = torch.cat([torch.ones_like(far), torch.zeros_like(far)])
+    value = above if act == "sigmoid" else torch.cat([far, torch.zeros_like(far)])
+    assert torch.equal(h.detach()[:, 0], value)
+    d, = torch.autograd.grad(h.sum(), x)
+    assert torch.equal(d[:, 0], torch.zeros_like(above) if act == "sigmoid" else above) and torch.equal(d[:, 1], value)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows", [9, 150])
 def test_strides(dtype, rows):
