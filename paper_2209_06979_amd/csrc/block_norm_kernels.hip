@@ -195,7 +195,7 @@ __device__ __forceinline__ void decode_parameters(const RawParameters &r, int ty
 template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __global__ __launch_bounds__(THREADS *PACKED) void block_norm_kernel(NormArgs a)
 {
     __shared__ float shared[4 * THREADS / 64];
-    const int64_t row = (int64_t)blockIdx.x * PACKED + (PACKED > 1 ? threadIdx.x / THREADS : 0);
+    const int64_t row = a.first + (int64_t)blockIdx.x * PACKED + (PACKED > 1 ? threadIdx.x / THREADS : 0);
     if (row >= a.rows) return;
     Row<THREADS, E> of = {(int)(PACKED > 1 ? threadIdx.x % THREADS : threadIdx.x), a.dim, 1.0f / a.dim, shared, 0};
     // (chunks beyond a whole row: the first elements, and zeros from where they are decoded on)
@@ -533,12 +533,18 @@ __global__ __launch_bounds__(SUM_COLUMNS / 4 * SUM_LINES) void block_norm_sum_ke
     store_one(out, a.p_type, (slot >= 0 ? 0 : group * a.dgate_stride) + blockIdx.x * SUM_COLUMNS + threadIdx.x, sum);
 }
 
-template <int TYPE, int RTYPE, int THREADS, int E> hipError_t forward(const NormArgs &a, hipStream_t s)
+template <int TYPE, int RTYPE, int THREADS, int E> hipError_t forward(NormArgs a, hipStream_t s)
 {
     constexpr int PACKED = THREADS == 64 ? 4 : 1;
-    const dim3 grid((unsigned)((a.rows + PACKED - 1) / PACKED)), block(THREADS * PACKED);
-    return a.dim % 8 == 0 ? launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, true>), grid, block, 0, s, a)
-                          : launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, false>), grid, block, 0, s, a);
+    constexpr int64_t MOST = NORM_LAUNCH_THREADS / (THREADS * PACKED) * PACKED; // rows of a launch
+    hipError_t e = hipSuccess;
+    for (a.first = 0; a.first < a.rows && e == hipSuccess; a.first += MOST) {
+        const int64_t rows = a.rows - a.first < MOST ? a.rows - a.first : MOST;
+        const dim3 grid((unsigned)((rows + PACKED - 1) / PACKED)), block(THREADS * PACKED);
+        e = a.dim % 8 == 0 ? launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, true>), grid, block, 0, s, a)
+                           : launch_kernel((block_norm_kernel<TYPE, RTYPE, THREADS, E, PACKED, false>), grid, block, 0, s, a);
+    }
+    return e;
 }
 template <int TYPE, int RTYPE> hipError_t forward_of(const NormArgs &a, hipStream_t s)
 {

@@ -17,6 +17,7 @@ struct NormArgs {
     float branch_scale, residual_scale, eps;
     void *y, *n;                   // null: not written
     int64_t y_stride, n_stride;
+    int64_t first;                 // first row of a launch (filled by the launcher)
     // backward
     const void *dy, *dn;           // null: zeros
     int64_t dy_stride, dn_stride;
@@ -29,6 +30,7 @@ struct NormArgs {
     float *partial;                // workgroups x (2 for the gate, 4) x dim; rows of more than NORM_SUMS elements: eight floats for each row
 };
 constexpr int NORM_MOST_DIM = 16384, NORM_SUMS = 4096;
+constexpr int64_t NORM_LAUNCH_THREADS = (int64_t)1 << 31; // (a grid's threads are counted in 32 bits: more rows take further launches)
 // Workgroups that a backward pass is cut into, at most: as many as run at once
 inline int norm_workgroups(int64_t rows, int dim)
 {

@@ -191,6 +191,21 @@ def test_no_rows():
     assert not dw.any() and not dg.any() and dg.shape == gate.shape
 
 
+def test_more_rows_than_a_grid_has():
+    """Rows of one element, 64 threads each: 2^32 + 320 threads.  n is within a rounding to bf16 and 1e-6 (a few fp32 roundings) of the formula's."""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    rows = (1 << 26) + 5
+    x = torch.randn(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).to(torch.bfloat16)[:, None]
+    w = torch.full((1,), 3.0, device="cuda", dtype=torch.bfloat16)
+    y, n = mc.block_norm(x, weight=w, eps=0.5)
+    assert y is x and n.shape == x.shape
+    for i in range(0, rows, 1 << 24):
+        v = x[i:i + (1 << 24)].float()
+        want = 3 * v / torch.sqrt(v * v + 0.5)
+        assert ((n[i:i + (1 << 24)].float() - want).abs() <= (2.0 ** -8 + 1e-6) * want.abs()).all()
+
+
 def test_runs_are_alike_and_streams():
     import torch
     v, kw = _problem(3001, 776, PAIRS[2], pre="rms", post="rms", groups=1)
