@@ -20,18 +20,18 @@ using mcu::v4i;
 // Eight elements as they lie in memory
 template <int TYPE> struct Raw { v4i v[TYPE == MC_F32 ? 2 : 1]; };
 
-// `n` of them from element `at` on (any alignment), zeros behind them
-template <int TYPE> __device__ __forceinline__ Raw<TYPE> load(const void *p, int64_t at, int n)
+// Those from element `at` on, at any alignment; of a row of fewer than eight (`dim`), zeros behind them
+template <int TYPE> __device__ __forceinline__ Raw<TYPE> load(const void *p, int64_t at, int dim)
 {
     typedef typename RealOf<TYPE>::type T;
     const T *from = static_cast<const T *>(p) + at;
-    Raw<TYPE> r = {};
-    if (n >= 8) {
+    Raw<TYPE> r;
+    if (dim >= 8) {
         __builtin_memcpy(&r, from, sizeof r);
-    } else if (n > 0) {
+    } else {
         T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? from[i] : (T)0;
+        for (int i = 0; i < 8; ++i) e[i] = i < dim ? from[i] : (T)0;
         __builtin_memcpy(&r, e, sizeof r);
     }
     return r;
@@ -43,19 +43,20 @@ template <int TYPE> __device__ __forceinline__ void decode(const Raw<TYPE> &r, f
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)e[i];
 }
-template <int TYPE> __device__ __forceinline__ void store(void *p, int64_t at, int n, const float (&v)[8])
+// Elements lo .. n - 1
+template <int TYPE> __device__ __forceinline__ void store(void *p, int64_t at, int lo, int n, const float (&v)[8])
 {
     typedef typename RealOf<TYPE>::type T;
     T *to = static_cast<T *>(p) + at, e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = (T)v[i];
-    if (n >= 8) {
+    if (lo <= 0 && n >= 8) {
         __builtin_memcpy(to, e, sizeof e);
-    } else if (n > 0) {
+    } else if (lo < n) {
         asm volatile("" ::: "memory"); // (the compiler would else make some elements' stores those of both cases, and write whole chunks in parts)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) to[i] = e[i];
+            if (i >= lo && i < n) to[i] = e[i];
         asm volatile("" ::: "memory");
     }
 }
@@ -74,30 +75,50 @@ __device__ __forceinline__ float wave_sum(float x)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A row over THREADS threads, E chunks of eight elements each: chunk k of thread t begins at element 8 (t + k THREADS).
+// A row over THREADS threads, E chunks of eight elements each: chunk k of thread t begins at element 8 (t + k THREADS).  A last chunk that would reach
+// beyond the row is the row's last eight elements, of which the chunk's own follow those of the one before; chunks that begin beyond it have none.  So
+// every load is a whole one, without a branch that would wait for it (the gradient of 16384 x 4096 bf16 225 -> 180 us, of 4016 x 1153 fp32, with two sums' barriers less, 55 -> 44).
+// Elements that are not the chunk's own are taken for zeros.
 template <int THREADS, int E> struct Row {
     static constexpr int WAVES = THREADS / 64;
     int t, dim;
     float inverse;    // 1 / dim
-    float *shared;    // 2 x WAVES x 2 floats
+    float *shared;    // 2 x WAVES x 4 floats
     int turn;         // which half of them the next sum uses (one barrier to a sum)
 
     __device__ __forceinline__ int at(int k) const { return 8 * (t + k * THREADS); }
-    __device__ __forceinline__ int count(int k) const { return min(max(dim - at(k), 0), 8); }
-    __device__ __forceinline__ void sums(float &a, float &b)
+    __device__ __forceinline__ int place(int k) const { return max(min(at(k), dim - 8), 0); }
+    __device__ __forceinline__ int elements() const { return min(dim, 8); }
+    __device__ __forceinline__ int first(int k) const { return at(k) - place(k); } // of the chunk's own
+    __device__ __forceinline__ bool own(int k, int e) const { return e >= first(k) && (e == 0 || e < dim); }
+    __device__ __forceinline__ bool full() const { return E * THREADS * 8 == dim; } // every chunk is whole
+    __device__ __forceinline__ void trim(float (&v)[E][8]) const
     {
-        a = wave_sum(a);
-        b = wave_sum(b);
+        if (full()) return;
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = own(k, e) ? v[k][e] : 0;
+    }
+    template <int N> __device__ __forceinline__ void sums(float (&v)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
         if constexpr (WAVES > 1) {
-            float *s = shared + turn * 2 * WAVES;
+            float *s = shared + turn * 4 * WAVES;
             turn ^= 1;
-            if ((t & 63) == 0) s[2 * (t >> 6)] = a, s[2 * (t >> 6) + 1] = b;
+            if ((t & 63) == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[4 * (t >> 6) + i] = v[i];
             __syncthreads();
-            a = s[2 * (t & (WAVES - 1))], b = s[2 * (t & (WAVES - 1)) + 1]; // (a wave's to each lane)
-            a += exchanged<0xb1>(a), b += exchanged<0xb1>(b);
-            if constexpr (WAVES > 2) a += exchanged<0x4e>(a), b += exchanged<0x4e>(b);
-            if constexpr (WAVES > 4) a += exchanged<0x141>(a), b += exchanged<0x141>(b);
-            if constexpr (WAVES > 8) a += exchanged<0x140>(a), b += exchanged<0x140>(b);
+#pragma unroll
+            for (int i = 0; i < N; ++i) { // (a wave's to each lane)
+                v[i] = s[4 * (t & (WAVES - 1)) + i];
+                v[i] += exchanged<0xb1>(v[i]);
+                if constexpr (WAVES > 2) v[i] += exchanged<0x4e>(v[i]);
+                if constexpr (WAVES > 4) v[i] += exchanged<0x141>(v[i]);
+                if constexpr (WAVES > 8) v[i] += exchanged<0x140>(v[i]);
+            }
         }
     }
     // v (zeros beyond the row) becomes its normed values, zeros beyond the row; returns 1 / deviation.
@@ -108,28 +129,50 @@ template <int THREADS, int E> struct Row {
     }
     __device__ __forceinline__ float norm(float (&v)[E][8], int kind, float eps, float &m)
     {
-        float q = 0, none = 0;
-        m = 0;
-        if (kind == MC_NORM_LAYER) {
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m += v[k][e];
-            sums(m, none);
-            m /= dim;
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                const int n = count(k);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] = e < n ? v[k][e] - m : 0;
-            }
-        }
+        float z[2] = {0, 0}; // of squares, of elements
 #pragma unroll
         for (int k = 0; k < E; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q += v[k][e] * v[k][e];
-        sums(q, none);
-        const float r = 1.0f / sqrtf(q * inverse + eps);
+            for (int e = 0; e < 8; ++e) z[0] += v[k][e] * v[k][e], z[1] += v[k][e];
+        if (kind == MC_NORM_LAYER) {
+            sums(z);
+            return centred(v, z[1], z[0], eps, m);
+        }
+        float q[1] = {z[0]};
+        sums(q);
+        m = 0;
+        const float r = 1.0f / sqrtf(q[0] * inverse + eps);
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] *= r;
+        return r;
+    }
+    // Whether a variance may be taken from the sums of elements and of squares: its error is a rounding times 1 + mean^2 / variance, here at most two.
+    __device__ __forceinline__ bool near(float sum, float squares) const
+    {
+        const float m = sum / dim;
+        return __builtin_amdgcn_readfirstlane(m * m <= squares * inverse - m * m);
+    }
+    // The layer norm, from the sums; around the mean where that is far from 0.
+    __device__ __forceinline__ float centred(float (&v)[E][8], float sum, float squares, float eps, float &m)
+    {
+        m = sum / dim;
+        const bool direct = near(sum, squares);
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] -= m;
+        trim(v);
+        float q[1] = {0};
+        if (!direct) {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[0] += v[k][e] * v[k][e];
+            sums(q);
+        }
+        const float r = 1.0f / sqrtf((direct ? squares * inverse - m * m : q[0] * inverse) + eps);
 #pragma unroll
         for (int k = 0; k < E; ++k)
 #pragma unroll
@@ -141,23 +184,23 @@ template <int THREADS, int E> struct Row {
     {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            const int n = count(k);
             if (!p) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] = e < n ? otherwise : 0;
+                for (int e = 0; e < 8; ++e) v[k][e] = otherwise;
             } else if (type == MC_F32) {
-                decode(load<MC_F32>(p, from + at(k), n), v[k]);
+                decode(load<MC_F32>(p, from + place(k), dim), v[k]);
             } else if (type == MC_F16) {
-                decode(load<MC_F16>(p, from + at(k), n), v[k]);
+                decode(load<MC_F16>(p, from + place(k), dim), v[k]);
             } else {
-                decode(load<MC_BF16>(p, from + at(k), n), v[k]);
+                decode(load<MC_BF16>(p, from + place(k), dim), v[k]);
             }
         }
+        trim(v);
     }
     template <int TYPE> __device__ __forceinline__ void write(void *p, int64_t from, const float (&v)[E][8]) const
     {
 #pragma unroll
-        for (int k = 0; k < E; ++k) store<TYPE>(p, from + at(k), count(k), v[k]);
+        for (int k = 0; k < E; ++k) store<TYPE>(p, from + place(k), first(k), elements(), v[k]);
     }
     __device__ __forceinline__ void write_parameters(void *p, int type, int64_t from, const float (&v)[E][8]) const
     {
@@ -174,13 +217,13 @@ template <int THREADS, int E> struct Row {
 
 // Parameters as they lie in memory, of a type that is known when the kernel runs
 struct RawParameters { v4i lo, hi; };
-__device__ __forceinline__ RawParameters load_parameters(const void *p, int type, int64_t at, int n)
+__device__ __forceinline__ RawParameters load_parameters(const void *p, int type, int64_t at, int dim)
 {
     if (type == MC_F32) {
-        const Raw<MC_F32> r = load<MC_F32>(p, at, n);
+        const Raw<MC_F32> r = load<MC_F32>(p, at, dim);
         return {r.v[0], r.v[1]};
     }
-    const Raw<MC_F16> r = load<MC_F16>(p, at, n); // (or bf16: bits, and zeros)
+    const Raw<MC_F16> r = load<MC_F16>(p, at, dim); // (or bf16: bits, and zeros)
     return {r.v[0], r.v[0]};
 }
 __device__ __forceinline__ void decode_parameters(const RawParameters &r, int type, float (&v)[8])
@@ -194,29 +237,27 @@ __device__ __forceinline__ void decode_parameters(const RawParameters &r, int ty
 // 4096 bf16 took 141 us instead of 101.)
 template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __global__ __launch_bounds__(THREADS *PACKED) void block_norm_kernel(NormArgs a)
 {
-    __shared__ float shared[4 * THREADS / 64];
+    __shared__ float shared[8 * THREADS / 64];
     const int64_t row = a.first + (int64_t)blockIdx.x * PACKED + (PACKED > 1 ? threadIdx.x / THREADS : 0);
     if (row >= a.rows) return;
     Row<THREADS, E> of = {(int)(PACKED > 1 ? threadIdx.x % THREADS : threadIdx.x), a.dim, 1.0f / a.dim, shared, 0};
-    // (chunks beyond a whole row: the first elements, and zeros from where they are decoded on)
-    auto at = [&](int k) { return WHOLE && of.at(k) >= a.dim ? 0 : of.at(k); };
-    auto count = [&](int k) { return WHOLE ? 8 : of.count(k); };
+    const int loaded = WHOLE ? 8 : a.dim;
     Raw<TYPE> x[E];
     Raw<RTYPE> r[E];
     RawParameters pw[E], g[E], w[E];
 #pragma unroll
-    for (int k = 0; k < E; ++k) x[k] = load<TYPE>(a.x, row * a.x_stride + at(k), count(k));
+    for (int k = 0; k < E; ++k) x[k] = load<TYPE>(a.x, row * a.x_stride + of.place(k), loaded);
     if (a.r)
 #pragma unroll
-        for (int k = 0; k < E; ++k) r[k] = load<RTYPE>(a.r, row * a.r_stride + at(k), count(k));
+        for (int k = 0; k < E; ++k) r[k] = load<RTYPE>(a.r, row * a.r_stride + of.place(k), loaded);
     auto ask = [&](RawParameters (&to)[E], const void *p, int64_t from) {
         if (!p) return;
         if (a.p_type == MC_F32) {
 #pragma unroll
-            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F32, from + at(k), count(k));
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F32, from + of.place(k), loaded);
         } else {
 #pragma unroll
-            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F16, from + at(k), count(k));
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F16, from + of.place(k), loaded);
         }
     };
     ask(pw, a.post_weight, 0);
@@ -242,18 +283,9 @@ template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __glo
             }
         }
     };
-    auto trim = [&] { // zeros beyond the row
-        if (WHOLE && E * THREADS * 8 == a.dim) return;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const int n = of.count(k);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] = e < n ? v[k][e] : 0;
-        }
-    };
 #pragma unroll
     for (int k = 0; k < E; ++k) decode(x[k], v[k]);
-    trim();
+    of.trim(v);
     if (a.post) {
         of.norm(v, a.post, a.eps);
         times(pw, a.post_weight, a.post_bias);
@@ -265,7 +297,7 @@ template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __glo
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[k][e] = a.branch_scale * v[k][e] + (a.r ? a.residual_scale * f[e] : 0);
     }
-    trim();
+    of.trim(v);
     if (a.y) of.template write<RTYPE>(a.y, row * a.y_stride, v);
     if (!a.pre) return;
     of.norm(v, a.pre, a.eps);
@@ -273,16 +305,17 @@ template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __glo
     of.template write<TYPE>(a.n, row * a.n_stride, v);
 }
 
-// LAYER: one of the norms takes means, or there are biases.  Parameters stay in registers with one chunk to a thread, and are read again for each row (from
-// the caches) with more; the next row is asked for ahead with up to two.  SUMS false: the sums over rows, which would not fit into the registers of so wide a row, are left to
+// LAYER: one of the norms takes means, or there are biases.  With one chunk to a thread parameters stay in registers and the next row is asked for ahead; with two
+// parameters are read again for each row (from the caches), where they are used.  SUMS false: the sums over rows, which would not fit into the registers of so wide a row, are left to
 // the kernel below, for which a row's means and deviations are written out.
-template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __global__ __launch_bounds__(THREADS, THREADS == 512 || (LAYER && RTYPE == MC_F32) ? 2 : 3) void block_norm_backward_kernel(NormArgs a)
+template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : THREADS == 512 || (LAYER && RTYPE == MC_F32) ? 2 : 3) void block_norm_backward_kernel(NormArgs a)
 {
-    __shared__ float shared[4 * THREADS / 64];
+    __shared__ float shared[8 * THREADS / 64];
     Row<THREADS, E> of = {(int)threadIdx.x, a.dim, 1.0f / a.dim, shared, 0};
     const int64_t first = blockIdx.x * a.per, end = min(first + a.per, a.rows);
     float w[E][8], pw[E][8], pb[LAYER ? E : 1][8], g[E][8]; // (g: times the branch's scale)
-    constexpr bool HELD = E == 1, AHEAD = E <= 2;
+    constexpr bool HELD = E == 1, AHEAD = E == 1;
+    auto read_here = [] { if constexpr (!HELD) asm volatile("" ::: "memory"); }; // (parameters that are read again are not asked for ahead, into registers that are not there)
     auto post_parameters = [&] {
         of.parameters(pw, a.post_weight, a.p_type, 0, 1);
         if constexpr (LAYER) of.parameters(pb, a.post_bias, a.p_type, 0, 0);
@@ -294,16 +327,15 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
     if (!a.gate) EACH(k, e) g[k][e] = a.branch_scale;
     float sum_g[E][8] = {}, sum_w[E][8] = {}, sum_pw[E][8] = {}, sum_b[LAYER ? E : 1][8] = {}, sum_pb[LAYER ? E : 1][8] = {};
     float *const mine = a.partial + (int64_t)blockIdx.x * 6 * a.dim;
-    Raw<TYPE> rx[E], rdn[E];
-    Raw<RTYPE> rr[E], rdy[E];
+    Raw<TYPE> rx[E], rdn[E] = {};
+    Raw<RTYPE> rr[E] = {}, rdy[E] = {};
     auto ask = [&](int64_t row) {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            const int n = row < end ? of.count(k) : 0;
-            rx[k] = load<TYPE>(a.x, row * a.x_stride + of.at(k), n);
-            rr[k] = load<RTYPE>(a.r, row * a.r_stride + of.at(k), a.r ? n : 0);
-            rdn[k] = load<TYPE>(a.dn, row * a.dn_stride + of.at(k), a.dn ? n : 0);
-            rdy[k] = load<RTYPE>(a.dy, row * a.dy_stride + of.at(k), a.dy ? n : 0);
+            rx[k] = load<TYPE>(a.x, row * a.x_stride + of.place(k), a.dim);
+            if (a.r) rr[k] = load<RTYPE>(a.r, row * a.r_stride + of.place(k), a.dim);
+            if (a.dn) rdn[k] = load<TYPE>(a.dn, row * a.dn_stride + of.place(k), a.dim);
+            if (a.dy) rdy[k] = load<RTYPE>(a.dy, row * a.dy_stride + of.place(k), a.dim);
         }
     };
     if constexpr (AHEAD) ask(first);
@@ -319,47 +351,85 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
             decode(rdn[k], d[k]);
             decode(rdy[k], dy[k]);
         }
-        if constexpr (AHEAD) ask(row + 1);
-        if (a.gate && (fresh || !HELD)) {
+        of.trim(hat1);
+        of.trim(hat2);
+        of.trim(d);
+        if constexpr (AHEAD) ask(min(row + 1, end - 1));
+        if (HELD && a.gate && fresh) {
             of.parameters(g, a.gate, a.p_type, group * a.gate_stride, 1);
             EACH(k, e) g[k][e] *= a.branch_scale;
         }
         float m1 = 0, m2 = 0, r2 = 0, mean2 = 0, dot2 = 0;
         const float r1 = a.post ? of.norm(hat1, a.post, a.eps, m1) : 1;
-        if constexpr (!HELD) post_parameters();
-        EACH(k, e) {
-            float b = hat1[k][e] * pw[k][e];
-            if constexpr (LAYER) b += pb[k][e];
-            hat2[k][e] = g[k][e] * b + (a.r ? a.residual_scale * hat2[k][e] : 0); // y
+        if constexpr (HELD) {
+            EACH(k, e) {
+                float b = hat1[k][e] * pw[k][e];
+                if constexpr (LAYER) b += pb[k][e];
+                hat2[k][e] = g[k][e] * b + (a.r ? a.residual_scale * hat2[k][e] : 0); // y
+            }
+        } else {
+            float b[E][8], f[E][8];
+            read_here();
+            of.parameters(b, a.post_weight, a.p_type, 0, 1);
+            EACH(k, e) b[k][e] *= hat1[k][e];
+            if constexpr (LAYER) {
+                read_here();
+                of.parameters(f, a.post_bias, a.p_type, 0, 0);
+                EACH(k, e) b[k][e] += f[k][e];
+            }
+            if (a.gate) {
+                read_here();
+                of.parameters(f, a.gate, a.p_type, group * a.gate_stride, 1);
+                EACH(k, e) b[k][e] *= f[k][e];
+            }
+            EACH(k, e) hat2[k][e] = a.branch_scale * b[k][e] + (a.r ? a.residual_scale * hat2[k][e] : 0);
+            read_here();
         }
         if (a.pre && a.dn) {
-            float mean = 0, dot = 0;
+            float mean, dot;
             if constexpr (!HELD) of.parameters(w, a.weight, a.p_type, 0, 1);
+            if constexpr (!SUMS) EACH(k, e) d[k][e] *= w[k][e];
+            auto dw = [&](int k, int e) { return SUMS ? d[k][e] * w[k][e] : d[k][e]; };
+            // (all sums at once, of y that is not normed yet)
             if (LAYER) {
-                r2 = of.norm(hat2, a.pre, a.eps, m2);
+                float z[4] = {0, 0, 0, 0};
                 EACH(k, e) {
-                    mean += d[k][e] * w[k][e];
-                    dot += d[k][e] * w[k][e] * hat2[k][e];
+                    z[0] += hat2[k][e], z[1] += hat2[k][e] * hat2[k][e], z[2] += dw(k, e), z[3] += dw(k, e) * hat2[k][e];
                 }
-                of.sums(mean, dot);
-                mean = a.pre == MC_NORM_LAYER ? mean / a.dim : 0;
-                dot /= a.dim;
-            } else { // (both sums at once, of y that is not normed yet)
-                float q = 0;
+                of.sums(z);
+                if (a.pre != MC_NORM_LAYER) {
+                    r2 = 1.0f / sqrtf(z[1] * of.inverse + a.eps);
+                    EACH(k, e) hat2[k][e] *= r2;
+                    mean = 0, dot = r2 * z[3] * of.inverse;
+                } else {
+                    const bool direct = of.near(z[0], z[1]);
+                    r2 = of.centred(hat2, z[0], z[1], a.eps, m2);
+                    if (!direct) {
+                        float far[1] = {0};
+                        EACH(k, e) far[0] += dw(k, e) * hat2[k][e];
+                        of.sums(far);
+                        dot = far[0] * of.inverse;
+                    } else {
+                        dot = r2 * (z[3] - m2 * z[2]) * of.inverse;
+                    }
+                    mean = z[2] * of.inverse;
+                }
+            } else {
+                float z[2] = {0, 0};
                 EACH(k, e) {
-                    q += hat2[k][e] * hat2[k][e];
-                    dot += d[k][e] * w[k][e] * hat2[k][e];
+                    z[0] += hat2[k][e] * hat2[k][e];
+                    z[1] += dw(k, e) * hat2[k][e];
                 }
-                of.sums(q, dot);
-                r2 = 1.0f / sqrtf(q * of.inverse + a.eps);
-                dot *= r2 * of.inverse;
+                of.sums(z);
+                r2 = 1.0f / sqrtf(z[0] * of.inverse + a.eps);
+                mean = 0, dot = z[1] * r2 * of.inverse;
                 EACH(k, e) hat2[k][e] *= r2;
             }
             mean2 = mean, dot2 = dot;
             EACH(k, e) {
                 if constexpr (SUMS) sum_w[k][e] += d[k][e] * hat2[k][e];
                 if constexpr (SUMS && LAYER) sum_b[k][e] += d[k][e];
-                dy[k][e] += r2 * (d[k][e] * w[k][e] - mean - hat2[k][e] * dot);
+                dy[k][e] += r2 * (dw(k, e) - mean - hat2[k][e] * dot);
             }
         }
         if (a.dr) {
@@ -370,8 +440,9 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
             float *to = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
             to[0] = m1, to[1] = r1, to[2] = m2, to[3] = r2, to[4] = mean2, to[5] = dot2;
         }
-        float mean = 0, dot = 0;
+        float z[2] = {0, 0};
         if constexpr (!HELD) {
+            read_here();
             post_parameters();
             if (a.gate) {
                 of.parameters(g, a.gate, a.p_type, group * a.gate_stride, 1);
@@ -388,8 +459,9 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
                 if constexpr (LAYER) sum_pb[k][e] += da;
             }
             d[k][e] = da * pw[k][e];
-            mean += e < of.count(k) ? d[k][e] : 0;
-            dot += e < of.count(k) ? d[k][e] * hat1[k][e] : 0;
+            const float mine = of.own(k, e) ? d[k][e] : 0; // (dy is there beyond the row, too)
+            z[0] += mine;
+            z[1] += mine * hat1[k][e];
         }
         // a row of the gate ends here, or the workgroup does: written out whole, or left for the second kernel in the place of a gate's row that began before (0) or in (1) these rows
         fresh = row + 1 == group_end;
@@ -402,9 +474,8 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
         if (fresh) ++group, group_end += a.gate_rows;
         if (!a.dx) continue;
         if (a.post) {
-            of.sums(mean, dot);
-            mean = LAYER && a.post == MC_NORM_LAYER ? mean / a.dim : 0;
-            dot /= a.dim;
+            of.sums(z);
+            const float mean = LAYER && a.post == MC_NORM_LAYER ? z[0] * of.inverse : 0, dot = z[1] * of.inverse;
             EACH(k, e) d[k][e] = r1 * (d[k][e] - mean - hat1[k][e] * dot);
         }
         of.template write<TYPE>(a.dx, row * a.dx_stride, d);
@@ -427,7 +498,7 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
     const int64_t first = blockIdx.y * a.per, end = min(first + a.per, a.rows);
     const int left = a.dim - (int)blockIdx.x * COLUMNS_EACH, shift = blockIdx.x * COLUMNS_EACH; // columns from here on
     Row<COLUMN_THREADS, 1> of = {(int)threadIdx.x, left, 0, nullptr, 0};
-    const int n = of.count(0), at = shift + of.at(0);
+    const int at = shift + of.place(0);
     auto from = [&](const void *p) { return p ? static_cast<const char *>(p) + (int64_t)shift * (a.p_type == MC_F32 ? 4 : 2) : nullptr; };
     float w[1][8], pw[1][8], pb[1][8], g[1][8];
     of.parameters(w, from(a.weight), a.p_type, 0, 1);
@@ -442,8 +513,11 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
         const float *of_row = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
         const float m1 = of_row[0], r1 = of_row[1], m2 = of_row[2], r2 = of_row[3], mean = of_row[4], dot = of_row[5];
         float x[8], r[8], dn[8], dy[8];
-        const Raw<TYPE> rx = load<TYPE>(a.x, row * a.x_stride + at, n), rdn = load<TYPE>(a.dn, row * a.dn_stride + at, a.dn ? n : 0);
-        const Raw<RTYPE> rr = load<RTYPE>(a.r, row * a.r_stride + at, a.r ? n : 0), rdy = load<RTYPE>(a.dy, row * a.dy_stride + at, a.dy ? n : 0);
+        Raw<TYPE> rx = load<TYPE>(a.x, row * a.x_stride + at, left), rdn = {};
+        Raw<RTYPE> rr = {}, rdy = {};
+        if (a.r) rr = load<RTYPE>(a.r, row * a.r_stride + at, left);
+        if (a.dn) rdn = load<TYPE>(a.dn, row * a.dn_stride + at, left);
+        if (a.dy) rdy = load<RTYPE>(a.dy, row * a.dy_stride + at, left);
         if (a.gate && fresh) {
             of.parameters(g, from(a.gate), a.p_type, group * a.gate_stride, 1);
             EACH(k, e) g[k][e] *= a.branch_scale;
@@ -562,14 +636,20 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> hipErr
     if (SUMS || e != hipSuccess || !(a.grads[0] || a.grads[1] || a.grads[2] || a.grads[3] || a.grads[4])) return e;
     return launch_kernel((block_norm_columns_kernel<TYPE, RTYPE>), dim3((a.dim + COLUMNS_EACH - 1) / COLUMNS_EACH, a.workgroups), dim3(COLUMN_THREADS), 0, s, a);
 }
+// Rows of more than 4096 elements, gradients, us (a copy of their bytes takes 78, 78, 78, 157, 157):
+//                                  6510 x 5120 bf16 rms, layer   2712 x 12288 bf16 layer   6510 x 5120 fp32 rms   2034 x 16384 fp32 layer
+//   512 threads, sums with the row     194
+//   512 threads, sums by columns                  279                     637                       333                    687
+//   1024 threads, sums with the row    186        384                                               523
+//   1024 threads, sums by columns      201        196                     455                       283                    497
 template <int TYPE, int RTYPE, bool LAYER> hipError_t backward_kind(const NormArgs &a, hipStream_t s)
 {
     if (a.dim <= 512) return backward<TYPE, RTYPE, 64, 1, LAYER, true>(a, s);
     if (a.dim <= 1024) return backward<TYPE, RTYPE, 128, 1, LAYER, true>(a, s);
     if (a.dim <= 2048) return backward<TYPE, RTYPE, 256, 1, LAYER, true>(a, s);
     if (a.dim <= 4096) return backward<TYPE, RTYPE, 512, 1, LAYER, true>(a, s);
-    if (a.dim <= 8192) return backward<TYPE, RTYPE, 512, 2, LAYER, !LAYER && TYPE != MC_F32>(a, s);
-    return backward<TYPE, RTYPE, 512, 4, LAYER, false>(a, s);
+    if (a.dim <= 8192) return !LAYER && TYPE != MC_F32 ? backward<TYPE, RTYPE, 512, 2, LAYER, true>(a, s) : backward<TYPE, RTYPE, 1024, 1, LAYER, false>(a, s);
+    return backward<TYPE, RTYPE, 1024, 2, LAYER, false>(a, s);
 }
 template <int TYPE, int RTYPE> hipError_t backward_of(const NormArgs &a, hipStream_t s)
 {

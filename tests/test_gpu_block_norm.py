@@ -147,6 +147,16 @@ def test_large_means_and_small_deviations():
     _check(v, kw, *_call(v, kw))
 
 
+@pytest.mark.parametrize("rows,dim", [(5, 7), (6, 1153), (4, 4100), (3, 8192), (3, 16384)])
+@pytest.mark.parametrize("offset", [1.0, 300.0])
+def test_gradients_of_rows_with_means(rows, dim, offset):
+    """Means of both norms' rows about as large as their deviations, and far larger."""
+    for types in (PAIRS[0], PAIRS[3]):
+        v, kw = _problem(rows, dim, types, pre="layer", post="layer", bias=True, offset=offset)
+        v["residual"] += offset
+        _train(v, kw)
+
+
 def test_infinities_and_nan_stay_in_their_rows():
     import torch
     v, kw = _problem(6, 520, post="rms", groups=1)
