@@ -27,7 +27,7 @@ struct NormArgs {
     int64_t dgate_stride;
     int64_t per;                   // rows of a workgroup (filled by the launcher)
     int workgroups;
-    float *partial;                // workgroups x (2 for the gate, 4) x dim; rows of more than NORM_SUMS elements: eight floats for each row
+    float *partial;                // workgroups x (2 for the gate, 4) x dim; rows of more than NORM_SUMS elements, whose sums may be taken by columns: eight floats for each row
 };
 constexpr int NORM_MOST_DIM = 16384, NORM_SUMS = 4096;
 constexpr int64_t NORM_LAUNCH_THREADS = (int64_t)1 << 31; // (a grid's threads are counted in 32 bits: more rows take further launches)

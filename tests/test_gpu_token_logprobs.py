@@ -89,6 +89,27 @@ def test_infinities_and_nan(dtype):
     assert all(torch.equal(a[2:3], b) for a, b in zip((logp, h, tops, at), clean))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,top", [(63, 63), (64, 64), (65, 64), (71, 0), (1003, 1), (9001, 20), (50257, 5)])
+def test_first_elements_of_odd_rows(dtype, vocab, top):
+    """Rows that begin on both sides of a dword, whose first element is the largest, equal to others, forbidden, alone, an infinity or a NaN."""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    x, tokens = _logits(12, vocab + 1, dtype, wider=vocab % 2)
+    x = x[:, 1:]                                          # (an even stride from an odd place, or an odd stride)
+    tokens = torch.zeros_like(tokens)
+    x[:2, 0] = 30.0
+    x[2:4] = 1.5
+    x[4:6, 0] = -math.inf
+    x[6:8, 1:] = -math.inf
+    _check(x[:10], tokens[:10], top)
+    _check(x[1:10], tokens[1:10], top)
+    x[10, 0], x[11, 0] = math.nan, math.inf
+    logp, h, tops, at = mc.token_logprobs(x, tokens, top=top)
+    assert bool(logp[10:].isnan().all() and h[10:].isnan().all() and tops[10:].isnan().all()) and not (top and bool(at[10:, 0].any()))
+    assert not bool(logp[:10].isnan().any())
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "alike", "sawtooth"])
 def test_orders_that_fill_the_list(order):
     """Each element above all before it, and the like."""
