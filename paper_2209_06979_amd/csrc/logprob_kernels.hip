@@ -7,6 +7,8 @@
 // bound: where each has a quarter of `top` keys that reach it, what is below it is not among the row's `top`.  It comes first from the largest element of
 // each lane after the first vectors, sorted, so that only about `top` elements are put in place at the start, and rises with the waves' keys.
 // A row is read by one workgroup, or cut into pieces where there are few rows; a second kernel joins these.
+// Reading bounds them: fp32 8192 x 50257 272 us, 6.0 TB/s; of 16-bit logits an element's conversion, difference, exponential and sums take most of the time that its bytes do (2048 x 128000 bf16 101 us, 5.2 TB/s;
+// with 20 alternatives 116).  The gradient reads and writes as a copy does: 8192 x 50257 bf16 294 us, 5.6 TB/s.
 #include "layer.h"
 
 #include "lds_async.h"
