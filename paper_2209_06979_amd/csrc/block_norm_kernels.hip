@@ -21,11 +21,19 @@ using mcu::v4i;
 // Eight elements as they lie in memory
 template <int TYPE> struct Raw { v4i v[TYPE == MC_F32 ? 2 : 1]; };
 
-// Those from element `at` on, at any alignment; of a row of fewer than eight (`dim`), zeros behind them
-template <int TYPE> __device__ __forceinline__ Raw<TYPE> load(const void *p, int64_t at, int dim)
+// Element `at` behind element `row`, which is the same in all threads.  SHORT: a thread's share of the address is 32 bits, which takes fewer registers and decides how many rows run at
+// once beside a 16-bit stream, and orders the loads worse where it decides nothing (gradients of layer norms, 400 MB of bf16 or 800 of fp32, us with and without: 32552 x 1024 bf16 115, 135, beside
+// fp32 191, 161, fp32 233, 205; 16276 x 2048 bf16 108, 128; 2034 x 16384 bf16 359, 388)
+template <class T, bool SHORT, class V> __device__ __forceinline__ T *address(V *p, int64_t row, int at)
+{
+    if constexpr (SHORT) return reinterpret_cast<T *>(reinterpret_cast<uintptr_t>(static_cast<T *>(p) + row) + (uintptr_t)((unsigned)at * (unsigned)sizeof(T)));
+    else return static_cast<T *>(p) + (row + at);
+}
+// Those from element `at` of a row on, at any alignment; of a row of fewer than eight (`dim`), zeros behind them
+template <int TYPE, bool SHORT = false> __device__ __forceinline__ Raw<TYPE> load(const void *p, int64_t row, int at, int dim)
 {
     typedef typename RealOf<TYPE>::type T;
-    const T *from = static_cast<const T *>(p) + at;
+    const T *from = address<const T, SHORT>(p, row, at);
     Raw<TYPE> r;
     if (dim >= 8) {
         __builtin_memcpy(&r, from, sizeof r);
@@ -45,10 +53,10 @@ template <int TYPE> __device__ __forceinline__ void decode(const Raw<TYPE> &r, f
     for (int i = 0; i < 8; ++i) v[i] = (float)e[i];
 }
 // Elements lo .. n - 1
-template <int TYPE> __device__ __forceinline__ void store(void *p, int64_t at, int lo, int n, const float (&v)[8])
+template <int TYPE, bool SHORT = false> __device__ __forceinline__ void store(void *p, int64_t row, int at, int lo, int n, const float (&v)[8])
 {
     typedef typename RealOf<TYPE>::type T;
-    T *to = static_cast<T *>(p) + at, e[8];
+    T *to = address<T, SHORT>(p, row, at), e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = (T)v[i];
     if (lo <= 0 && n >= 8) {
@@ -80,7 +88,7 @@ __device__ __forceinline__ float wave_sum(float x)
 // beyond the row is the row's last eight elements, of which the chunk's own follow those of the one before; chunks that begin beyond it have none.  So
 // every load is a whole one, without a branch that would wait for it (the gradient of 16384 x 4096 bf16 225 -> 180 us, of 4016 x 1153 fp32, with two sums' barriers less, 55 -> 44).
 // Elements that are not the chunk's own are taken for zeros.
-template <int THREADS, int E> struct Row {
+template <int THREADS, int E, bool SHORT = false> struct Row {
     static constexpr int WAVES = THREADS / 64;
     int t, dim;
     float inverse;    // 1 / dim
@@ -189,11 +197,11 @@ template <int THREADS, int E> struct Row {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[k][e] = otherwise;
             } else if (type == MC_F32) {
-                decode(load<MC_F32>(p, from + place(k), dim), v[k]);
+                decode(load<MC_F32, SHORT>(p, from, place(k), dim), v[k]);
             } else if (type == MC_F16) {
-                decode(load<MC_F16>(p, from + place(k), dim), v[k]);
+                decode(load<MC_F16, SHORT>(p, from, place(k), dim), v[k]);
             } else {
-                decode(load<MC_BF16>(p, from + place(k), dim), v[k]);
+                decode(load<MC_BF16, SHORT>(p, from, place(k), dim), v[k]);
             }
         }
         trim(v);
@@ -201,7 +209,7 @@ template <int THREADS, int E> struct Row {
     template <int TYPE> __device__ __forceinline__ void write(void *p, int64_t from, const float (&v)[E][8]) const
     {
 #pragma unroll
-        for (int k = 0; k < E; ++k) store<TYPE>(p, from + place(k), first(k), elements(), v[k]);
+        for (int k = 0; k < E; ++k) store<TYPE, SHORT>(p, from, place(k), first(k), elements(), v[k]);
     }
     __device__ __forceinline__ void write_parameters(void *p, int type, int64_t from, const float (&v)[E][8]) const
     {
@@ -218,13 +226,13 @@ template <int THREADS, int E> struct Row {
 
 // Parameters as they lie in memory, of a type that is known when the kernel runs
 struct RawParameters { v4i lo, hi; };
-__device__ __forceinline__ RawParameters load_parameters(const void *p, int type, int64_t at, int dim)
+__device__ __forceinline__ RawParameters load_parameters(const void *p, int type, int64_t row, int at, int dim)
 {
     if (type == MC_F32) {
-        const Raw<MC_F32> r = load<MC_F32>(p, at, dim);
+        const Raw<MC_F32> r = load<MC_F32>(p, row, at, dim);
         return {r.v[0], r.v[1]};
     }
-    const Raw<MC_F16> r = load<MC_F16>(p, at, dim); // (or bf16: bits, and zeros)
+    const Raw<MC_F16> r = load<MC_F16>(p, row, at, dim); // (or bf16: bits, and zeros)
     return {r.v[0], r.v[0]};
 }
 __device__ __forceinline__ void decode_parameters(const RawParameters &r, int type, float (&v)[8])
@@ -247,18 +255,18 @@ template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __glo
     Raw<RTYPE> r[E];
     RawParameters pw[E], g[E], w[E];
 #pragma unroll
-    for (int k = 0; k < E; ++k) x[k] = load<TYPE>(a.x, row * a.x_stride + of.place(k), loaded);
+    for (int k = 0; k < E; ++k) x[k] = load<TYPE>(a.x, row * a.x_stride, of.place(k), loaded);
     if (a.r)
 #pragma unroll
-        for (int k = 0; k < E; ++k) r[k] = load<RTYPE>(a.r, row * a.r_stride + of.place(k), loaded);
+        for (int k = 0; k < E; ++k) r[k] = load<RTYPE>(a.r, row * a.r_stride, of.place(k), loaded);
     auto ask = [&](RawParameters (&to)[E], const void *p, int64_t from) {
         if (!p) return;
         if (a.p_type == MC_F32) {
 #pragma unroll
-            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F32, from + of.place(k), loaded);
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F32, from, of.place(k), loaded);
         } else {
 #pragma unroll
-            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F16, from + of.place(k), loaded);
+            for (int k = 0; k < E; ++k) to[k] = load_parameters(p, MC_F16, from, of.place(k), loaded);
         }
     };
     ask(pw, a.post_weight, 0);
@@ -312,7 +320,8 @@ template <int TYPE, int RTYPE, int THREADS, int E, int PACKED, bool WHOLE> __glo
 template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : THREADS == 512 || (LAYER && RTYPE == MC_F32) ? 2 : 3) void block_norm_backward_kernel(NormArgs a)
 {
     __shared__ float shared[8 * THREADS / 64];
-    Row<THREADS, E> of = {(int)threadIdx.x, a.dim, 1.0f / a.dim, shared, 0};
+    constexpr bool SHORT = RTYPE != MC_F32;
+    Row<THREADS, E, SHORT> of = {(int)threadIdx.x, a.dim, 1.0f / a.dim, shared, 0};
     const int64_t first = blockIdx.x * a.per, end = min(first + a.per, a.rows);
     float w[E][8], pw[E][8], pb[LAYER ? E : 1][8], g[E][8]; // (g: times the branch's scale)
     constexpr bool HELD = E == 1, AHEAD = E == 1;
@@ -333,10 +342,10 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> __glob
     auto ask = [&](int64_t row) {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            rx[k] = load<TYPE>(a.x, row * a.x_stride + of.place(k), a.dim);
-            if (a.r) rr[k] = load<RTYPE>(a.r, row * a.r_stride + of.place(k), a.dim);
-            if (a.dn) rdn[k] = load<TYPE>(a.dn, row * a.dn_stride + of.place(k), a.dim);
-            if (a.dy) rdy[k] = load<RTYPE>(a.dy, row * a.dy_stride + of.place(k), a.dim);
+            rx[k] = load<TYPE, SHORT>(a.x, row * a.x_stride, of.place(k), a.dim);
+            if (a.r) rr[k] = load<RTYPE, SHORT>(a.r, row * a.r_stride, of.place(k), a.dim);
+            if (a.dn) rdn[k] = load<TYPE, SHORT>(a.dn, row * a.dn_stride, of.place(k), a.dim);
+            if (a.dy) rdy[k] = load<RTYPE, SHORT>(a.dy, row * a.dy_stride, of.place(k), a.dim);
         }
     };
     if constexpr (AHEAD) ask(first);
@@ -499,7 +508,7 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
     const int64_t first = blockIdx.y * a.per, end = min(first + a.per, a.rows);
     const int left = a.dim - (int)blockIdx.x * COLUMNS_EACH, shift = blockIdx.x * COLUMNS_EACH; // columns from here on
     Row<COLUMN_THREADS, 1> of = {(int)threadIdx.x, left, 0, nullptr, 0};
-    const int at = shift + of.place(0);
+    const int at = of.place(0);
     auto from = [&](const void *p) { return p ? static_cast<const char *>(p) + (int64_t)shift * (a.p_type == MC_F32 ? 4 : 2) : nullptr; };
     float w[1][8], pw[1][8], pb[1][8], g[1][8];
     of.parameters(w, from(a.weight), a.p_type, 0, 1);
@@ -514,11 +523,11 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
         const float *of_row = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
         const float m1 = of_row[0], r1 = of_row[1], m2 = of_row[2], r2 = of_row[3], mean = of_row[4], dot = of_row[5];
         float x[8], r[8], dn[8], dy[8];
-        Raw<TYPE> rx = load<TYPE>(a.x, row * a.x_stride + at, left), rdn = {};
+        Raw<TYPE> rx = load<TYPE>(a.x, row * a.x_stride + shift, at, left), rdn = {};
         Raw<RTYPE> rr = {}, rdy = {};
-        if (a.r) rr = load<RTYPE>(a.r, row * a.r_stride + at, left);
-        if (a.dn) rdn = load<TYPE>(a.dn, row * a.dn_stride + at, left);
-        if (a.dy) rdy = load<RTYPE>(a.dy, row * a.dy_stride + at, left);
+        if (a.r) rr = load<RTYPE>(a.r, row * a.r_stride + shift, at, left);
+        if (a.dn) rdn = load<TYPE>(a.dn, row * a.dn_stride + shift, at, left);
+        if (a.dy) rdy = load<RTYPE>(a.dy, row * a.dy_stride + shift, at, left);
         if (a.gate && fresh) {
             of.parameters(g, from(a.gate), a.p_type, group * a.gate_stride, 1);
             EACH(k, e) g[k][e] *= a.branch_scale;
@@ -642,7 +651,7 @@ template <int TYPE, int RTYPE, int THREADS, int E, bool LAYER, bool SUMS> hipErr
 //   512 threads, sums with the row     194
 //   512 threads, sums by columns                  279                     637                       333                    687
 //   1024 threads, sums with the row    186        384                                               523
-//   1024 threads, sums by columns      201        196                     455                       283                    497
+//   1024 threads, sums by columns      201        198                     419                       282                    506
 template <int TYPE, int RTYPE, bool LAYER> hipError_t backward_kind(const NormArgs &a, hipStream_t s)
 {
     if (a.dim <= 512) return backward<TYPE, RTYPE, 64, 1, LAYER, true>(a, s);
