@@ -21,6 +21,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <cmath>
 
@@ -992,6 +993,26 @@ bool recorded(std::initializer_list<const at::Tensor *> tensors)
             if (x && x->requires_grad()) return true;
     return false;
 }
+// Whether this call is being captured while a graph from outside, of another stream, holds on to a leaf: the backward pass would make that
+// stream wait inside the capture, which torch cannot undo (the process ends).  Refused, with what to do.
+bool captured_beside(const char *what, std::initializer_list<const at::Tensor *> tensors)
+{
+    const c10::Stream here = c10::hip::getCurrentHIPStream().unwrap();
+    for (const at::Tensor *x : tensors) {
+        if (!x || !x->requires_grad() || !x->is_leaf()) continue;
+        const auto node = torch::autograd::impl::try_get_grad_accumulator(*x);
+        if (!node) continue;
+        const std::optional<c10::Stream> there = node->stream();
+        if (!there || *there == here) continue;
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(static_cast<hipStream_t>(stream()), &status) != hipSuccess || status != hipStreamCaptureStatusNone) {
+            PyErr_Format(PyExc_RuntimeError, "%s: captured while results of another stream still hold on to one of the tensors that require grad: free them before the capture", what);
+            return true;
+        }
+        return false;
+    }
+    return false;
+}
 PyObject *no_out_gradient(const char *what)
 {
     PyErr_Format(PyExc_RuntimeError, "%s: out= does not record gradients, and one of the tensors requires grad", what);
@@ -1156,6 +1177,7 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
     at::TensorBase made[2];
     if (recorded({c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) {
         if (out) return no_out_gradient("block_norm");
+        if (captured_beside("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6]})) return nullptr;
         if (!c.trivial || c.args.pre) {
             try {
                 variable_list r = NormNode::apply(*c.t[0], maybe(c.t[1]), maybe(c.t[2]), maybe(c.t[3]), maybe(c.t[4]), maybe(c.t[5]), maybe(c.t[6]), c);
@@ -1268,6 +1290,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
     if (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous())) return assertion();
     if (recorded({c.x, c.gate, c.up, out})) {
         if (out) return no_out_gradient("gated_ffn");
+        if (captured_beside("gated_ffn", {c.x, c.gate, c.up})) return nullptr;
         try {
             return wrap(FfnNode::apply(*c.x, *c.gate, *c.up, c));
         } catch (const Refused &e) {
@@ -1359,6 +1382,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     if (!(c.x = tensor(v[0])) || !(c.tokens = tensor(v[1])) || !integer(v[2], 0, &c.top) || (v[3] && !number(v[3], &c.scale)) || !optional(v[4], &ws)) return nullptr;
     if (!c.fill() || (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous()))) return assertion();
     if (recorded({c.x})) {
+        if (captured_beside("token_logprobs", {c.x})) return nullptr;
         try {
             variable_list r = LogprobNode::apply(*c.x, c);
             return tuple_of(r.data(), 4);

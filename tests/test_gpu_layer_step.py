@@ -192,6 +192,38 @@ def test_a_captured_training_step():
                 assert torch.equal(a, b) or (a - b).abs().max() <= 2.0 ** -6 * b.abs().max()
 
 
+def test_captures_beside_results_that_hold_the_leaves_are_refused():
+    """Each call with leaves that an eager result of another stream holds on to: refused before anything is launched; captured once that result is gone."""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    randn = lambda *s: torch.randn(s, device="cuda").requires_grad_(True)
+    x, w, wg, wu, logits, tokens = randn(40, 64), randn(64), randn(96, 64), randn(96, 64), randn(40, 1000), torch.zeros(40, dtype=torch.long, device="cuda")
+    calls = [lambda: mc.block_norm(x.detach(), weight=w)[1], lambda: mc.gated_ffn(x.detach(), wg, wu), lambda: mc.token_logprobs(logits, tokens)[0]]
+    leaves = [(w,), (wg, wu), (logits,)]
+    side = torch.cuda.Stream()
+    for call, of in zip(calls, leaves):
+        held = call()
+        want = [d.clone() for d in torch.autograd.grad(held.sum(), of, retain_graph=True)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                torch.zeros(4, device="cuda")
+                with pytest.raises(RuntimeError, match="free them"):
+                    call()
+            del held, graph
+            torch.autograd.grad(call().sum(), of)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                got = torch.autograd.grad(call().sum(), of)
+            for _ in range(2):
+                graph.replay()
+                side.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del graph, got
+
+
 def test_two_streams_at_once():
     """The same calls on two streams that run beside each other: each gets what it gets alone."""
     import torch
