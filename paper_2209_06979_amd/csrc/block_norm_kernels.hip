@@ -519,6 +519,7 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
     float *const mine = a.partial + (int64_t)blockIdx.y * 6 * a.dim + shift;
     int64_t group = first / a.gate_rows, group_end = (group + 1) * a.gate_rows;
     bool fresh = true;
+    const bool through = a.pre && a.dn; // (else the gradient does not see y, which may be infinite)
     for (int64_t row = first; row < end; ++row) {
         const float *of_row = a.partial + (int64_t)a.workgroups * 6 * a.dim + 8 * row;
         const float m1 = of_row[0], r1 = of_row[1], m2 = of_row[2], r2 = of_row[3], mean = of_row[4], dot = of_row[5];
@@ -537,8 +538,8 @@ template <int TYPE, int RTYPE> __global__ __launch_bounds__(COLUMN_THREADS) void
         decode(rdn, dn);
         decode(rdy, dy);
         EACH(k, e) {
-            const float hat1 = (x[e] - m1) * r1, b = hat1 * pw[k][e] + pb[k][e], y = g[k][e] * b + (a.r ? a.residual_scale * r[e] : 0), hat2 = (y - m2) * r2;
-            const float dyt = dy[e] + r2 * (dn[e] * w[k][e] - mean - hat2 * dot), da = g[k][e] * dyt;
+            const float hat1 = (x[e] - m1) * r1, b = hat1 * pw[k][e] + pb[k][e], y = g[k][e] * b + (a.r ? a.residual_scale * r[e] : 0), hat2 = through ? (y - m2) * r2 : 0;
+            const float dyt = through ? dy[e] + r2 * (dn[e] * w[k][e] - mean - hat2 * dot) : dy[e], da = g[k][e] * dyt;
             sum_w[k][e] += dn[e] * hat2;
             sum_b[k][e] += dn[e];
             sum_g[k][e] += a.branch_scale * b * dyt;
