@@ -18,7 +18,8 @@ namespace {
 typedef unsigned long long Key; // an orderable logit, and the complement of its index: larger is earlier
 
 constexpr int THREADS = 256, WAVES = THREADS / 64, UNROLL = 4;
-constexpr float LOWEST = -3.402823466e38f, FAR = -1e30f;
+// FAR: what a difference counts as at most: 2^30 times it is finite, and the smallest scale times it has an exponential of 0.
+constexpr float LOWEST = -3.402823466e38f, FAR = -1e28f;
 
 template <int TYPE> struct Vector {
     typedef typename RealOf<TYPE>::type T;
