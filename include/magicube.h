@@ -708,7 +708,7 @@ int mc_gated_ffn_backward(const mc_gated_ffn_args *args, const void *dh_dev, int
  *   top          0 (top_logprobs_dev and top_tokens_dev may be NULL then) .. 64, at most vocab
  *   sums_dev     rows x 2 floats for the gradient (a row's largest logit, log of its sum), or NULL
  * A logit of -infinity has probability 0 (log probability -infinity).  A row of nothing else has log probabilities of -infinity and entropy 0.  A row that holds a NaN or +infinity has
- * NaN for all of them; its top tokens are in order, NaN above all.  1 <= vocab <= 2^30, scale > 0 and finite; rows * ceil(vocab / 4096) at most 8 million.
+ * NaN for all of them; its top tokens are in order, NaN above all.  1 <= vocab <= 2^30, 2^-64 <= scale < 2.3e38; rows * ceil(vocab / 4096) at most 8 million.
  * The workspace is as for mc_block_norm_backward; mc_token_logprobs_workspace gives its bytes, 0: none is needed. */
 size_t mc_token_logprobs_workspace(int64_t rows, int vocab, mc_type type, int top);
 int mc_token_logprobs(const void *logits_dev, mc_type type, int64_t rows, int vocab, int64_t stride, const int64_t *tokens_dev, float scale, int top,

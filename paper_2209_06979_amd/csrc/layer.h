@@ -61,6 +61,7 @@ struct LogprobArgs {
     int64_t dstride;
 };
 constexpr int LOGPROB_MOST_TOP = 64;
+constexpr float LOGPROB_LEAST_SCALE = 0x1p-64f; // (with smaller ones differences of logits beyond 1e28 would count, which the kernels clamp)
 // A piece's maximum, sum and weighted sum (and one float more), and its keys
 constexpr int logprob_partial(int top) { return 4 + 2 * top; }
 constexpr int LOGPROB_GROUPS_WANTED = 1024; // workgroups that all rows together are cut into, where they are fewer

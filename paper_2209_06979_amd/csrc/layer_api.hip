@@ -289,7 +289,7 @@ namespace {
 int check_logprobs(mc_type type, int64_t rows, int vocab, int64_t stride, float scale, int top)
 {
     if (!valid_type(type)) return MC_EUNSUPPORTED;
-    if (rows < 0 || vocab < 1 || vocab > (1 << 30) || !(scale > 0) || !std::isfinite(scale * 1.4426950408889634f) || top < 0 || top > LOGPROB_MOST_TOP || top > vocab ||
+    if (rows < 0 || vocab < 1 || vocab > (1 << 30) || !(scale >= LOGPROB_LEAST_SCALE) || !std::isfinite(scale * 1.4426950408889634f) || top < 0 || top > LOGPROB_MOST_TOP || top > vocab ||
         (rows > 1 && stride < vocab) || rows > MOST_GROUPS / ((vocab + 4095) / 4096))
         return MC_EINVAL;
     return MC_OK;
