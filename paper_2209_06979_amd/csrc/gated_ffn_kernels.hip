@@ -15,24 +15,28 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 // ---- activations ----------------------------------------------------------------------------------------------------------
-// The hardware's exponential and reciprocal, each within a step or two: of a sigmoid some |g| 2^-23 of itself where it is small.  (With the
-// library's exponential and quotient the activation of a 256 x 128 tile took as long as a seventh of its products.)
-__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)); }
+// Of 16-bit types: the hardware's exponential and reciprocal, each within a step or two: of a sigmoid some |g| 2^-23 of itself where it is small, far below a rounding
+// of h, dg and du.  (With the library's exponential and quotient the activation of a 256 x 128 tile took as long as a seventh of its products.)  fp32 keeps all of its bits.
+template <int TYPE> __device__ __forceinline__ float sigmoid(float g)
+{
+    if constexpr (TYPE == MC_F32) return 1.0f / (1.0f + expf(-g));
+    else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
+}
 constexpr float GELU_A = 0.7978845608028654f, GELU_B = 0.044715f;
 
-template <int KIND> __device__ __forceinline__ float activated(float g)
+template <int KIND, int TYPE> __device__ __forceinline__ float activated(float g)
 {
-    if constexpr (KIND == MC_ACT_SILU) return g * sigmoid(g);
+    if constexpr (KIND == MC_ACT_SILU) return g * sigmoid<TYPE>(g);
     else if constexpr (KIND == MC_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
-    else if constexpr (KIND == MC_ACT_GELU_TANH) return g * sigmoid(2.0f * GELU_A * (g + GELU_B * g * g * g)); // ((1 + tanh v) / 2 is sigmoid 2 v)
+    else if constexpr (KIND == MC_ACT_GELU_TANH) return g * sigmoid<TYPE>(2.0f * GELU_A * (g + GELU_B * g * g * g)); // ((1 + tanh v) / 2 is sigmoid 2 v)
     else if constexpr (KIND == MC_ACT_RELU) return g > 0 ? g : g != g ? g : 0;
-    else return sigmoid(g);
+    else return sigmoid<TYPE>(g);
 }
 // act(g), and its slope
-template <int KIND> __device__ __forceinline__ float activated(float g, float &slope)
+template <int KIND, int TYPE> __device__ __forceinline__ float activated(float g, float &slope)
 {
     if constexpr (KIND == MC_ACT_SILU) {
-        const float p = sigmoid(g);
+        const float p = sigmoid<TYPE>(g);
         slope = p * (1.0f + g * (1.0f - p));
         return g * p;
     } else if constexpr (KIND == MC_ACT_GELU) {
@@ -40,7 +44,7 @@ template <int KIND> __device__ __forceinline__ float activated(float g, float &s
         slope = c + g * __builtin_amdgcn_exp2f(g * g * -0.7213475204444817f) * 0.3989422804014327f;
         return g * c;
     } else if constexpr (KIND == MC_ACT_GELU_TANH) {
-        const float p = sigmoid(2.0f * GELU_A * (g + GELU_B * g * g * g));
+        const float p = sigmoid<TYPE>(2.0f * GELU_A * (g + GELU_B * g * g * g));
         const float q = p * (1.0f - p); // (0 far from 0, where the cube may be infinite)
         slope = q == 0 ? p : p + q * 2.0f * GELU_A * (g + 3.0f * GELU_B * g * g * g);
         return g * p;
@@ -48,7 +52,7 @@ template <int KIND> __device__ __forceinline__ float activated(float g, float &s
         slope = g > 0 ? 1 : g != g ? g : 0;
         return g > 0 ? g : g != g ? g : 0;
     } else {
-        const float p = sigmoid(g);
+        const float p = sigmoid<TYPE>(g);
         slope = p * (1.0f - p);
         return p;
     }
@@ -305,7 +309,7 @@ template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, b
                         for (int e = 0; e < RUN; ++e) {
                             g[e] = acc[n + e / 4][m][e % 4];
                             u[e] = acc[NF / 2 + n + e / 4][m][e % 4];
-                            h[e] = activated<decltype(kind)::value>(g[e]) * u[e];
+                            h[e] = activated<decltype(kind)::value, TYPE>(g[e]) * u[e];
                         }
                         store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
                         if (a.g) {
@@ -575,7 +579,7 @@ template <int TYPE, int MT> __global__ __launch_bounds__(64 * FEW_WAVES) void fe
         for (int e = 0; e < 4; ++e) gs[e] = sg[e], us[e] = su[e];
         with_activation(a.activation, [&](auto kind) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = activated<decltype(kind)::value>(gs[e]) * us[e];
+            for (int e = 0; e < 4; ++e) h[e] = activated<decltype(kind)::value, TYPE>(gs[e]) * us[e];
         });
         store_run(static_cast<T *>(a.h) + row * a.h_stride + column, h, count);
         if (a.g) {
@@ -616,7 +620,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void gated_grad_kernel(Gat
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float slope;
-                const float act = activated<decltype(kind)::value>(gs[e], slope);
+                const float act = activated<decltype(kind)::value, TYPE>(gs[e], slope);
                 du[e] = (float)d[e] * act;
                 dg[e] = (float)d[e] * us[e] * slope;
             }
