@@ -13,6 +13,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
@@ -741,6 +742,19 @@ inline bool array(const at::Tensor &t, at::ScalarType type, int64_t n, const at:
 // what is worked on is on the current device, whose stream the call goes to
 inline bool current(const at::Tensor &t) { return t.device().index() == c10::hip::current_device(); }
 
+// A tangent of forward-mode differentiation, which the calls would drop
+inline bool has_tangent(const at::Tensor &t) { return c10::AutogradState::get_tls_state().get_fw_grad_mode() && t.defined() && t._fw_grad(0).defined(); }
+// Whether one of these carries one: refused.
+bool carries_tangent(const char *what, std::initializer_list<const at::Tensor *> tensors)
+{
+    for (const at::Tensor *x : tensors)
+        if (x && has_tangent(*x)) {
+            PyErr_Format(PyExc_RuntimeError, "%s: there is no derivative in forward mode, and one of the tensors carries a tangent", what);
+            return true;
+        }
+    return false;
+}
+
 Params<7> p_rope = {"rope", 3, {"x", "positions", "inv_freq", "interleaved", "magnitude", "inverse", "out"}, {}};
 
 PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
@@ -761,6 +775,7 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
         if (!(out = tensor(v[6]))) return nullptr;
         if (!(token_major(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->sizes() == x->sizes())) return assertion();
     }
+    if (carries_tangent("rope", {x, freq, out})) return nullptr;
     if (c10::GradMode::is_enabled()) { // gradients are recorded, or the call is refused: never dropped
         if (freq->requires_grad()) {
             PyErr_SetString(PyExc_RuntimeError, "rope: inv_freq requires grad, for which there is no gradient");
@@ -1050,7 +1065,10 @@ at::Tensor as_rows(const at::Tensor &d)
 variable_list once(variable_list &&grads, const variable_list &from)
 {
     bool asked = false;
-    for (const at::Tensor &d : from) asked = asked || (d.defined() && d.requires_grad());
+    for (const at::Tensor &d : from) {
+        TORCH_CHECK(!has_tangent(d), "this gradient has no derivative in forward mode, and what it is given carries a tangent");
+        asked = asked || (d.defined() && d.requires_grad());
+    }
     if (!c10::GradMode::is_enabled() || !asked) return std::move(grads);
     const auto refuse = std::make_shared<torch::autograd::DelayedError>("this gradient has no gradient of its own", (int64_t)grads.size());
     for (at::Tensor &d : grads)
@@ -1175,6 +1193,7 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
         if ((y && !rows_like(*y, *c.t[0], c.stream_type)) || !n != !c.args.pre || (n && !rows_like(*n, *c.t[0], c.t[0]->scalar_type()))) return assertion();
     }
     at::TensorBase made[2];
+    if (carries_tangent("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) return nullptr;
     if (recorded({c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) {
         if (out) return no_out_gradient("block_norm");
         if (captured_beside("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6]})) return nullptr;
@@ -1288,6 +1307,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
     if (out && !(rows_of(*out) && out->device() == c.x->device() && out->scalar_type() == c.x->scalar_type() && out->size(0) == c.x->size(0) && out->size(1) == c.gate->size(0)))
         return assertion();
     if (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous())) return assertion();
+    if (carries_tangent("gated_ffn", {c.x, c.gate, c.up, out})) return nullptr;
     if (recorded({c.x, c.gate, c.up, out})) {
         if (out) return no_out_gradient("gated_ffn");
         if (captured_beside("gated_ffn", {c.x, c.gate, c.up})) return nullptr;
@@ -1381,6 +1401,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     const at::Tensor *ws = nullptr;
     if (!(c.x = tensor(v[0])) || !(c.tokens = tensor(v[1])) || !integer(v[2], 0, &c.top) || (v[3] && !number(v[3], &c.scale)) || !optional(v[4], &ws)) return nullptr;
     if (!c.fill() || (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous()))) return assertion();
+    if (carries_tangent("token_logprobs", {c.x})) return nullptr;
     if (recorded({c.x})) {
         if (captured_beside("token_logprobs", {c.x})) return nullptr;
         try {

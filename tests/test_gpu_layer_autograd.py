@@ -1,0 +1,38 @@
+"""Norms, feed-forward block, log probabilities and rope beside torch's autograd: what they do not serve is refused, and never dropped."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _calls():
+    """(name, call, what it takes): each call takes the tensor that is looked at."""
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    g = torch.Generator(device="cuda").manual_seed(0)
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda")
+    x, w, wg, wu, logits, q = randn(40, 64), randn(64), randn(96, 64), randn(96, 64), randn(40, 1000), randn(40, 2, 64)
+    tokens, positions = torch.zeros(40, dtype=torch.long, device="cuda"), torch.arange(40, device="cuda")
+    freq = torch.rand(32, dtype=torch.float64, device="cuda", generator=g)
+    return [("block_norm", lambda t: mc.block_norm(t, weight=w)[1], x), ("block_norm", lambda t: mc.block_norm(x, weight=t)[1], w), ("block_norm", lambda t: mc.block_norm(t, pre=None, branch_scale=2)[0], x),
+            ("gated_ffn", lambda t: mc.gated_ffn(t, wg, wu), x), ("gated_ffn", lambda t: mc.gated_ffn(x, wg, t), wu), ("token_logprobs", lambda t: mc.token_logprobs(t, tokens)[0], logits),
+            ("rope", lambda t: mc.rope(t, positions, freq), q)]
+
+
+def test_tangents_are_refused():
+    import torch
+    import torch.autograd.forward_ad as fwd
+    for name, call, t in _calls():
+        with fwd.dual_level():
+            dual = fwd.make_dual(t, torch.ones_like(t))
+            with pytest.raises(RuntimeError, match=f"{name}.*forward"):
+                call(dual)
+            with torch.no_grad(), pytest.raises(RuntimeError, match=f"{name}.*forward"):     # (no_grad does not end forward mode)
+                call(dual)
+            with pytest.raises(RuntimeError):
+                call(fwd.make_dual(t.clone().requires_grad_(True), torch.ones_like(t)))
+            call(fwd.unpack_dual(dual).primal)
+            leaf = t.clone().requires_grad_(True)
+            out = call(leaf)
+            with pytest.raises(RuntimeError, match="forward"):                                # forward over reverse
+                torch.autograd.grad((out * fwd.make_dual(torch.ones_like(out), torch.ones_like(out))).sum(), leaf)
+        call(t)
