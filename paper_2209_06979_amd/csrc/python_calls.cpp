@@ -15,6 +15,7 @@
 #include <ATen/core/Tensor.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -23,6 +24,7 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <cmath>
 
@@ -755,6 +757,14 @@ bool carries_tangent(const char *what, std::initializer_list<const at::Tensor *>
     return false;
 }
 
+// Whether torch's operators are being recorded into a program, which would hold this call's results as constants: refused.
+bool traced(const char *what)
+{
+    if (!torch::jit::tracer::isTracing() && !c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY)) return false;
+    PyErr_Format(PyExc_RuntimeError, "%s: cannot be traced: its results would become constants of the trace", what);
+    return true;
+}
+
 Params<7> p_rope = {"rope", 3, {"x", "positions", "inv_freq", "interleaved", "magnitude", "inverse", "out"}, {}};
 
 PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
@@ -775,7 +785,7 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
         if (!(out = tensor(v[6]))) return nullptr;
         if (!(token_major(*out) && out->device() == x->device() && out->scalar_type() == x->scalar_type() && out->sizes() == x->sizes())) return assertion();
     }
-    if (carries_tangent("rope", {x, freq, out})) return nullptr;
+    if (traced("rope") || carries_tangent("rope", {x, freq, out})) return nullptr;
     if (c10::GradMode::is_enabled()) { // gradients are recorded, or the call is refused: never dropped
         if (freq->requires_grad()) {
             PyErr_SetString(PyExc_RuntimeError, "rope: inv_freq requires grad, for which there is no gradient");
@@ -1193,7 +1203,7 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
         if ((y && !rows_like(*y, *c.t[0], c.stream_type)) || !n != !c.args.pre || (n && !rows_like(*n, *c.t[0], c.t[0]->scalar_type()))) return assertion();
     }
     at::TensorBase made[2];
-    if (carries_tangent("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) return nullptr;
+    if (traced("block_norm") || carries_tangent("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) return nullptr;
     if (recorded({c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6], y, n})) {
         if (out) return no_out_gradient("block_norm");
         if (captured_beside("block_norm", {c.t[0], c.t[1], c.t[2], c.t[3], c.t[4], c.t[5], c.t[6]})) return nullptr;
@@ -1307,7 +1317,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
     if (out && !(rows_of(*out) && out->device() == c.x->device() && out->scalar_type() == c.x->scalar_type() && out->size(0) == c.x->size(0) && out->size(1) == c.gate->size(0)))
         return assertion();
     if (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous())) return assertion();
-    if (carries_tangent("gated_ffn", {c.x, c.gate, c.up, out})) return nullptr;
+    if (traced("gated_ffn") || carries_tangent("gated_ffn", {c.x, c.gate, c.up, out})) return nullptr;
     if (recorded({c.x, c.gate, c.up, out})) {
         if (out) return no_out_gradient("gated_ffn");
         if (captured_beside("gated_ffn", {c.x, c.gate, c.up})) return nullptr;
@@ -1401,7 +1411,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     const at::Tensor *ws = nullptr;
     if (!(c.x = tensor(v[0])) || !(c.tokens = tensor(v[1])) || !integer(v[2], 0, &c.top) || (v[3] && !number(v[3], &c.scale)) || !optional(v[4], &ws)) return nullptr;
     if (!c.fill() || (ws && !(ws->is_cuda() && ws->device() == c.x->device() && ws->is_contiguous()))) return assertion();
-    if (carries_tangent("token_logprobs", {c.x})) return nullptr;
+    if (traced("token_logprobs") || carries_tangent("token_logprobs", {c.x})) return nullptr;
     if (recorded({c.x})) {
         if (captured_beside("token_logprobs", {c.x})) return nullptr;
         try {

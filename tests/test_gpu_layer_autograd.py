@@ -36,3 +36,14 @@ def test_tangents_are_refused():
             with pytest.raises(RuntimeError, match="forward"):                                # forward over reverse
                 torch.autograd.grad((out * fwd.make_dual(torch.ones_like(out), torch.ones_like(out))).sum(), leaf)
         call(t)
+
+
+def test_traces_are_refused():
+    import torch
+    from torch.fx.experimental.proxy_tensor import make_fx
+    for name, call, t in _calls():
+        with pytest.raises(RuntimeError, match=f"{name}.*trace"):
+            torch.jit.trace(lambda t: call(t) * 2, (t,), check_trace=False)
+        with pytest.raises(RuntimeError, match=f"{name}.*trace"):
+            make_fx(lambda t: call(t) * 2)(t)
+        call(t)
