@@ -1071,15 +1071,12 @@ at::Tensor as_rows(const at::Tensor &d)
 {
     return !d.defined() || (rows_of(d) && (d.size(0) <= 1 || d.stride(0) >= d.size(1))) ? d : d.contiguous();
 }
-// Gradients that are no functions of theirs: a second derivative is refused, never taken for zero.
+// Gradients that are no functions of theirs: a second derivative is refused, never taken for zero.  (They depend on the forward call's tensors, whether or not what they are made from
+// requires a gradient.)
 variable_list once(variable_list &&grads, const variable_list &from)
 {
-    bool asked = false;
-    for (const at::Tensor &d : from) {
-        TORCH_CHECK(!has_tangent(d), "this gradient has no derivative in forward mode, and what it is given carries a tangent");
-        asked = asked || (d.defined() && d.requires_grad());
-    }
-    if (!c10::GradMode::is_enabled() || !asked) return std::move(grads);
+    for (const at::Tensor &d : from) TORCH_CHECK(!has_tangent(d), "this gradient has no derivative in forward mode, and what it is given carries a tangent");
+    if (!c10::GradMode::is_enabled()) return std::move(grads);
     const auto refuse = std::make_shared<torch::autograd::DelayedError>("this gradient has no gradient of its own", (int64_t)grads.size());
     for (at::Tensor &d : grads)
         if (d.defined()) d.requires_grad_(true);

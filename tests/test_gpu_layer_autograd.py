@@ -47,3 +47,17 @@ def test_traces_are_refused():
         with pytest.raises(RuntimeError, match=f"{name}.*trace"):
             make_fx(lambda t: call(t) * 2)(t)
         call(t)
+
+
+def test_second_derivatives_of_sums_are_refused():
+    """The incoming gradient requires none, the outgoing one depends on the inputs all the same."""
+    import torch
+    for name, call, t in _calls():
+        if name == "rope":                                          # (linear: it has second derivatives, of zero and of dy)
+            continue
+        t = t.clone().requires_grad_(True)
+        d, = torch.autograd.grad(call(t).sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError, match="no gradient of its own"):
+            (call(t).sum() + (d * d).sum()).backward()
+        d, = torch.autograd.grad(call(t).sum(), t)                  # without create_graph: an ordinary tensor
+        assert not d.requires_grad
