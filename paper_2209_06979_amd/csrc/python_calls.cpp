@@ -244,6 +244,12 @@ inline int elements(int64_t containers, const at::Tensor &t, int bits) { return 
 inline bool dense_rows(const at::Tensor &t) { return t.is_cuda() && t.dim() == 2 && t.stride(1) == 1; }
 inline PyObject *wrap(at::TensorBase &&t) { return THPVariable_Wrap(std::move(t)); }
 inline PyObject *same(PyObject *o) { Py_INCREF(o); return o; }
+// A tensor of the caller's has been written to: a backward pass that holds on to what it was is told so (inference tensors have no versions).
+inline void written(const at::Tensor *t)
+{
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+inline PyObject *filled(PyObject *o, const at::Tensor *t) { written(t); return same(o); }
 
 // ---- SpMM --------------------------------------------------------------------------------------------
 Params<7> p_spmm = {"spmm", 3, {"A", "B", "prec", "out", "lhs_unsigned", "rhs_unsigned", "options"}, {}};
@@ -279,7 +285,7 @@ PyObject *spmm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
                       : mc_spmm_flags(A->mat, B->data_ptr(), N, ldb, p->prec, flags, c, ldc, stream());
     }
     if (rc != MC_OK) return status_error(rc, opts.ptr ? "mc_spmm_ex" : "mc_spmm_flags");
-    return out ? same(v[3]) : wrap(std::move(made));
+    return out ? filled(v[3], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -317,7 +323,7 @@ PyObject *spmm_dequant(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyOb
                              (int)(out ? out->stride(0) : N), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_spmm_dequant");
-    return out ? same(v[5]) : wrap(std::move(made));
+    return out ? filled(v[5], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -370,7 +376,7 @@ PyObject *sddmm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *k
                       : mc_sddmm_flags(d.Q->data_ptr(), d.ldq, d.K->data_ptr(), d.ldk, d.Kd, mask->mat, p->prec, flags, s, stream());
     }
     if (rc != MC_OK) return status_error(rc, opts.ptr ? "mc_sddmm_ex" : "mc_sddmm_flags");
-    return out ? same(v[4]) : wrap(std::move(made));
+    return out ? filled(v[4], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -406,7 +412,7 @@ PyObject *sddmm_dequant(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyO
                               out ? out->data_ptr() : made.data_ptr(), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_sddmm_dequant");
-    return out ? same(v[6]) : wrap(std::move(made));
+    return out ? filled(v[6], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -474,7 +480,7 @@ PyObject *absmax(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *
         rc = mc_absmax(static_cast<const float *>(x->data_ptr()), x->numel(), static_cast<float *>(out ? out->data_ptr() : made.data_ptr()), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_absmax");
-    return out ? same(v[1]) : wrap(std::move(made));
+    return out ? filled(v[1], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -509,7 +515,7 @@ PyObject *quantize(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject
         rc = mc_quantize(static_cast<const float *>(x->data_ptr()), x->numel(), scale, bits, out ? out->data_ptr() : made.data_ptr(), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_quantize");
-    return out ? same(v[3]) : wrap(std::move(made));
+    return out ? filled(v[3], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -542,6 +548,7 @@ PyObject *sparse_softmax(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
                                     out ? out->data_ptr() : made.data_ptr(), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_sparse_softmax_bits");
+    written(out);
     return wrap(out ? at::TensorBase(out->reshape(S->sizes())) : std::move(made));
     END_HANDLE_TH_ERRORS
 }
@@ -661,7 +668,7 @@ PyObject *sparse_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, 
                                                 wbytes, stream());
     }
     if (rc != MC_OK) return status_error(rc, opts.ptr ? "mc_sparse_attention_ex" : "mc_sparse_attention_out");
-    return out ? same(v[8]) : wrap(std::move(made));
+    return out ? filled(v[8], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -688,7 +695,7 @@ PyObject *sparse_attention_static(PyObject *, PyObject *const *args, Py_ssize_t 
                                         out->scalar_type() == at::kHalf ? MC_OUT_F16 : MC_OUT_F32, opts.ptr, out->data_ptr(), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_sparse_attention_static");
-    return same(v[8]);
+    return filled(v[8], out);
     END_HANDLE_TH_ERRORS
 }
 
@@ -809,7 +816,7 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
                      out ? out->stride(0) : x->size(1) * x->size(2), out ? out->stride(1) : x->size(2), stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_rope");
-    return out ? same(v[6]) : wrap(std::move(made));
+    return out ? filled(v[6], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -899,6 +906,8 @@ PyObject *cache_read(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
                            k ? w->stride(1) : head, stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_cache_read");
+    written(k);
+    written(w);
     if (k) return same(v[3]);
     PyObject *a = wrap(std::move(made_k)), *b = wrap(std::move(made_v)), *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
     Py_XDECREF(a);
@@ -970,7 +979,7 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, P
                                 out ? out->stride(0) : q->size(1) * q->size(2), out ? out->stride(1) : q->size(2), w, wbytes, stream());
     }
     if (rc != MC_OK) return status_error(rc, "mc_cache_attention");
-    return out ? same(v[8]) : wrap(std::move(made));
+    return out ? filled(v[8], out) : wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }
 
@@ -1220,6 +1229,8 @@ PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
             rc = out ? mc_block_norm(&c.args, data(y), y ? row_stride(*y) : 0, data(n), n ? row_stride(*n) : 0, stream()) : c.run(&made[0], &made[1]);
         }
         if (rc != MC_OK) return status_error(rc, "mc_block_norm");
+        written(y);
+        written(n);
         if (out) return same(v[12]);
     }
     PyObject *a = c.trivial ? same(v[0]) : wrap(std::move(made[0])), *b = wrap_or_none(std::move(made[1])), *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
@@ -1331,7 +1342,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
         rc = c.run(out, ws, false, made);
     }
     if (rc != MC_OK) return status_error(rc, "mc_gated_ffn");
-    return out ? same(v[4]) : wrap(std::move(made[0]));
+    return out ? filled(v[4], out) : wrap(std::move(made[0]));
     END_HANDLE_TH_ERRORS
 }
 

@@ -61,3 +61,30 @@ def test_second_derivatives_of_sums_are_refused():
             (call(t).sum() + (d * d).sum()).backward()
         d, = torch.autograd.grad(call(t).sum(), t)                  # without create_graph: an ordinary tensor
         assert not d.requires_grad
+
+
+def test_a_tensor_that_is_written_to_is_not_taken_for_the_saved_one():
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    randn = lambda *s: torch.randn(s, device="cuda")
+    writes = {"block_norm y": lambda t: mc.block_norm(randn(40, 64), t, out=(t, randn(40, 64))), "block_norm n": lambda t: mc.block_norm(randn(40, 64), out=(None, t)),
+              "gated_ffn": lambda t: mc.gated_ffn(randn(40, 32), randn(64, 32), randn(64, 32), out=t),
+              "rope": lambda t: mc.rope(t.view(40, 1, 64), torch.arange(40, device="cuda"), torch.ones(32, dtype=torch.float64, device="cuda"), out=t.view(40, 1, 64))}
+    cache, slots = mc.KVCache.zeros(4, 16, 1, 64), torch.arange(40, device="cuda")
+    mc.cache_write(cache, randn(40, 1, 64), randn(40, 1, 64), slots)
+    table = torch.zeros((40, 1), dtype=torch.int32, device="cuda")
+    writes["cache_read"] = lambda t: mc.cache_read(cache, slots, out=(randn(40, 1, 64), t.view(40, 1, 64)))
+    writes["cache_attention"] = lambda t: mc.cache_attention(randn(40, 1, 64), cache, table, torch.full((40,), 5, dtype=torch.int32, device="cuda"), out=t.view(40, 1, 64))
+    for what, write in writes.items():
+        saved, w = randn(40, 64), randn(64).requires_grad_(True)
+        for result in ((saved * w).sum(), mc.block_norm(saved, weight=w)[1].sum()):
+            before = saved._version
+            write(saved)
+            assert saved._version > before, what
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                result.backward()
+    with torch.inference_mode():                                    # (tensors without versions are written to as before)
+        t = randn(40, 64)
+        for write in writes.values():
+            write(t)
+    writes["gated_ffn"](t)
