@@ -1275,10 +1275,10 @@ struct FfnCall {
 };
 
 struct FfnNode : torch::autograd::Function<FfnNode> {
-    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &x, const at::Tensor &gate, const at::Tensor &up, const FfnCall &call)
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &x, const at::Tensor &gate, const at::Tensor &up, const FfnCall &call, const at::Tensor *ws)
     {
         at::TensorBase made[3];
-        accept(call.run(nullptr, nullptr, true, made));
+        accept(call.run(nullptr, ws, true, made));
         ctx->save_for_backward({x, gate, up, at::Tensor(made[1]), at::Tensor(made[2])});
         ctx->saved_data["activation"] = (int64_t)call.args.activation;
         return at::Tensor(std::move(made[0]));
@@ -1290,7 +1290,7 @@ struct FfnNode : torch::autograd::Function<FfnNode> {
         c.args.activation = (mc_activation)ctx->saved_data["activation"].toInt();
         TORCH_CHECK(c.fill(), "gated_ffn: the tensors have changed since the forward call");
         const at::Tensor dh = as_rows(given[0]);
-        variable_list grads(4);
+        variable_list grads(5);
         void *to[3] = {};
         for (int i = 0; i < 3; ++i)
             if (ctx->needs_input_grad(i)) {
@@ -1330,7 +1330,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
         if (out) return no_out_gradient("gated_ffn");
         if (captured_beside("gated_ffn", {c.x, c.gate, c.up})) return nullptr;
         try {
-            return wrap(FfnNode::apply(*c.x, *c.gate, *c.up, c));
+            return wrap(FfnNode::apply(*c.x, *c.gate, *c.up, c, ws));
         } catch (const Refused &e) {
             return status_error(e.status, "mc_gated_ffn");
         }
@@ -1376,11 +1376,11 @@ struct LogprobCall {
 };
 
 struct LogprobNode : torch::autograd::Function<LogprobNode> {
-    static variable_list forward(AutogradContext *ctx, const at::Tensor &x, const LogprobCall &call)
+    static variable_list forward(AutogradContext *ctx, const at::Tensor &x, const LogprobCall &call, const at::Tensor *ws)
     {
         ctx->set_materialize_grads(false);
         at::TensorBase made[5];
-        accept(call.run(nullptr, true, made));
+        accept(call.run(ws, true, made));
         variable_list out;
         for (int i = 0; i < 4; ++i) out.emplace_back(made[i]);
         ctx->mark_non_differentiable({out[3]});
@@ -1396,7 +1396,7 @@ struct LogprobNode : torch::autograd::Function<LogprobNode> {
         at::Tensor d[3];
         for (int i = 0; i < 3; ++i) d[i] = given[i].defined() ? given[i].contiguous() : given[i];
         const at::Tensor &x = saved[0];
-        variable_list grads(2);
+        variable_list grads(3);
         grads[0] = at::Tensor(empty(x.sizes(), x.scalar_type(), x));
         check_status(mc_token_logprobs_backward(x.data_ptr(), c.type, x.size(0), (int)x.size(1), row_stride(x), static_cast<const int64_t *>(saved[1].data_ptr()),
                                                 (float)ctx->saved_data["scale"].toDouble(), (int)saved[3].size(1), static_cast<const int64_t *>(saved[3].data_ptr()),
@@ -1423,7 +1423,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     if (recorded({c.x})) {
         if (captured_beside("token_logprobs", {c.x})) return nullptr;
         try {
-            variable_list r = LogprobNode::apply(*c.x, c);
+            variable_list r = LogprobNode::apply(*c.x, c, ws);
             return tuple_of(r.data(), 4);
         } catch (const Refused &e) {
             return status_error(e.status, "mc_token_logprobs");
@@ -1534,12 +1534,13 @@ PyMethodDef functions[] = {
     {"gated_ffn", FAST(gated_ffn),
      "gated_ffn(x, w_gate, w_up, activation='silu', out=None, workspace=None)\n--\n\n"
      "act(x w_gate^T) * (x w_up^T): x (rows, dim), weights (hidden, dim), all fp32, fp16 or bf16; activation 'silu', 'gelu',\n"
-     "'gelu_tanh', 'relu' or 'sigmoid'.  Autograd records it (out must be None then)."},
+     "'gelu_tanh', 'relu' or 'sigmoid'.  out overlaps none of these.  Autograd records it (out must be None then; the workspace is the forward call's alone)."},
     {"token_logprobs", FAST(token_logprobs),
      "token_logprobs(logits, tokens, top=0, scale=1.0, workspace=None)\n--\n\n"
      "(log probabilities of the tokens, entropies, log probabilities of the `top` most likely tokens, these tokens) of rows of\n"
      "scale * logits (rows, vocab) fp32, fp16 or bf16: (rows,), (rows,), (rows, top) fp32 and (rows, top) int64.  tokens (rows,) int64, those\n"
-     "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three."},
+     "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three\n"
+     "(the workspace is the forward call's alone)."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};

@@ -88,3 +88,22 @@ def test_a_tensor_that_is_written_to_is_not_taken_for_the_saved_one():
         for write in writes.values():
             write(t)
     writes["gated_ffn"](t)
+
+
+def test_the_workspace_is_taken_where_gradients_are_recorded():
+    import torch
+    from paper_2209_06979_amd import binding as mc
+    x, wg, wu = (torch.randn(s, device="cuda").requires_grad_(True) for s in ((200, 63), (40, 63), (40, 63)))
+    logits, tokens = torch.randn((2, 50000), device="cuda").requires_grad_(True), torch.tensor([3, 4], device="cuda")
+    for call, leaves in ((lambda ws: mc.gated_ffn(x, wg, wu, workspace=ws), (x, wg, wu)), (lambda ws: mc.token_logprobs(logits, tokens, top=3, workspace=ws)[0], (logits,))):
+        for small in (torch.zeros(64, dtype=torch.uint8, device="cuda"),):
+            with pytest.raises(mc.MagicubeError):
+                call(small)
+            with torch.no_grad(), pytest.raises(mc.MagicubeError):
+                call(small)
+        ws = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+        out = call(ws)
+        assert bool(ws.any())
+        ws.fill_(255)                                               # nothing of the gradient lies in it
+        want = call(None)
+        assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out.sum(), leaves), torch.autograd.grad(want.sum(), leaves)))
