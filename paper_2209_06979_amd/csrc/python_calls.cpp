@@ -17,6 +17,7 @@
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -1031,7 +1032,7 @@ bool recorded(std::initializer_list<const at::Tensor *> tensors)
 // stream wait inside the capture, which torch cannot undo (the process ends).  Refused, with what to do.
 bool captured_beside(const char *what, std::initializer_list<const at::Tensor *> tensors)
 {
-    const c10::Stream here = c10::hip::getCurrentHIPStream().unwrap();
+    const c10::Stream here = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA().unwrap(); // (as autograd's nodes name theirs)
     for (const at::Tensor *x : tensors) {
         if (!x || !x->requires_grad() || !x->is_leaf()) continue;
         const auto node = torch::autograd::impl::try_get_grad_accumulator(*x);
