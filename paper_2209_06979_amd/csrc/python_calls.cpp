@@ -23,11 +23,13 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/graph_task.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include <cmath>
+#include <unordered_set>
 
 #include "../../include/magicube.h"
 
@@ -1028,8 +1030,20 @@ bool recorded(std::initializer_list<const at::Tensor *> tensors)
             if (x && x->requires_grad()) return true;
     return false;
 }
-// Whether this call is being captured while a graph from outside, of another stream, holds on to a leaf: the backward pass would make that
-// stream wait inside the capture, which torch cannot undo (the process ends).  Refused, with what to do.
+// Whether a stream is being captured
+bool capturing(hipStream_t s)
+{
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone;
+}
+// Whether a node of this stream is outside the capture of `here`: a backward pass that goes on to it would make it wait inside the capture, which torch cannot undo (the process ends).
+bool outside(const std::optional<c10::Stream> &there, const c10::Stream &here)
+{
+    if (!there || *there == here) return false;
+    const hipStream_t s = c10::hip::HIPStreamMasqueradingAsCUDA(*there).stream();
+    return !s || !capturing(s);
+}
+// Whether this call is being captured while results from outside hold on to a leaf that it takes.  Refused, with what to do.
 bool captured_beside(const char *what, std::initializer_list<const at::Tensor *> tensors)
 {
     const c10::Stream here = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA().unwrap(); // (as autograd's nodes name theirs)
@@ -1039,14 +1053,36 @@ bool captured_beside(const char *what, std::initializer_list<const at::Tensor *>
         if (!node) continue;
         const std::optional<c10::Stream> there = node->stream();
         if (!there || *there == here) continue;
-        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-        if (hipStreamIsCapturing(static_cast<hipStream_t>(stream()), &status) != hipSuccess || status != hipStreamCaptureStatusNone) {
-            PyErr_Format(PyExc_RuntimeError, "%s: captured while results of another stream still hold on to one of the tensors that require grad: free them before the capture", what);
-            return true;
-        }
-        return false;
+        if (!capturing(static_cast<hipStream_t>(stream()))) return false;
+        if (!outside(there, here)) continue;
+        PyErr_Format(PyExc_RuntimeError, "%s: captured while results of another stream still hold on to one of the tensors that require grad: free them before the capture", what);
+        return true;
     }
     return false;
+}
+// The same in a backward pass that is being captured, for what lies behind views, casts and other operators: everything that this pass still comes to is looked at before anything of it runs.
+void check_capture(const char *what)
+{
+    if (!capturing(static_cast<hipStream_t>(stream()))) return;
+    const c10::Stream here = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA().unwrap(); // (as autograd's nodes name theirs)
+    const auto *wanted = torch::autograd::get_current_graph_task_exec_info(); // (empty: all of it)
+    const std::shared_ptr<torch::autograd::Node> self = torch::autograd::get_current_node();
+    std::unordered_set<const torch::autograd::Node *> seen;
+    std::vector<torch::autograd::Node *> from = {self.get()};
+    while (!from.empty()) {
+        torch::autograd::Node *node = from.back();
+        from.pop_back();
+        for (const torch::autograd::Edge &edge : node->next_edges()) {
+            torch::autograd::Node *next = edge.function.get();
+            if (!next || !seen.insert(next).second) continue;
+            if (wanted && !wanted->empty()) {
+                const auto at = wanted->find(next);
+                if (at == wanted->end() || !at->second.should_execute()) continue;
+            }
+            TORCH_CHECK(!outside(next->stream(), here), what, ": captured while results of another stream still hold on to a tensor that requires grad and this backward pass comes to: free them before the capture");
+            from.push_back(next);
+        }
+    }
 }
 PyObject *no_out_gradient(const char *what)
 {
@@ -1156,6 +1192,7 @@ struct NormNode : torch::autograd::Function<NormNode> {
     }
     static variable_list backward(AutogradContext *ctx, variable_list given)
     {
+        check_capture("block_norm");
         const variable_list saved = ctx->get_saved_variables();
         const std::vector<double> v = ctx->saved_data["call"].toDoubleVector();
         NormCall c;
@@ -1286,6 +1323,7 @@ struct FfnNode : torch::autograd::Function<FfnNode> {
     }
     static variable_list backward(AutogradContext *ctx, variable_list given)
     {
+        check_capture("gated_ffn");
         const variable_list saved = ctx->get_saved_variables();
         FfnCall c = {&saved[0], &saved[1], &saved[2]};
         c.args.activation = (mc_activation)ctx->saved_data["activation"].toInt();
@@ -1391,6 +1429,7 @@ struct LogprobNode : torch::autograd::Function<LogprobNode> {
     }
     static variable_list backward(AutogradContext *ctx, variable_list given)
     {
+        check_capture("token_logprobs");
         const variable_list saved = ctx->get_saved_variables();
         LogprobCall c = {&saved[0], &saved[1]};
         TORCH_CHECK(c.fill(), "token_logprobs: the tensors have changed since the forward call");
