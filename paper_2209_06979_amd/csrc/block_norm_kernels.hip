@@ -659,7 +659,10 @@ template <int TYPE, int RTYPE, bool LAYER> hipError_t backward_kind(const NormAr
     if (a.dim <= 1024) return backward<TYPE, RTYPE, 128, 1, LAYER, true>(a, s);
     if (a.dim <= 2048) return backward<TYPE, RTYPE, 256, 1, LAYER, true>(a, s);
     if (a.dim <= 4096) return backward<TYPE, RTYPE, 512, 1, LAYER, true>(a, s);
-    if (a.dim <= 8192) return !LAYER && TYPE != MC_F32 ? backward<TYPE, RTYPE, 512, 2, LAYER, true>(a, s) : backward<TYPE, RTYPE, 1024, 1, LAYER, false>(a, s);
+    if (a.dim <= 8192) {
+        if constexpr (!LAYER && TYPE != MC_F32) return backward<TYPE, RTYPE, 512, 2, LAYER, true>(a, s);
+        else return backward<TYPE, RTYPE, 1024, 1, LAYER, false>(a, s);
+    }
     return backward<TYPE, RTYPE, 1024, 2, LAYER, false>(a, s);
 }
 template <int TYPE, int RTYPE> hipError_t backward_of(const NormArgs &a, hipStream_t s)
