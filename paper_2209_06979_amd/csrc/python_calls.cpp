@@ -1030,32 +1030,28 @@ bool recorded(std::initializer_list<const at::Tensor *> tensors)
             if (x && x->requires_grad()) return true;
     return false;
 }
-// Whether a stream is being captured
-bool capturing(hipStream_t s)
+// Whether what this thread calls is being captured
+bool capturing()
 {
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    return hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing(static_cast<hipStream_t>(stream()), &status) != hipSuccess || status != hipStreamCaptureStatusNone;
 }
-// Whether a node of this stream is outside the capture of `here`: a backward pass that goes on to it would make it wait inside the capture, which torch cannot undo (the process ends).
-bool outside(const std::optional<c10::Stream> &there, const c10::Stream &here)
+// Whether a node lives on the default stream, which can take no part in a capture: a captured backward pass that goes on to it would make it wait, which torch cannot undo (the process
+// ends).  (Any other stream joins the capture, and is waited for at the backward pass's end.)
+bool on_default_stream(torch::autograd::Node &node)
 {
-    if (!there || *there == here) return false;
-    const hipStream_t s = c10::hip::HIPStreamMasqueradingAsCUDA(*there).stream();
-    return !s || !capturing(s);
+    const std::optional<c10::Stream> there = node.stream();
+    return there && !c10::hip::HIPStreamMasqueradingAsCUDA(*there).stream(); // (autograd names its streams by CUDA's device type)
 }
-// Whether this call is being captured while results from outside hold on to a leaf that it takes.  Refused, with what to do.
+// Whether this call is being captured while results of the default stream hold on to a leaf that it takes.  Refused, with what to do.
 bool captured_beside(const char *what, std::initializer_list<const at::Tensor *> tensors)
 {
-    const c10::Stream here = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA().unwrap(); // (as autograd's nodes name theirs)
     for (const at::Tensor *x : tensors) {
         if (!x || !x->requires_grad() || !x->is_leaf()) continue;
         const auto node = torch::autograd::impl::try_get_grad_accumulator(*x);
-        if (!node) continue;
-        const std::optional<c10::Stream> there = node->stream();
-        if (!there || *there == here) continue;
-        if (!capturing(static_cast<hipStream_t>(stream()))) return false;
-        if (!outside(there, here)) continue;
-        PyErr_Format(PyExc_RuntimeError, "%s: captured while results of another stream still hold on to one of the tensors that require grad: free them before the capture", what);
+        if (!node || !on_default_stream(*node)) continue;
+        if (!capturing()) return false;
+        PyErr_Format(PyExc_RuntimeError, "%s: captured while results of the default stream still hold on to one of the tensors that require grad: free them before the capture", what);
         return true;
     }
     return false;
@@ -1063,8 +1059,7 @@ bool captured_beside(const char *what, std::initializer_list<const at::Tensor *>
 // The same in a backward pass that is being captured, for what lies behind views, casts and other operators: everything that this pass still comes to is looked at before anything of it runs.
 void check_capture(const char *what)
 {
-    if (!capturing(static_cast<hipStream_t>(stream()))) return;
-    const c10::Stream here = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA().unwrap(); // (as autograd's nodes name theirs)
+    if (!capturing()) return;
     const auto *wanted = torch::autograd::get_current_graph_task_exec_info(); // (empty: all of it)
     const std::shared_ptr<torch::autograd::Node> self = torch::autograd::get_current_node();
     std::unordered_set<const torch::autograd::Node *> seen;
@@ -1079,7 +1074,8 @@ void check_capture(const char *what)
                 const auto at = wanted->find(next);
                 if (at == wanted->end() || !at->second.should_execute()) continue;
             }
-            TORCH_CHECK(!outside(next->stream(), here), what, ": captured while results of another stream still hold on to a tensor that requires grad and this backward pass comes to: free them before the capture");
+            TORCH_CHECK(!on_default_stream(*next), what,
+                        ": captured while results of the default stream still hold on to a tensor that requires grad and this backward pass comes to: free them before the capture");
             from.push_back(next);
         }
     }
