@@ -642,7 +642,7 @@ typedef enum { MC_NORM_NONE = 0, MC_NORM_RMS = 1, MC_NORM_LAYER = 2 } mc_norm_ki
  *   weight_dev, bias_dev, post_weight_dev, post_bias_dev   dim elements of param_type (`type` or MC_F32); NULL: ones, zeros.  Not given for a norm that there is not
  *   gate_dev       gate_groups rows of param_type; rows / gate_groups consecutive rows share one (gate_groups divides rows; 1: one for all).  NULL: ones, gate_groups 0
  * 1 <= dim <= 16384, rows up to 2^31 - 1, eps >= 0, scales finite.  A row that holds an infinity or a NaN becomes NaN in part or whole, and no other does.  Squares
- * are fp32: a row with elements beyond 2^63 is 0 or NaN. */
+ * are fp32: a row with elements beyond 2^63 is 0 or NaN, and of elements below 2^-63 only eps is left under the root. */
 typedef struct mc_block_norm_args {
     int64_t rows;
     int dim;
@@ -675,7 +675,8 @@ int mc_block_norm_backward(const mc_block_norm_args *args, const void *dy_dev, i
 /* The gated feed-forward block: h = act(x Wg^T) * (x Wu^T), rows x dim against two hidden x dim weights, and its gradient
  *   dg = dh * u * act'(g),  du = dh * act(g)  (g = x Wg^T, u = x Wu^T),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
  * Products of 16-bit types take whole elements and add in fp32, those of fp32 are fp32 throughout; h comes from the unrounded g and u.  For the gradient g and u
- * are kept in fp32; dg and du are rounded to the type, once, before the products.
+ * are kept in fp32 (rows x hidden x 8 bytes); dg and du are rounded to the type, once, before the products (beyond fp16's range they are infinite) and lie in the
+ * gradient's workspace.  Activations of fp32 calls are fp32 throughout; those of 16-bit types are off by some |g| 2^-23 of themselves where a sigmoid is small.
  *   MC_ACT_SILU v sigmoid(v), MC_ACT_GELU v Phi(v), MC_ACT_GELU_TANH v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2, MC_ACT_RELU max(v, 0) (slope 0 at 0), MC_ACT_SIGMOID
  * 1 <= dim, hidden <= 2^20, rows up to 2^21 (0 is accepted: the weights' gradients are zeros then), all products of two of these at most 2^34; rows of x and of the weights
  * are less than 16 MiB apart. */

@@ -197,8 +197,10 @@ __device__ __forceinline__ uint64_t here(unsigned x)
 struct Work { int m0, n0, z, split, first, steps; };
 
 // The matrix units bound it, and tiles as large as the registers hold (256 x 256 of 16-bit types: 128 accumulators a lane) have the fewest bytes from LDS to a product.  8192 rows of 4096
-// bf16: h of 14336 in 1440 us, 1336 Tflop/s (a library's 8192^3 product on the same card 1320); with g and u kept h of 11008 in 1232, dx 1104 (1338 Tflop/s), both weights' gradients 1354 (1091: all operands are
-// transposed on their way out of LDS).  fp32, 777 rows of 1001 to 2731: 103, 105 and 90 us, 82 Tflop/s (a library's 4096^3 132): 440 tiles of 64 x 64 are not quite two rounds.
+// bf16: h of 14336 in 1430 .. 1480 us, 1300 .. 1345 Tflop/s (a library's 8192^3 product on the same card 1320); with g and u kept h of 11008 in 1232, dx 1104 (1338 Tflop/s), both weights' gradients 1354 (1091: all operands are
+// transposed on their way out of LDS).  fp32, 777 rows of 1001 to 2731: 103, 105 and 90 us, 82 Tflop/s (a library's 4096^3 132): 1118 tiles of 64 x 64 for
+// h, 208 of them in six pieces along k for dx, 704 of 128 x 64 for the weights are 4.4, 4.9 and 2.75 to a compute unit, and the slowest unit has five, five and three.  Operands that have to be
+// copied first: 777 rows of bf16, 1001 to 2731 28 us where 1000 to 2736 take 19, both passes 87 and 77; 8192 rows of 4095 to 11008, both passes, 4199 and (4096) 3994.
 // BM x BN tiles, WM x WN waves, NS stages of STEP bytes of k.  GATED: the rows of B are half gate's, half up's, such that each wave has both of its columns; where it has 32 of
 // them, a lane's eight neighbouring ones.
 template <int TYPE, int BM, int BN, int WM, int WN, int STEP, int NS, bool AR, bool BR, int MODE> __global__ __launch_bounds__(64 * WM *WN) void product_kernel(ProductArgs a)
@@ -525,7 +527,8 @@ template <class T> __device__ __forceinline__ v4i load_piece(const T *p, int cou
 }
 
 constexpr int FEW_WAVES = 4;
-// MT tiles of 16 rows of x against 16 rows of either weight, whose pieces go straight into registers: the weights' bytes bound it (1 row of 4096 to 11008 bf16, 180 MB: 31 us, 5.8 TB/s).  The
+// MT tiles of 16 rows of x against 16 rows of either weight, whose pieces go straight into registers: the weights' bytes bound it (1 row of 4096 to 11008 bf16, 180 MB: 31 us, 5.8 TB/s;
+// whole calls of fp32, 361 MB: 1 row 73 us, 16 rows 87, 48 rows 116).  The
 // waves take turns along k, and their sums meet in LDS.
 template <int TYPE, int MT> __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(FewRowsArgs a)
 {

@@ -53,7 +53,7 @@ struct LogprobArgs {
     int64_t *top_tokens;
     int pieces;                    // pieces of a row
     int piece_vectors;             // vectors of 16 bytes of a piece
-    float *partial;                // pieces of all rows x LOGPROB_PARTIAL
+    float *partial;                // rows x pieces x logprob_partial(top) floats
     // backward
     const float *dlogprobs, *dentropy, *dtop; // null: zeros
     const int64_t *chosen;         // rows x top
@@ -62,7 +62,7 @@ struct LogprobArgs {
 };
 constexpr int LOGPROB_MOST_TOP = 64;
 constexpr float LOGPROB_LEAST_SCALE = 0x1p-64f; // (with smaller ones differences of logits beyond 1e28 would count, which the kernels clamp)
-// A piece's maximum, sum and weighted sum (and one float more), and its keys
+// Floats of a piece: its maximum, sum and weighted sum (and one float more), and its keys of 64 bits (an even number, for their alignment)
 constexpr int logprob_partial(int top) { return 4 + 2 * top; }
 constexpr int LOGPROB_GROUPS_WANTED = 1024; // workgroups that all rows together are cut into, where they are fewer
 constexpr int LOGPROB_LEAST_VECTORS = 1024; // vectors of a piece: four a thread (512, 1024, 2048: 1 x 131072 bf16 with 20 alternatives 17.1, 14.3, 16.8 us; 64 x 32000 with 5 13.6, 12.2, 14.1)
@@ -124,8 +124,8 @@ struct PadRowsArgs { // rows of `width` elements into rows of `padded`, zeros be
     int count, width, padded;
 };
 constexpr int FEW_ROWS = 64;
-// Up to 64 rows go to the kernel that cuts k among waves and copies nothing where the tiles of 64 x 64 would be fewer than compute units, or weights would have to be copied
-// for them.  That kernel and the tiles, bf16, us: 16 rows of 4096 to 4096 18.3, 27.8, 64 rows 30.8, 28.6; 16 rows of 1024 to 2816 5.9, 9.2; fp16 1 row of 4096 to 14336 49.5, 47.8,
+// Few rows go to the kernel that cuts k among waves and copies nothing: up to 64 where weights would have to be copied for the tiles, up to 32 where tiles of 64 x 64 (32 columns of
+// h each) would be no more than compute units, up to 4 where they would be no more than 1.5 times as many.  That kernel and the tiles, bf16, us: 16 rows of 4096 to 4096 18.3, 27.8, 64 rows 30.8, 28.6; 16 rows of 1024 to 2816 5.9, 9.2; fp16 1 row of 4096 to 14336 49.5, 47.8,
 // 16 rows 57.8, 47.6, 48 rows 85.3, 52.5; bf16 1 row of 4096 to 11008 35.4, 37.2.
 inline bool few_rows_best(int64_t rows, int hidden, bool copies)
 {

@@ -1566,17 +1566,19 @@ PyMethodDef functions[] = {
      "returns (y, n).  x (rows, dim) fp32, fp16 or bf16, residual the same or fp32 (y has its type); pre and post 'rms', 'layer' or None (n is\n"
      "None without pre); weights and biases (dim,), gate (dim,) or (groups, dim), each row for rows / groups consecutive rows, all of one\n"
      "type (x's or fp32).  y is x itself where there is nothing to add or to scale.  out: a tuple (y or None, n) to write to; y may be the\n"
-     "residual, or either may be x.  Autograd records it (out must be None then)."},
+     "residual, or either may be x.  Autograd records it (out must be None then): first derivatives, backward.  Under capture, results of the\n"
+     "default stream must not hold on to its leaves."},
     {"gated_ffn", FAST(gated_ffn),
      "gated_ffn(x, w_gate, w_up, activation='silu', out=None, workspace=None)\n--\n\n"
      "act(x w_gate^T) * (x w_up^T): x (rows, dim), weights (hidden, dim), all fp32, fp16 or bf16; activation 'silu', 'gelu',\n"
-     "'gelu_tanh', 'relu' or 'sigmoid'.  out overlaps none of these.  Autograd records it (out must be None then; the workspace is the forward call's alone)."},
+     "'gelu_tanh', 'relu' or 'sigmoid'.  out overlaps none of these.  Autograd records it as block_norm (out must be\n"
+     "None then; the workspace is the forward call's alone)."},
     {"token_logprobs", FAST(token_logprobs),
      "token_logprobs(logits, tokens, top=0, scale=1.0, workspace=None)\n--\n\n"
      "(log probabilities of the tokens, entropies, log probabilities of the `top` most likely tokens, these tokens) of rows of\n"
      "scale * logits (rows, vocab) fp32, fp16 or bf16: (rows,), (rows,), (rows, top) fp32 and (rows, top) int64.  tokens (rows,) int64, those\n"
-     "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three\n"
-     "(the workspace is the forward call's alone)."},
+     "that are not 0 .. vocab - 1 are none (log probability 0).  Equal logits: the lower token first.  Autograd records the first three,\n"
+     "as block_norm (the workspace is the forward call's alone)."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "The binding's compute calls over the C ABI of libmagicube.so.", -1, functions};
