@@ -107,11 +107,13 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float c)
     const float fa = __builtin_amdgcn_exp2f(da * c), fb = __builtin_amdgcn_exp2f(db * c);
     return {m, a.s * fa + b.s * fb, (a.t + a.s * da) * fa + (b.t + b.s * db) * fb};
 }
+// Of all lanes, the same in each (their sums by themselves may differ by a rounding: equal logits would have unequal log probabilities)
 __device__ __forceinline__ Sums over_lanes(Sums a, float c)
 {
 #pragma unroll
     for (int j = 32; j > 0; j >>= 1) a = joined(a, {__shfl_xor(a.m, j), __shfl_xor(a.s, j), __shfl_xor(a.t, j)}, c);
-    return a;
+    auto first = [](float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); };
+    return {first(a.m), first(a.s), first(a.t)};
 }
 
 // One wave writes a row's results.
